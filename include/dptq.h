@@ -17,7 +17,9 @@
  * (Section 4.2), the same 4-bit x 4-bit product on the FP6 matrix cores,
  * and variants of the path: randomized-sign (QuaRot-style) rotation, decode
  * from fp16 activations in one launch, and the range quantizer of Eq. 1 with
- * a zero point.
+ * a zero point.  What a serving step needs beside its linears: the norm that
+ * gives 8-bit activations, an 8-bit paged KV cache with the attention that
+ * reads it, and log probabilities of tokens.
  *
  * Conventions shared by every entry point
  *   - Every pointer named "device" is GPU memory owned by the caller; the
@@ -349,6 +351,167 @@ int dptq_kv_quant(const void* kv, int64_t T, int64_t D, int32_t group, uint8_t* 
  */
 int dptq_kv_dequant(const uint8_t* codes, const float* scales, const float* mins, int64_t T,
                     int64_t D, int32_t group, void* kv_out, void* stream);
+
+/*
+ * dptq_rms_norm_quant - residual addition, RMS norm, and 8-bit codes with a
+ * scale per row: the 8-bit activations of dptq_qlinear where the rotation has
+ * been absorbed into the weights around it (weights prepared with had_size 1).
+ *
+ *   h      = fl16(x + residual)             (h = x where residual is NULL)
+ *   t_k    = h_k * weight_k                 (exact in fp32)
+ *   s      = fl32(max|t| / 127)
+ *   code_k = RNE(fl32(t_k / s))             (0 where s = 0)
+ *   scale  = fl32(s * r), r = 1 / sqrt(sum(h^2) / K + eps)     (0 where s = 0)
+ *
+ * code * scale stands for the normalised row r * h * weight.  The codes do not
+ * depend on r, and so on no order of summation.
+ *
+ *   x, residual  device, fp16 [M, K]; residual may be NULL
+ *   weight       device, fp16 [K]
+ *   M            rows, >= 0 (M = 0 enqueues nothing)
+ *   K            multiple of 8, 8 <= K <= 65536
+ *   eps          >= 0, finite
+ *   sum          device, fp16 [M, K] output h; may be x or residual; required
+ *                with a residual, NULL without
+ *   codes        device, int8 [M, K] output
+ *   scales       device, float [M] output
+ *
+ * Non-finite inputs, and sums beyond fp16's range, give unspecified codes and
+ * scales in their rows.
+ */
+int dptq_rms_norm_quant(const void* x, const void* residual, const void* weight, int64_t M, int64_t K,
+                        float eps, void* sum, int8_t* codes, float* scales, void* stream);
+
+/*
+ * The 8-bit paged KV cache of dptq_kv8_append and dptq_kv8_attention.
+ *
+ * A page holds DPTQ_KV8_PAGE tokens of every KV head:
+ *   k_pages  device, uint8 [num_pages, kv_heads, 64, head_dim]   OCP e4m3 codes
+ *   v_pages  device, uint8 [num_pages, kv_heads, head_dim, 64]   the same, channel-major
+ *   k_scales, v_scales  device, float [num_pages, kv_heads]
+ * The value of a code is code * scale; scales are positive powers of two.
+ * head_dim is 64, 128 or 256.
+ *
+ * B sequences, each with new tokens and a length that counts them:
+ *   cu_seqlens  device, int32 [B + 1]: the new tokens of sequence b are rows
+ *               cu_seqlens[b] to cu_seqlens[b + 1] - 1 of k, v and q; starts at
+ *               0, does not decrease and ends at T
+ *   lengths     device, int32 [B]: the tokens of sequence b, the new ones
+ *               included: those stand at its last positions
+ *   page_table  device, int32 [B, max_pages]: the page of tokens 64 i to
+ *               64 i + 63 of sequence b at [b, i].  Entries past the sequence's
+ *               end are not read.  Tokens whose entry is outside [0, num_pages),
+ *               or that lie beyond max_pages, are neither written nor seen.
+ *
+ * These three are read on the device when the call's work runs; offsets and
+ * lengths out of range are clamped.  k_pages, v_pages and the activations must
+ * be 16-byte aligned, all else to its elements.
+ */
+#define DPTQ_KV8_PAGE 64
+
+/*
+ * dptq_kv8_append - writes the new tokens' keys and values into the cache.
+ *
+ * For each page that new tokens fall into, each head, and K and V apart, with a
+ * the largest |x| of the page's new tokens:
+ *
+ *   e    = the smallest integer >= -32 with a <= 448 * 2^e
+ *   s    = max(2^e, scale of the page)      (2^e where the page's first slot is new)
+ *   code = e4m3(x / s), half to even; the page's older codes become
+ *          e4m3(code * scale / s), which changes them only where they fall below
+ *          e4m3's normal range
+ *
+ * The slots after the last token of a page whose first slot is new are cleared;
+ * those of other pages stay as they are.  A page takes new tokens of one
+ * sequence only in one call.
+ *
+ *   k, v        device, fp16 [T, kv_heads, head_dim], ld_k and ld_v elements
+ *               from a token to the next (multiples of 8, >= kv_heads * head_dim)
+ *   T           new tokens of all sequences, 0 <= T < 2^30
+ *   max_new     the most new tokens of a sequence, as far as the caller knows:
+ *               sizes the launch and changes no result (0: T)
+ *   B           sequences, 0 <= B <= 65535; kv_heads <= 1024
+ *
+ * The same call again leaves the cache as it is.  Non-finite inputs give
+ * unspecified codes in the pages they fall into.
+ */
+int dptq_kv8_append(const void* k, int64_t ld_k, const void* v, int64_t ld_v, int64_t T,
+                    const int32_t* cu_seqlens, const int32_t* lengths, int64_t B,
+                    const int32_t* page_table, int64_t max_pages, int64_t num_pages, int32_t kv_heads,
+                    int32_t head_dim, uint8_t* k_pages, uint8_t* v_pages, float* k_scales,
+                    float* v_scales, int64_t max_new, void* stream);
+
+/*
+ * dptq_kv8_attention - attention of the new tokens' queries over the cache,
+ * which holds their keys and values already.
+ *
+ * A query at position p sees positions j <= p; with window > 0 only those with
+ * j > p - window or j < sinks.  Per query head a of KV head a / (heads / kv_heads):
+ *
+ *   S_j = scale * k_scale * (q . k_code_j),   P = softmax(S over the j it sees)
+ *   out = fl16(sum_j P_j * v_scale * v_code_j),   lse = log sum_j exp(S_j)
+ *
+ * Products and sums in fp32, P rounded to fp16.  A query that sees nothing
+ * gives out 0 and lse -inf.  What a masked slot past the sequence's end holds
+ * does not matter, NaN included.
+ *
+ *   q           device, fp16 [T, heads, head_dim], ld_q elements from a token to
+ *               the next (a multiple of 8, >= heads * head_dim)
+ *   heads       a multiple of kv_heads
+ *   scale       finite
+ *   window      >= 0 (0: none), sinks >= 0; both < 2^30
+ *   max_q       the most queries of a sequence, max_len the longest sequence, as
+ *               far as the caller knows: they size the launch and change no
+ *               result beyond the order of fp32 sums (0: T, and 64 * max_pages)
+ *   out         device, fp16 [T, heads, head_dim] output, dense
+ *   lse         device, float [T, heads] output
+ *   workspace   device, 16-byte aligned, dptq_kv8_attention_workspace bytes for
+ *               the same sizes (NULL where that is 0)
+ */
+int64_t dptq_kv8_attention_workspace(int64_t T, int64_t B, int64_t max_pages, int32_t heads,
+                                     int32_t kv_heads, int32_t head_dim, int32_t window, int32_t sinks,
+                                     int64_t max_q, int64_t max_len); /* -1: invalid arguments */
+int dptq_kv8_attention(const void* q, int64_t ld_q, int64_t T, const int32_t* cu_seqlens,
+                       const int32_t* lengths, int64_t B, const int32_t* page_table, int64_t max_pages,
+                       int64_t num_pages, int32_t heads, int32_t kv_heads, int32_t head_dim,
+                       const uint8_t* k_pages, const uint8_t* v_pages, const float* k_scales,
+                       const float* v_scales, float scale, int32_t window, int32_t sinks,
+                       int64_t max_q, int64_t max_len, void* out, float* lse, void* workspace,
+                       int64_t workspace_bytes, void* stream);
+
+/*
+ * dptq_token_logprobs - log probabilities of given tokens under softmax(logits),
+ * the entropy of each row, and its most likely tokens.
+ *
+ *   lse         = log sum_v exp(x_v)
+ *   logprob     = x_token - lse       (0 for a negative token: not scored; NaN
+ *                 for a token >= V)
+ *   entropy     = -sum_v p_v log p_v
+ *   top_ids     = the indices of the `top` largest logits, largest first, equal
+ *                 ones by index; top_logprobs = their x - lse
+ *
+ * Sums in fp32.  A logit of -inf is masked: probability 0, log probability -inf.
+ * A row of nothing else has entropy 0.  Rows that hold NaN or +inf give
+ * unspecified values and indices in [0, V).
+ *
+ *   logits      device, fp16 (dtype DPTQ_F16) or float (DPTQ_F32) [M, V], ld
+ *               elements from a row to the next (>= V), aligned to its elements
+ *   M           rows, 0 <= M < 2^31; V: 1 <= V < 2^30
+ *   tokens      device, int64 [M]
+ *   top         0 <= top <= min(V, DPTQ_MAX_TOP)
+ *   logprobs, entropy  device, float [M] outputs
+ *   top_logprobs, top_ids  device, float and int64 [M, top] outputs (NULL where
+ *               top = 0)
+ *   workspace   device, 16-byte aligned, dptq_token_logprobs_workspace bytes
+ *               (NULL where that is 0)
+ */
+#define DPTQ_MAX_TOP 64
+typedef enum { DPTQ_F16 = 0, DPTQ_F32 = 1 } dptq_float_type;
+int64_t dptq_token_logprobs_workspace(int64_t M, int64_t V, int32_t top, int32_t dtype); /* -1: invalid */
+int dptq_token_logprobs(const void* logits, int32_t dtype, int64_t ld, int64_t M, int64_t V,
+                        const int64_t* tokens, int32_t top, float* logprobs, float* entropy,
+                        float* top_logprobs, int64_t* top_ids, void* workspace, int64_t workspace_bytes,
+                        void* stream);
 
 /*
  * dptq_layer_policy - phase-aware activation precision (host only).

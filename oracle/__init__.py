@@ -28,6 +28,8 @@ Modules
             its weight absorption (Eq. 4-5).
   range_quant  the range-based quantizer of Eq. 1 with an integer zero point,
             and the zero-point correction of the integer GEMM.
+  serving   RMS norm with 8-bit codes, the 8-bit paged KV cache and the
+            attention over it, log probabilities of tokens.
 """
 
 from .hadamard import (sylvester, paley28, hadamard, split_had_size,

@@ -12,6 +12,7 @@ calling a function whose library is missing raises.
     y = qlinear(codes, scales, 4, w_packed, w_scales)
 """
 
+import collections
 import ctypes
 import importlib.util
 import os
@@ -24,6 +25,8 @@ __all__ = ["DptqError", "lib", "library_path", "rotate_quant", "qlinear", "qline
            "qlinear_fp6_acc", "pack_w4_a8", "qlinear_a8", "prepacked_bytes", "prepack_weights",
            "WEIGHTS_FP6", "WEIGHTS_A8_ORDER", "WEIGHTS_DECODE", "qlinear_decode_native",
            "qlinear_decode_native_acc",
+           "rms_norm_quant", "KV8Cache", "KV8_PAGE", "kv8_cache", "kv8_append", "kv8_attention",
+           "token_logprobs", "MAX_TOP",
            "EXPORTED_FUNCTIONS", "GEMM_AUTO",
            "GEMM_DECODE", "GEMM_TILE_256X128", "GEMM_TILE_192X256"]
 
@@ -44,7 +47,9 @@ EXPORTED_FUNCTIONS = ("dptq_status_string", "dptq_version", "dptq_rotate_quant",
                       "dptq_qlinear_decode_fused", "dptq_rotate_quant_range",
                       "dptq_weight_sums", "dptq_qlinear_range", "dptq_pack_w4_a8",
                       "dptq_qlinear_a8", "dptq_prepacked_bytes", "dptq_prepack_weights",
-                      "dptq_qlinear_decode_native")
+                      "dptq_qlinear_decode_native", "dptq_rms_norm_quant", "dptq_kv8_append",
+                      "dptq_kv8_attention_workspace", "dptq_kv8_attention",
+                      "dptq_token_logprobs_workspace", "dptq_token_logprobs")
 
 # Code layouts of dptq_rotate_quant_ex.
 LAYOUT_PACKED, LAYOUT_FP6 = 0, 1
@@ -100,6 +105,20 @@ def lib():
         L.dptq_kv_quant.restype = ctypes.c_int
         L.dptq_kv_dequant.argtypes = [vp, vp, vp, i64, i64, i32, vp, vp]
         L.dptq_kv_dequant.restype = ctypes.c_int
+        L.dptq_rms_norm_quant.argtypes = [vp, vp, vp, i64, i64, ctypes.c_float, vp, vp, vp, vp]
+        L.dptq_rms_norm_quant.restype = ctypes.c_int
+        L.dptq_kv8_append.argtypes = [vp, i64, vp, i64, i64, vp, vp, i64, vp, i64, i64, i32, i32, vp, vp, vp, vp,
+                                      i64, vp]
+        L.dptq_kv8_append.restype = ctypes.c_int
+        L.dptq_kv8_attention_workspace.argtypes = [i64, i64, i64, i32, i32, i32, i32, i32, i64, i64]
+        L.dptq_kv8_attention_workspace.restype = ctypes.c_int64
+        L.dptq_kv8_attention.argtypes = [vp, i64, i64, vp, vp, i64, vp, i64, i64, i32, i32, i32, vp, vp, vp, vp,
+                                         ctypes.c_float, i32, i32, i64, i64, vp, vp, vp, i64, vp]
+        L.dptq_kv8_attention.restype = ctypes.c_int
+        L.dptq_token_logprobs_workspace.argtypes = [i64, i64, i32, i32]
+        L.dptq_token_logprobs_workspace.restype = ctypes.c_int64
+        L.dptq_token_logprobs.argtypes = [vp, i32, i64, i64, i64, vp, i32, vp, vp, vp, vp, vp, i64, vp]
+        L.dptq_token_logprobs.restype = ctypes.c_int
         L.dptq_layer_policy.argtypes = [i32, vp, vp]
         L.dptq_layer_policy.restype = ctypes.c_int
         L.dptq_prepare_weights.argtypes = [vp, i64, i64, i32, vp, vp, vp]
@@ -506,3 +525,62 @@ def qlinear_range(codes, scales, zeros, bits, w_packed, w_scales, w_sums, y=None
     """Quantized linear on range-quantized activations (zero-point corrected
     in the GEMM epilogue).  Returns y [M, N] fp16."""
     return _binding().qlinear_range(codes, scales, zeros, bits, w_packed, w_scales, w_sums, y)
+
+
+def rms_norm_quant(x, weight, eps, residual=None, sum=None, codes=None, scales=None):
+    """RMS norm of fp16 rows x [M, K] (K a multiple of 8), after the addition of a residual if there is one, with
+    8-bit codes: (codes int8 [M, K], scales fp32 [M], h fp16 [M, K]).  h = x + residual (x itself without a
+    residual); codes * scales stand for h / sqrt(mean(h^2) + eps) * weight, and are activations for qlinear at 8
+    bits where the rotation is in the weights already (prepare_weights with had_size 1).  sum, the buffer of h, may
+    be x or the residual."""
+    return _binding().rms_norm_quant(x, weight, eps, residual, sum, codes, scales)
+
+
+# The 8-bit paged KV cache: pages of KV8_PAGE tokens.  k_pages float8_e4m3fn
+# [pages, kv_heads, 64, head_dim], v_pages float8_e4m3fn [pages, kv_heads, head_dim, 64] (channel-major), k_scales and
+# v_scales fp32 [pages, kv_heads]: a code stands for code * scale.
+KV8_PAGE = 64
+KV8Cache = collections.namedtuple("KV8Cache", ["k_pages", "v_pages", "k_scales", "v_scales"])
+
+
+def kv8_cache(pages, kv_heads, head_dim, device="cuda"):
+    """An empty 8-bit cache of one layer; head_dim 64, 128 or 256."""
+    torch = _torch()
+    f8 = torch.float8_e4m3fn
+    return KV8Cache(torch.empty((pages, kv_heads, KV8_PAGE, head_dim), dtype=f8, device=device),
+                    torch.empty((pages, kv_heads, head_dim, KV8_PAGE), dtype=f8, device=device),
+                    torch.ones((pages, kv_heads), device=device), torch.ones((pages, kv_heads), device=device))
+
+
+def kv8_append(k, v, cu_seqlens, lengths, page_table, cache, max_new=None):
+    """Writes new tokens' keys and values (fp16 [T, kv_heads, head_dim]; rows may be parts of wider ones) into the
+    cache, in place, and returns it.  cu_seqlens int32 [B + 1]: the token rows of each sequence; lengths int32 [B]:
+    its tokens, the new ones included, which stand last; page_table int32 [B, max_pages]: its pages.  max_new: the
+    most new tokens of a sequence if known (sizes the launch; no result depends on it)."""
+    _binding().kv8_append(k, v, cu_seqlens, lengths, page_table, *cache, max_new)
+    return cache
+
+
+def kv8_attention(q, cu_seqlens, lengths, page_table, cache, scale=None, window=0, sinks=0, max_q=None,
+                  max_len=None, out=None, lse=None):
+    """Causal attention of the new tokens' queries q (fp16 [T, heads, head_dim]; heads a multiple of the cache's)
+    over the cache, which holds their keys and values already (kv8_append with the same cu_seqlens, lengths and
+    page_table) -> (out fp16 [T, heads, head_dim], lse fp32 [T, heads], the log of each row's sum of exponentials).
+    scale: of the scores, head_dim ** -0.5 by default.  window > 0: a query sees only the last `window` positions up
+    to its own, and the first `sinks` ones.  max_q, max_len: the most queries and the longest length of a sequence
+    if known (they size the launch)."""
+    if scale is None:
+        scale = cache[0].shape[-1] ** -0.5
+    return _binding().kv8_attention(q, cu_seqlens, lengths, page_table, *cache, max_q, max_len, scale, window,
+                                    sinks, out, lse)
+
+
+MAX_TOP = 64   # most alternatives of token_logprobs
+
+
+def token_logprobs(logits, tokens, top=0, logprobs=None, entropy=None, top_logprobs=None, top_ids=None):
+    """Of each row of logits (fp16 or fp32 [M, V]; rows may be parts of wider ones): the log probability of its
+    token (int64 [M]; 0 where the token is negative), the entropy, and the `top` most likely tokens, likeliest first
+    and equal ones by index: (logprobs fp32 [M], entropy fp32 [M], top_logprobs fp32 [M, top], top_ids int64
+    [M, top]).  Logits of -inf are masked."""
+    return _binding().token_logprobs(logits, tokens, top, logprobs, entropy, top_logprobs, top_ids)

@@ -63,6 +63,66 @@ int check_kv_shape(int64_t T, int64_t D, int32_t group) {
   return DPTQ_OK;
 }
 
+bool aligned8(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 7u) == 0; }
+
+constexpr int64_t kMost30 = int64_t{1} << 30;
+
+// Sizes of the 8-bit paged KV cache and of the sequences in it.
+int check_kv8_shape(int64_t T, int64_t B, int64_t max_pages, int64_t num_pages, int32_t kv_heads,
+                    int32_t head_dim) {
+  if (T < 0 || B < 0 || max_pages < 0 || num_pages < 0 || kv_heads < 1 || head_dim < 1) return DPTQ_ERR_INVALID_ARG;
+  if (head_dim != 64 && head_dim != 128 && head_dim != 256) return DPTQ_ERR_UNSUPPORTED;
+  if (T >= kMost30 || B > 65535 || kv_heads > 1024) return DPTQ_ERR_UNSUPPORTED;
+  if (max_pages > kMost30 / DPTQ_KV8_PAGE || num_pages > 0x7FFFFFFF) return DPTQ_ERR_UNSUPPORTED;
+  return DPTQ_OK;
+}
+
+bool kv8_pointers(const dptq::Kv8Cache& c) {
+  return c.k_pages && c.v_pages && c.k_scales && c.v_scales && c.cu && c.lengths && c.table &&
+         aligned16(c.k_pages) && aligned16(c.v_pages) && aligned4(c.k_scales) && aligned4(c.v_scales) &&
+         aligned4(c.cu) && aligned4(c.lengths) && aligned4(c.table);
+}
+
+// Rows of n elements, ld apart, that 16-byte loads take.
+bool rows_ok(const void* p, int64_t ld, int64_t n) { return p && aligned16(p) && ld >= n && ld % 8 == 0; }
+
+// The sizes of a kv8_attention call; max_q and max_len within what T and the
+// page table allow.
+int attention_shape(int64_t T, int64_t B, int64_t max_pages, int64_t num_pages, int32_t heads, int32_t kv_heads,
+                    int32_t head_dim, int32_t window, int32_t sinks, int64_t max_q, int64_t max_len,
+                    dptq::Kv8Attention* c) {
+  const int st = check_kv8_shape(T, B, max_pages, num_pages, kv_heads, head_dim);
+  if (st != DPTQ_OK) return st;
+  if (heads < 1 || heads % kv_heads != 0 || window < 0 || sinks < 0 || max_q < 0 || max_len < 0)
+    return DPTQ_ERR_INVALID_ARG;
+  if (window >= kMost30 || sinks >= kMost30 || heads > 65536 || T > kMost30 / heads) return DPTQ_ERR_UNSUPPORTED;
+  const int64_t capacity = max_pages * DPTQ_KV8_PAGE;
+  c->cache.T = T;
+  c->cache.B = B;
+  c->cache.max_pages = max_pages;
+  c->cache.num_pages = num_pages;
+  c->cache.kv_heads = kv_heads;
+  c->cache.head_dim = head_dim;
+  c->heads = heads;
+  c->window = window;
+  c->sinks = sinks;
+  c->max_q = max_q > 0 && max_q < T ? max_q : T;
+  c->max_len = max_len > 0 && max_len < capacity ? max_len : capacity;
+  return DPTQ_OK;
+}
+
+int logprobs_shape(int64_t ld, int64_t M, int64_t V, int32_t top, int32_t dtype, dptq::TokenLogprobs* c) {
+  if (M < 0 || V < 1 || top < 0 || top > V || ld < V) return DPTQ_ERR_INVALID_ARG;
+  if (dtype != DPTQ_F16 && dtype != DPTQ_F32) return DPTQ_ERR_INVALID_ARG;
+  if (M > 0x7FFFFFFF || V >= kMost30 || top > DPTQ_MAX_TOP) return DPTQ_ERR_UNSUPPORTED;
+  c->fp32 = dtype == DPTQ_F32;
+  c->ld = ld;
+  c->M = M;
+  c->V = (int)V;
+  c->top = top;
+  return DPTQ_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -400,6 +460,111 @@ int dptq_qlinear_range(const void* codes, const float* a_scales, const int32_t* 
     return DPTQ_ERR_INVALID_ARG;
   return from_hip(dptq::launch_qlinear_zp(codes, a_scales, a_zeros, M, (int)K, bits, w_packed, w_scales,
                                           w_sums, N, y, static_cast<hipStream_t>(stream)));
+}
+
+int dptq_rms_norm_quant(const void* x, const void* residual, const void* weight, int64_t M, int64_t K,
+                        float eps, void* sum, int8_t* codes, float* scales, void* stream) {
+  if (M < 0 || K < 1 || K % 8 != 0) return DPTQ_ERR_INVALID_ARG;
+  if (!(eps >= 0.0f) || eps > 3.0e38f) return DPTQ_ERR_INVALID_ARG;   // also rejects NaN
+  if (K > 65536 || M > 0x7FFFFFFF) return DPTQ_ERR_UNSUPPORTED;
+  if (M == 0) return DPTQ_OK;
+  if (!x || !weight || !codes || !scales || (residual == nullptr) != (sum == nullptr)) return DPTQ_ERR_INVALID_ARG;
+  if (!aligned16(x) || !aligned16(residual) || !aligned16(weight) || !aligned16(sum) || !aligned16(codes) ||
+      !aligned4(scales))
+    return DPTQ_ERR_INVALID_ARG;
+  return from_hip(dptq::launch_rms_norm_quant(x, residual, weight, M, (int)K, eps, sum, codes, scales,
+                                              static_cast<hipStream_t>(stream)));
+}
+
+int dptq_kv8_append(const void* k, int64_t ld_k, const void* v, int64_t ld_v, int64_t T,
+                    const int32_t* cu_seqlens, const int32_t* lengths, int64_t B,
+                    const int32_t* page_table, int64_t max_pages, int64_t num_pages, int32_t kv_heads,
+                    int32_t head_dim, uint8_t* k_pages, uint8_t* v_pages, float* k_scales,
+                    float* v_scales, int64_t max_new, void* stream) {
+  const int st = check_kv8_shape(T, B, max_pages, num_pages, kv_heads, head_dim);
+  if (st != DPTQ_OK) return st;
+  if (max_new < 0) return DPTQ_ERR_INVALID_ARG;
+  if (T == 0 || B == 0 || max_pages == 0 || num_pages == 0) return DPTQ_OK;
+  const dptq::Kv8Cache c{k_pages, v_pages, k_scales, v_scales, cu_seqlens, lengths, page_table,
+                         T, B, max_pages, num_pages, kv_heads, head_dim};
+  const int64_t row = (int64_t)kv_heads * head_dim;
+  if (!kv8_pointers(c) || !rows_ok(k, ld_k, row) || !rows_ok(v, ld_v, row)) return DPTQ_ERR_INVALID_ARG;
+  return from_hip(dptq::launch_kv8_append(c, k, ld_k, v, ld_v, max_new > 0 && max_new < T ? max_new : T,
+                                          static_cast<hipStream_t>(stream)));
+}
+
+int64_t dptq_kv8_attention_workspace(int64_t T, int64_t B, int64_t max_pages, int32_t heads,
+                                     int32_t kv_heads, int32_t head_dim, int32_t window, int32_t sinks,
+                                     int64_t max_q, int64_t max_len) {
+  dptq::Kv8Attention c{};
+  if (attention_shape(T, B, max_pages, 1, heads, kv_heads, head_dim, window, sinks, max_q, max_len, &c) != DPTQ_OK)
+    return -1;
+  return T == 0 || B == 0 ? 0 : dptq::kv8_attention_workspace(c);
+}
+
+int dptq_kv8_attention(const void* q, int64_t ld_q, int64_t T, const int32_t* cu_seqlens,
+                       const int32_t* lengths, int64_t B, const int32_t* page_table, int64_t max_pages,
+                       int64_t num_pages, int32_t heads, int32_t kv_heads, int32_t head_dim,
+                       const uint8_t* k_pages, const uint8_t* v_pages, const float* k_scales,
+                       const float* v_scales, float scale, int32_t window, int32_t sinks,
+                       int64_t max_q, int64_t max_len, void* out, float* lse, void* workspace,
+                       int64_t workspace_bytes, void* stream) {
+  dptq::Kv8Attention c{};
+  const int st = attention_shape(T, B, max_pages, num_pages, heads, kv_heads, head_dim, window, sinks, max_q,
+                                 max_len, &c);
+  if (st != DPTQ_OK) return st;
+  if (!(scale >= -3.0e38f && scale <= 3.0e38f)) return DPTQ_ERR_INVALID_ARG;   // also rejects NaN
+  if (T == 0 || B == 0) return DPTQ_OK;
+  c.cache.k_pages = const_cast<uint8_t*>(k_pages);
+  c.cache.v_pages = const_cast<uint8_t*>(v_pages);
+  c.cache.k_scales = const_cast<float*>(k_scales);
+  c.cache.v_scales = const_cast<float*>(v_scales);
+  c.cache.cu = cu_seqlens;
+  c.cache.lengths = lengths;
+  c.cache.table = page_table;
+  if (!kv8_pointers(c.cache) || !rows_ok(q, ld_q, (int64_t)heads * head_dim)) return DPTQ_ERR_INVALID_ARG;
+  if (!out || !lse || !aligned16(out) || !aligned4(lse)) return DPTQ_ERR_INVALID_ARG;
+  const int64_t need = dptq::kv8_attention_workspace(c);
+  if (need > 0 && (!workspace || !aligned16(workspace) || workspace_bytes < need)) return DPTQ_ERR_INVALID_ARG;
+  c.q = q;
+  c.ld_q = ld_q;
+  c.scale = scale;
+  c.out = out;
+  c.lse = lse;
+  c.workspace = workspace;
+  return from_hip(dptq::launch_kv8_attention(c, static_cast<hipStream_t>(stream)));
+}
+
+int64_t dptq_token_logprobs_workspace(int64_t M, int64_t V, int32_t top, int32_t dtype) {
+  dptq::TokenLogprobs c{};
+  if (logprobs_shape(V, M, V, top, dtype, &c) != DPTQ_OK) return -1;
+  return M == 0 ? 0 : dptq::token_logprobs_workspace(c);
+}
+
+int dptq_token_logprobs(const void* logits, int32_t dtype, int64_t ld, int64_t M, int64_t V,
+                        const int64_t* tokens, int32_t top, float* logprobs, float* entropy,
+                        float* top_logprobs, int64_t* top_ids, void* workspace, int64_t workspace_bytes,
+                        void* stream) {
+  dptq::TokenLogprobs c{};
+  const int st = logprobs_shape(ld, M, V, top, dtype, &c);
+  if (st != DPTQ_OK) return st;
+  if (M == 0) return DPTQ_OK;
+  if (!logits || !tokens || !logprobs || !entropy || (top > 0 && (!top_logprobs || !top_ids)))
+    return DPTQ_ERR_INVALID_ARG;
+  const uintptr_t element = c.fp32 ? 4 : 2;
+  if (reinterpret_cast<uintptr_t>(logits) % element != 0 || !aligned8(tokens) || !aligned4(logprobs) ||
+      !aligned4(entropy) || !aligned4(top_logprobs) || !aligned8(top_ids))
+    return DPTQ_ERR_INVALID_ARG;
+  const int64_t need = dptq::token_logprobs_workspace(c);
+  if (need > 0 && (!workspace || !aligned16(workspace) || workspace_bytes < need)) return DPTQ_ERR_INVALID_ARG;
+  c.logits = logits;
+  c.tokens = tokens;
+  c.logprobs = logprobs;
+  c.entropy = entropy;
+  c.top_logprobs = top_logprobs;
+  c.top_ids = top_ids;
+  c.workspace = workspace;
+  return from_hip(dptq::launch_token_logprobs(c, static_cast<hipStream_t>(stream)));
 }
 
 int dptq_layer_policy(int32_t num_layers, const uint8_t* mask, int32_t* bits_out) {

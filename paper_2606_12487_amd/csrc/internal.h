@@ -49,6 +49,50 @@ hipError_t launch_kv_quant(const void* kv, int64_t T, int64_t D, int group, uint
 hipError_t launch_kv_dequant(const uint8_t* codes, const float* scales, const float* mins,
                              int64_t T, int64_t D, int group, void* out, hipStream_t stream);
 
+// Residual addition (residual may be nullptr, sum then is not written), RMS
+// norm and 8-bit codes with a scale per row; K % 8 == 0, K <= 65536.
+hipError_t launch_rms_norm_quant(const void* x, const void* residual, const void* weight, int64_t M, int K,
+                                 float eps, void* sum, int8_t* codes, float* scales, hipStream_t stream);
+
+// The 8-bit paged KV cache (kv8_device.h) and the sequences in it.
+struct Kv8Cache {
+  uint8_t *k_pages, *v_pages;
+  float *k_scales, *v_scales;
+  const int32_t *cu, *lengths, *table;   // [B + 1], [B], [B, max_pages]
+  int64_t T, B, max_pages, num_pages;
+  int kv_heads, head_dim;                // head_dim 64, 128 or 256
+};
+// ld_k, ld_v: elements from a token's row to the next; max_new sizes the grid.
+hipError_t launch_kv8_append(const Kv8Cache& c, const void* k, int64_t ld_k, const void* v, int64_t ld_v,
+                             int64_t max_new, hipStream_t stream);
+struct Kv8Attention {
+  Kv8Cache cache;
+  const void* q;
+  int64_t ld_q;
+  int heads;
+  float scale;
+  int window, sinks;        // window 0: none
+  int64_t max_q, max_len;   // size the grid and the split of the keys, no more
+  void* out;
+  float* lse;
+  void* workspace;
+};
+int64_t kv8_attention_workspace(const Kv8Attention& c);   // bytes
+hipError_t launch_kv8_attention(const Kv8Attention& c, hipStream_t stream);
+
+struct TokenLogprobs {
+  const void* logits;   // fp16 or fp32 rows, ld elements apart
+  bool fp32;
+  int64_t ld, M;
+  int V, top;
+  const int64_t* tokens;
+  float *logprobs, *entropy, *top_logprobs;
+  int64_t* top_ids;
+  void* workspace;
+};
+int64_t token_logprobs_workspace(const TokenLogprobs& c);   // bytes
+hipError_t launch_token_logprobs(const TokenLogprobs& c, hipStream_t stream);
+
 // One call of the K-split GEMM (qgemm_ksplit.hip): y from the dequant epilogue,
 // with the zero-point correction when a_zeros is given, or the raw
 // accumulators when acc is.

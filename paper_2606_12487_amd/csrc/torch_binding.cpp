@@ -39,6 +39,8 @@ const char* dtype_name(at::ScalarType t) {
     case at::kByte: return "torch.uint8";
     case at::kChar: return "torch.int8";
     case at::kInt: return "torch.int32";
+    case at::kLong: return "torch.int64";
+    case at::kFloat8_e4m3fn: return "torch.float8_e4m3fn";
     default: return "?";
   }
 }
@@ -54,9 +56,8 @@ std::string shape_text(at::IntArrayRef s) {
   return r + (s.size() == 1 ? ",)" : ")");
 }
 
-// The tensor o after its checks; shape only when `has_shape`.
-const at::Tensor& tensor(PyObject* o, const char* name, at::ScalarType dtype, at::IntArrayRef shape = {},
-                         bool has_shape = false) {
+// The tensor o, of that dtype and on the GPU.
+const at::Tensor& gpu_tensor(PyObject* o, const char* name, at::ScalarType dtype) {
   if (!THPVariable_Check(o)) fail(PyExc_TypeError, std::string(name) + " must be a torch.Tensor");
   const at::Tensor& t = THPVariable_Unpack(o);
   if (t.scalar_type() != dtype) {
@@ -67,6 +68,13 @@ const at::Tensor& tensor(PyObject* o, const char* name, at::ScalarType dtype, at
     throw Raised{};
   }
   if (!t.is_cuda()) fail(PyExc_ValueError, std::string(name) + " must be a GPU tensor");
+  return t;
+}
+
+// The tensor o after its checks; shape only when `has_shape`.
+const at::Tensor& tensor(PyObject* o, const char* name, at::ScalarType dtype, at::IntArrayRef shape = {},
+                         bool has_shape = false) {
+  const at::Tensor& t = gpu_tensor(o, name, dtype);
   if (!t.is_contiguous()) fail(PyExc_ValueError, std::string(name) + " must be contiguous");
   if (has_shape && t.sizes() != shape)
     fail(PyExc_ValueError, std::string(name) + " must have shape " + shape_text(shape) + ", got " +
@@ -151,7 +159,7 @@ class Unlocked {
 struct Out {
   PyObject* o = nullptr;   // a new reference
   at::Tensor t;
-  std::array<int64_t, 2> shape{};
+  std::array<int64_t, 3> shape{};
   int dims;
   at::TensorOptions options;
   Out(PyObject* given, const char* name, at::ScalarType dtype, std::initializer_list<int64_t> s,
@@ -485,6 +493,181 @@ PyObject* kv_dequant(PyObject* const* a) {
   return out.release();
 }
 
+void same_device(const at::Tensor& t, const char* name, const at::Tensor& x, const char* of) {
+  if (t.device() != x.device())
+    fail(PyExc_ValueError, std::string(name) + " must be on the same device as " + of);
+}
+
+// rms_norm_quant(x, weight, eps, residual, sum, codes, scales)
+PyObject* rms_norm_quant(PyObject* const* a) {
+  const at::Tensor& x = tensor(a[0], "x", at::kHalf);
+  two_d(x, "x must be 2-D [M, K]");
+  const int64_t M = x.size(0), K = x.size(1);
+  const at::Tensor& weight = tensor_of(a[1], "weight", at::kHalf, {K});
+  same_device(weight, "weight", x, "x");
+  const bool add = a[3] != Py_None;
+  const at::Tensor* residual = add ? &tensor_of(a[3], "residual", at::kHalf, {M, K}) : nullptr;
+  if (add) same_device(*residual, "residual", x, "x");
+  if (!add && a[4] != Py_None) fail(PyExc_ValueError, "sum is given without a residual");
+  // Without a residual the sum is x itself.
+  Out sum(add ? a[4] : a[0], "sum", at::kHalf, {M, K}, x);
+  Out codes(a[5], "codes", at::kChar, {M, K}, x);
+  Out scales(a[6], "scales", at::kFloat, {M}, x);
+  allocate(sum, codes, scales);
+  same_device(sum.t, "sum", x, "x");
+  same_device(codes.t, "codes", x, "x");
+  same_device(scales.t, "scales", x, "x");
+  PyObject* f = PyNumber_Float(a[2]);
+  if (!f) throw Raised{};
+  const double eps = PyFloat_AS_DOUBLE(f);
+  Py_DECREF(f);
+  call("dptq_rms_norm_quant", x, dptq_rms_norm_quant, ptr(x), add ? ptr(*residual) : nullptr, ptr(weight), M, K,
+       (float)eps, add ? sum.ptr() : nullptr, codes.ptr<int8_t>(), scales.ptr<float>());
+  return tuple(codes, scales, sum);
+}
+
+// Token rows [T, heads, D] with dense heads; *ld: elements from a token to the next.
+const at::Tensor& token_rows(PyObject* o, const char* name, int64_t T, int64_t heads, int64_t D, int64_t* ld) {
+  const at::Tensor& t = gpu_tensor(o, name, at::kHalf);
+  const std::array<int64_t, 3> shape{T < 0 && t.dim() == 3 ? t.size(0) : T,
+                                     heads < 0 && t.dim() == 3 ? t.size(1) : heads, D};
+  if (t.sizes() != at::IntArrayRef(shape))
+    fail(PyExc_ValueError, std::string(name) + " must be 3-D [T, heads, head_dim] with " +
+                               (T < 0 ? "" : "T = " + std::to_string(T) + ", ") +
+                               (heads < 0 ? "" : "heads = " + std::to_string(heads) + ", ") +
+                               "head_dim = " + std::to_string(D) + ", got " + shape_text(t.sizes()));
+  const int64_t row = t.size(1) * D;
+  *ld = t.size(0) > 1 ? t.stride(0) : (row + 7) / 8 * 8;
+  if ((D > 1 && t.stride(2) != 1) || (t.size(1) > 1 && t.stride(1) != D) || *ld < row || *ld % 8)
+    fail(PyExc_ValueError, std::string(name) + " must have dense heads and tokens a multiple of 8 elements apart");
+  return t;
+}
+
+// The cache's four tensors and the sequences' three (from a[0]).
+struct Cache {
+  const at::Tensor &cu, &lengths, &table, &k, &v, &ks, &vs;
+  int64_t B, max_pages, pages, heads, D;
+};
+
+Cache cache_args(PyObject* const* a) {
+  const at::Tensor& k = tensor(a[3], "k_pages", at::kFloat8_e4m3fn);
+  if (k.dim() != 4 || k.size(2) != DPTQ_KV8_PAGE)
+    fail(PyExc_ValueError, "k_pages must be 4-D [pages, kv_heads, 64, head_dim]");
+  const int64_t P = k.size(0), H = k.size(1), D = k.size(3);
+  const at::Tensor& v = tensor_of(a[4], "v_pages", at::kFloat8_e4m3fn, {P, H, D, DPTQ_KV8_PAGE});
+  const at::Tensor& ks = tensor_of(a[5], "k_scales", at::kFloat, {P, H});
+  const at::Tensor& vs = tensor_of(a[6], "v_scales", at::kFloat, {P, H});
+  const at::Tensor& lengths = tensor(a[1], "lengths", at::kInt);
+  if (lengths.dim() != 1) fail(PyExc_ValueError, "lengths must be 1-D [B]");
+  const int64_t B = lengths.size(0);
+  const at::Tensor& cu = tensor_of(a[0], "cu_seqlens", at::kInt, {B + 1});
+  const at::Tensor& table = tensor(a[2], "page_table", at::kInt);
+  if (table.dim() != 2 || table.size(0) != B) fail(PyExc_ValueError, "page_table must be 2-D [B, max_pages]");
+  same_device(v, "v_pages", k, "k_pages");
+  same_device(ks, "k_scales", k, "k_pages");
+  same_device(vs, "v_scales", k, "k_pages");
+  same_device(cu, "cu_seqlens", k, "k_pages");
+  same_device(lengths, "lengths", k, "k_pages");
+  same_device(table, "page_table", k, "k_pages");
+  return Cache{cu, lengths, table, k, v, ks, vs, B, table.size(1), P, H, D};
+}
+
+int64_t size_hint(PyObject* o, const char* name) {
+  const int64_t n = o == Py_None ? 0 : integer(o, name);
+  if (n < 0) fail(PyExc_ValueError, std::string(name) + " must not be negative");
+  return n;
+}
+
+int32_t small_count(PyObject* o, const char* name) {
+  const int64_t n = integer(o, name);
+  if (n < 0 || n > 0x7FFFFFFF) fail(PyExc_ValueError, std::string(name) + " must be in [0, 2^31)");
+  return (int32_t)n;
+}
+
+// kv8_append(k, v, cu_seqlens, lengths, page_table, k_pages, v_pages, k_scales, v_scales, max_new)
+PyObject* kv8_append(PyObject* const* a) {
+  const Cache c = cache_args(a + 2);
+  int64_t ld_k, ld_v;
+  const at::Tensor& k = token_rows(a[0], "k", -1, c.heads, c.D, &ld_k);
+  const at::Tensor& v = token_rows(a[1], "v", k.size(0), c.heads, c.D, &ld_v);
+  same_device(k, "k", c.k, "k_pages");
+  same_device(v, "v", c.k, "k_pages");
+  const int64_t max_new = size_hint(a[9], "max_new");
+  call("dptq_kv8_append", k, dptq_kv8_append, ptr(k), ld_k, ptr(v), ld_v, k.size(0), ptr<int32_t>(c.cu),
+       ptr<int32_t>(c.lengths), c.B, ptr<int32_t>(c.table), c.max_pages, c.pages, (int32_t)c.heads, (int32_t)c.D,
+       ptr<uint8_t>(c.k), ptr<uint8_t>(c.v), ptr<float>(c.ks), ptr<float>(c.vs), max_new);
+  Py_RETURN_NONE;
+}
+
+// kv8_attention(q, cu_seqlens, lengths, page_table, k_pages, v_pages, k_scales, v_scales, max_q, max_len, scale,
+//               window, sinks, out, lse)
+PyObject* kv8_attention(PyObject* const* a) {
+  const Cache c = cache_args(a + 1);
+  int64_t ld;
+  const at::Tensor& q = token_rows(a[0], "q", -1, -1, c.D, &ld);
+  same_device(q, "q", c.k, "k_pages");
+  const int64_t T = q.size(0), H = q.size(1);
+  if (c.heads == 0 || H % c.heads != 0 || H == 0)
+    fail(PyExc_ValueError, "the heads of q must be a multiple of the cache's kv_heads");
+  const int64_t max_q = size_hint(a[8], "max_q"), max_len = size_hint(a[9], "max_len");
+  PyObject* f = PyNumber_Float(a[10]);
+  if (!f) throw Raised{};
+  const double scale = PyFloat_AS_DOUBLE(f);
+  Py_DECREF(f);
+  const int32_t window = small_count(a[11], "window"), sinks = small_count(a[12], "sinks");
+  Out out(a[13], "out", at::kHalf, {T, H, c.D}, q);
+  Out lse(a[14], "lse", at::kFloat, {T, H}, q);
+  const int64_t bytes = dptq_kv8_attention_workspace(T, c.B, c.max_pages, (int32_t)H, (int32_t)c.heads,
+                                                     (int32_t)c.D, window, sinks, max_q, max_len);
+  // The call's own scratch, in the order of the stream.  Sizes that the library
+  // does not cover are its to refuse.
+  Out work(Py_None, "workspace", at::kByte, {bytes > 0 ? bytes : 0}, q);
+  if (bytes > 0) allocate(out, lse, work);
+  else allocate(out, lse);
+  same_device(out.t, "out", q, "q");
+  same_device(lse.t, "lse", q, "q");
+  call("dptq_kv8_attention", q, dptq_kv8_attention, ptr(q), ld, T, ptr<int32_t>(c.cu), ptr<int32_t>(c.lengths), c.B,
+       ptr<int32_t>(c.table), c.max_pages, c.pages, (int32_t)H, (int32_t)c.heads, (int32_t)c.D, ptr<uint8_t>(c.k),
+       ptr<uint8_t>(c.v), ptr<float>(c.ks), ptr<float>(c.vs), (float)scale, window, sinks, max_q, max_len, out.ptr(),
+       lse.ptr<float>(), bytes > 0 ? work.ptr() : nullptr, bytes > 0 ? bytes : 0);
+  return tuple(out, lse);
+}
+
+// token_logprobs(logits, tokens, top, logprobs, entropy, top_logprobs, top_ids)
+PyObject* token_logprobs(PyObject* const* a) {
+  if (!THPVariable_Check(a[0])) fail(PyExc_TypeError, "logits must be a torch.Tensor");
+  const at::ScalarType type = THPVariable_Unpack(a[0]).scalar_type();
+  const bool half = type == at::kHalf;
+  if (!half && type != at::kFloat) fail(PyExc_TypeError, "logits must have dtype torch.float16 or torch.float32");
+  const at::Tensor& x = gpu_tensor(a[0], "logits", half ? at::kHalf : at::kFloat);
+  two_d(x, "logits must be 2-D [M, V]");
+  const int64_t M = x.size(0), V = x.size(1);
+  const int64_t ld = M > 1 ? x.stride(0) : V;
+  if ((V > 1 && x.stride(1) != 1) || ld < V) fail(PyExc_ValueError, "logits must have dense rows");
+  const at::Tensor& tokens = tensor_of(a[1], "tokens", at::kLong, {M});
+  same_device(tokens, "tokens", x, "logits");
+  const int32_t top = small_count(a[2], "top");
+  if (top > V || top > DPTQ_MAX_TOP)
+    fail(PyExc_ValueError, "top must be at most min(V, " + std::to_string(DPTQ_MAX_TOP) + ")");
+  Out lp(a[3], "logprobs", at::kFloat, {M}, x);
+  Out entropy(a[4], "entropy", at::kFloat, {M}, x);
+  Out top_lp(a[5], "top_logprobs", at::kFloat, {M, top}, x);
+  Out ids(a[6], "top_ids", at::kLong, {M, top}, x);
+  const int32_t dtype = half ? DPTQ_F16 : DPTQ_F32;
+  const int64_t bytes = dptq_token_logprobs_workspace(M, V, top, dtype);
+  Out work(Py_None, "workspace", at::kByte, {bytes > 0 ? bytes : 0}, x);
+  if (bytes > 0) allocate(lp, entropy, top_lp, ids, work);
+  else allocate(lp, entropy, top_lp, ids);
+  same_device(lp.t, "logprobs", x, "logits");
+  same_device(entropy.t, "entropy", x, "logits");
+  same_device(top_lp.t, "top_logprobs", x, "logits");
+  same_device(ids.t, "top_ids", x, "logits");
+  call("dptq_token_logprobs", x, dptq_token_logprobs, ptr(x), dtype, ld, M, V, ptr<int64_t>(tokens), top,
+       lp.ptr<float>(), entropy.ptr<float>(), top_lp.ptr<float>(), ids.ptr<int64_t>(),
+       bytes > 0 ? work.ptr() : nullptr, bytes > 0 ? bytes : 0);
+  return tuple(lp, entropy, top_lp, ids);
+}
+
 // init(raise_error, raw_stream)
 PyObject* init(PyObject* const* a) {
   Py_INCREF(a[0]);
@@ -526,6 +709,10 @@ PyMethodDef kMethods[] = {
     DPTQ_ENTRY(residual_dynamics, 8),
     DPTQ_ENTRY(kv_quant, 5),
     DPTQ_ENTRY(kv_dequant, 5),
+    DPTQ_ENTRY(rms_norm_quant, 7),
+    DPTQ_ENTRY(kv8_append, 10),
+    DPTQ_ENTRY(kv8_attention, 15),
+    DPTQ_ENTRY(token_logprobs, 7),
     {nullptr, nullptr, 0, nullptr},
 };
 

@@ -1,0 +1,129 @@
+"""GPU parity of token_logprobs against the float64 definition."""
+
+import numpy as np
+import pytest
+
+from oracle.serving import token_logprobs_ref
+
+torch = pytest.importorskip("torch")
+dptq = pytest.importorskip("paper_2606_12487_amd")
+
+pytestmark = pytest.mark.gpu
+
+
+def _d(a):
+    return torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+
+def _close(got, ref, tol, what):
+    assert np.array_equal(np.isnan(got), np.isnan(ref)), what
+    inf = np.isinf(ref)
+    assert np.array_equal(got[inf], ref[inf].astype(np.float32)), what
+    ok = np.isfinite(ref)
+    assert np.all(np.abs(got[ok] - ref[ok]) <= tol), (what, np.abs(got[ok] - ref[ok]).max(), tol)
+
+
+def _check(x, tokens, top, xd=None):
+    lp, ent, tops, ids = (t.cpu().numpy() for t in dptq.token_logprobs(_d(x) if xd is None else xd, _d(tokens), top))
+    r_lp, r_ent, r_tops, r_ids = token_logprobs_ref(x, tokens, top)
+    finite = x[np.isfinite(x)].astype(np.float64)
+    size = np.abs(finite).max() if finite.size else 0.0
+    # Arguments of the exponential are off by a few units of 2^-24 of the logits'
+    # size, the sums by their chains of at most a few hundred fp32 additions in a
+    # thread and the final logarithm by an ulp; the entropy weighs each of these
+    # by a log probability, at most the range and the vocabulary's logarithm.
+    tol = 2.0 ** -21 * (size + 32)
+    _close(lp, r_lp, tol, "logprobs")
+    _close(ent, r_ent, 2 * tol, "entropy")
+    _close(tops, r_tops, tol, "top_logprobs")
+    assert np.array_equal(ids, r_ids)
+
+
+CASES = [(1, 1, 0), (1, 1, 1), (3, 2, 2), (5, 7, 7), (1, 63, 5), (2, 64, 64), (4, 1000, 20), (1, 32768, 20),
+         (9, 50001, 1), (2, 131072, 64), (300, 257, 3), (17, 4097, 0), (3, 8191, 33), (1, 300007, 20)]
+
+
+@pytest.mark.parametrize("M,V,top", CASES)
+@pytest.mark.parametrize("dtype", [np.float16, np.float32])
+def test_logprobs_match_definition(M, V, top, dtype):
+    rng = np.random.default_rng(M * 100003 + V + top)
+    x = (4 * rng.standard_normal((M, V))).astype(dtype)
+    _check(x, rng.integers(0, V, M), top)
+
+
+@pytest.mark.parametrize("dtype", [np.float16, np.float32])
+@pytest.mark.parametrize("V", [40, 3001, 70000])
+def test_logprobs_masks_and_ties(dtype, V):
+    rng = np.random.default_rng(V)
+    x = (2 * rng.standard_normal((10, V))).astype(dtype)
+    x[0] = 0                                        # all equal: ties by index
+    x[1, rng.random(V) < 0.9] = -np.inf             # masked off
+    x[2] = -np.inf                                  # nothing left
+    x[3] = -np.inf
+    x[3, V - 3] = 2.5                               # one token left
+    x[4] = np.round(x[4])                           # many ties
+    x[5] = np.finfo(dtype).min                      # masks of the type's lowest value
+    x[5, 7] = 1
+    x[6] = np.finfo(dtype).min
+    x[7] = np.where(np.arange(V) % 2, 5, -np.inf)   # half of the row ties
+    x[8, :20] = 60000                               # a few ties far above the rest
+    tokens = np.array([3, 5, 1, V - 3, 0, 7, 9, 1, V - 1, -1])
+    keep = [r for r in range(10) if r != 5 and r != 6]
+    _check(x[keep], tokens[keep], 20)
+    if dtype == np.float16:
+        _check(x[[5, 6]], tokens[[5, 6]], 20)
+    else:   # the lowest fp32 value: only what does not scale with it
+        lp, ent, tops, ids = (t.cpu().numpy() for t in dptq.token_logprobs(_d(x[[5, 6]]), _d(tokens[[5, 6]]), 20))
+        assert lp[0] == 0 and ent[0] == 0 and ids[0, 0] == 7 and abs(ent[1] - np.log(V)) < 2e-5
+        assert np.array_equal(ids[1], np.arange(20)) and np.array_equal(ids[0, 1:], np.delete(np.arange(20), 7))
+
+
+def test_logprobs_token_bounds():
+    x = np.linspace(-1, 1, 10, dtype=np.float32).reshape(2, 5).repeat(2, 0)
+    lp = dptq.token_logprobs(_d(x), _d(np.array([-1, 5, -100, 4])))[0].cpu().numpy()
+    assert lp[0] == 0 and np.isnan(lp[1]) and lp[2] == 0
+    assert abs(lp[3] - token_logprobs_ref(x, [0, 0, 0, 4])[0][3]) < 1e-6
+
+
+@pytest.mark.parametrize("dtype", [np.float16, np.float32])
+def test_logprobs_rows_of_wider_ones(dtype):
+    rng = np.random.default_rng(3)
+    for V, first, wide in ((1001, 3, 1037), (50000, 1, 50003), (33, 5, 40)):
+        x = (3 * rng.standard_normal((4, wide))).astype(dtype)
+        x[:, :first] = np.nan                       # what lies beside the rows is not read into them
+        x[:, first + V:] = np.nan
+        view = _d(x)[:, first:first + V]
+        _check(np.ascontiguousarray(x[:, first:first + V]), rng.integers(0, V, 4), 20, view)
+
+
+def test_logprobs_non_finite_rows_stay_in_their_rows():
+    rng = np.random.default_rng(4)
+    x = rng.standard_normal((4, 5000)).astype(np.float32)
+    clean = x[[0, 3]].copy()
+    x[1, 17] = np.nan
+    x[2, 4000] = np.inf
+    lp, ent, tops, ids = (t.cpu().numpy() for t in dptq.token_logprobs(_d(x), _d(np.zeros(4, np.int64)), 8))
+    r = token_logprobs_ref(clean, [0, 0], 8)
+    assert np.abs(lp[[0, 3]] - r[0]).max() < 1e-4 and np.array_equal(ids[[0, 3]], r[3])
+    assert ids.min() >= 0 and ids.max() < 5000
+
+
+def test_logprobs_refusals():
+    x = torch.zeros((2, 100), device="cuda")
+    t = torch.zeros(2, dtype=torch.int64, device="cuda")
+    with pytest.raises(TypeError, match="logits must have dtype torch.float16 or torch.float32"):
+        dptq.token_logprobs(x.double(), t)
+    with pytest.raises(TypeError, match="tokens must have dtype torch.int64"):
+        dptq.token_logprobs(x, t.int())
+    with pytest.raises(ValueError, match="tokens must have shape"):
+        dptq.token_logprobs(x, t[:1])
+    with pytest.raises(ValueError, match="top must be at most"):
+        dptq.token_logprobs(x, t, 65)
+    with pytest.raises(ValueError, match="top must be at most"):
+        dptq.token_logprobs(x[:, :3], t, 4)
+    with pytest.raises(ValueError, match="dense rows"):
+        dptq.token_logprobs(x.t().contiguous().t(), t)
+    with pytest.raises(ValueError, match="2-D"):
+        dptq.token_logprobs(x[0], t)
+    got = dptq.token_logprobs(x[:0], t[:0], 3)
+    assert [tuple(g.shape) for g in got] == [(0,), (0,), (0, 3), (0, 3)]
