@@ -21,60 +21,10 @@
 // rows.  The rows of the K operand are taken in an order that leaves each lane
 // with the scores of 16 consecutive tokens of one query, which is exactly what
 // the second product wants of P from that lane: P never leaves the registers.
-#include "internal.h"
-#include "kv8_device.h"
+#include "kv8_attn.h"
 
 namespace dptq {
 namespace {
-
-typedef _Float16 half8 __attribute__((ext_vector_type(8)));
-typedef _Float16 half2v __attribute__((ext_vector_type(2)));
-typedef float float4v __attribute__((ext_vector_type(4)));
-
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-
-struct AttnArgs {
-  const __half* q;
-  int64_t ld_q;
-  const uint8_t *k_pages, *v_pages;
-  const float *k_scales, *v_scales;
-  const int32_t *cu, *lengths, *table;
-  int T, max_pages, num_pages, heads, kv_heads, group;
-  float scale_log2;        // scale * log2(e)
-  int window, sinks;       // window 0: none
-  int splits;
-  __half* out;
-  float* lse;
-  float* part_o;           // [splits][T * heads][D], relative to their maxima
-  float2* part_ml;         // [splits][T * heads] (maximum, sum), base 2
-};
-
-__device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
-
-// Eight codes (two dwords) as halves.
-__device__ __forceinline__ half8 codes8(uint32_t a, uint32_t b) {
-  const half2v x0 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.0f, false);
-  const half2v x1 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.0f, true);
-  const half2v x2 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.0f, false);
-  const half2v x3 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.0f, true);
-  return half8{x0[0], x0[1], x1[0], x1[1], x2[0], x2[1], x3[0], x3[1]};
-}
-
-// Pages that a tile of rows with positions [pmin, pmax] reads: [0, sink_pages)
-// and [first, last].
-struct Visible {
-  int sink_pages, first, total;
-  __device__ int page(int i) const { return i < sink_pages ? i : first + (i - sink_pages); }
-};
-
-__device__ __forceinline__ Visible visible_pages(int pmin, int pmax, int window, int sinks, int max_pages) {
-  if (pmax < 0) return Visible{0, 0, 0};
-  const int low = window > 0 ? max(pmin - window + 1, 0) : 0;
-  const int last = min(pmax / kPage, max_pages - 1);
-  const int sink_pages = window > 0 ? min((min(sinks, low) + kPage - 1) / kPage, last + 1) : 0;
-  const int first = max(low / kPage, sink_pages);
-  return Visible{sink_pages, first, sink_pages + max(last - first + 1, 0)};
-}
 
 // 16 rows (queries of one KV head of one sequence; row r is query token
 // r / group, head r % group of the group) by one split of the visible pages.
@@ -89,14 +39,14 @@ __global__ void __launch_bounds__(256) kv8_decode_kernel(AttnArgs a) {
   const int col = lane & 15, quad = lane >> 4;
   const int head = (int)blockIdx.x % a.kv_heads, b = (int)blockIdx.x / a.kv_heads;
   const KvSeq seq = kv_seq(a.cu, a.lengths, b, a.T);
-  const int64_t rows = (int64_t)seq.count * a.group;
+  const int rows = seq.count * a.group;   // T * heads < 2^30
 
-  for (int64_t row0 = (int64_t)blockIdx.y * 16; row0 < rows; row0 += (int64_t)gridDim.y * 16) {
-    const int64_t row = row0 + col < rows ? row0 + col : rows - 1;    // lanes past the end repeat the last row
-    const int token = (int)(row / a.group), g = (int)(row % a.group);
+  for (int row0 = (int)blockIdx.y * 16; row0 < rows; row0 += (int)gridDim.y * 16) {
+    const int row = min(row0 + col, rows - 1);    // lanes past the end repeat the last row
+    const int token = row / a.group, g = row % a.group;
     const int pos = seq.start + token;
-    const int pmin = seq.start + (int)(row0 / a.group);
-    const int pmax = seq.start + (int)((row0 + 15 < rows ? row0 + 15 : rows - 1) / a.group);
+    const int pmin = seq.start + row0 / a.group;
+    const int pmax = seq.start + min(row0 + 15, rows - 1) / a.group;
     const Visible vis = visible_pages(pmin, pmax, a.window, a.sinks, a.max_pages);
     const int begin = (int)((int64_t)vis.total * blockIdx.z / a.splits);
     const int end = (int)((int64_t)vis.total * (blockIdx.z + 1) / a.splits);
@@ -143,15 +93,10 @@ __global__ void __launch_bounds__(256) kv8_decode_kernel(AttnArgs a) {
       }
       // Masks, where the page is not visible as a whole to every row.
       const int j0 = blk * kPage;
-      const bool whole = j0 + kPage - 1 <= pmin &&
-                         (a.window == 0 || j0 > pmax - a.window || j0 + kPage <= a.sinks);
-      if (!whole) {
+      if (!page_whole(j0, pmin, pmax, a.window, a.sinks)) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int j = j0 + 16 * quad + e;
-          const bool see = j <= pos && (a.window == 0 || j > pos - a.window || j < a.sinks);
-          s[e] = see ? s[e] : -INFINITY;
-        }
+        for (int e = 0; e < 16; ++e)
+          s[e] = sees(pos, j0 + 16 * quad + e, a.window, a.sinks) ? s[e] : -INFINITY;
       }
       float top = s[0];
 #pragma unroll
@@ -182,10 +127,7 @@ __global__ void __launch_bounds__(256) kv8_decode_kernel(AttnArgs a) {
         if (j0 + kPage > seq.length) {
           uint32_t* const w = &vc.x;
 #pragma unroll
-          for (int d = 0; d < 4; ++d) {
-            const int n = held - 4 * d;
-            w[d] &= n >= 4 ? 0xFFFFFFFFu : n <= 0 ? 0u : (1u << (8 * n)) - 1u;
-          }
+          for (int d = 0; d < 4; ++d) w[d] &= held_mask(held, 4 * d);
         }
         o[t] *= fix;
         o[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8(vc.x, vc.y), p[0], o[t], 0, 0, 0);
@@ -218,7 +160,7 @@ __global__ void __launch_bounds__(256) kv8_decode_kernel(AttnArgs a) {
     if (threadIdx.x < 16) wave_ml[0][threadIdx.x] = make_float2(M, L);   // lanes 0..15 hold rows 0..15
     __syncthreads();
     for (int e = threadIdx.x; e < 16 * D; e += 256) {
-      const int64_t r = row0 + e / D;
+      const int r = row0 + e / D;
       if (r >= rows) break;
       const int d = e % D;
       const float2 ml = wave_ml[0][e / D];
@@ -259,10 +201,18 @@ __global__ void __launch_bounds__(256) kv8_combine_kernel(AttnArgs a) {
   if (lane == 0) a.lse[row] = M * kLn2 + logf(L);
 }
 
+// Rows of a sequence's largest count that the tiles of 16 still take; more go
+// to the tiles of kPromptRows.
+constexpr int64_t kDecodeRows = 32;
+
+bool is_prompt(const Kv8Attention& c) { return c.max_q * (c.heads / c.cache.kv_heads) > kDecodeRows; }
+
 // Splits of the visible pages: enough workgroups for two on every compute
 // unit, of four pages (one a wave) or more.
 int choose_splits(const Kv8Attention& c) {
-  const int64_t tiles = ((c.max_q * (c.heads / c.cache.kv_heads) + 15) / 16) * c.cache.B * c.cache.kv_heads;
+  const int64_t height = is_prompt(c) ? kPromptRows : 16;
+  const int64_t tiles =
+      ((c.max_q * (c.heads / c.cache.kv_heads) + height - 1) / height) * c.cache.B * c.cache.kv_heads;
   int64_t keys = c.max_len;
   if (c.window > 0 && (int64_t)c.window + c.sinks + c.max_q + 2 * kPage < keys)
     keys = (int64_t)c.window + c.sinks + c.max_q + 2 * kPage;
@@ -274,10 +224,16 @@ int choose_splits(const Kv8Attention& c) {
 
 template <int D>
 hipError_t launch(const AttnArgs& a, const Kv8Attention& c, hipStream_t stream) {
-  const int64_t tiles = (c.max_q * a.group + 15) / 16;
-  const dim3 grid((unsigned)(c.cache.B * a.kv_heads), (unsigned)(tiles < 65535 ? tiles : 65535), (unsigned)a.splits);
-  kv8_decode_kernel<D><<<grid, 256, 0, stream>>>(a);
-  hipError_t e = hipGetLastError();
+  hipError_t e;
+  if (is_prompt(c)) {
+    e = launch_kv8_prompt(a, D, c.cache.B, c.max_q, stream);
+  } else {
+    const int64_t tiles = (c.max_q * a.group + 15) / 16;
+    const dim3 grid((unsigned)(c.cache.B * a.kv_heads), (unsigned)(tiles < 65535 ? tiles : 65535),
+                    (unsigned)a.splits);
+    kv8_decode_kernel<D><<<grid, 256, 0, stream>>>(a);
+    e = hipGetLastError();
+  }
   if (e != hipSuccess || a.splits == 1) return e;
   kv8_combine_kernel<D><<<(unsigned)(((int64_t)a.T * a.heads + 3) / 4), 256, 0, stream>>>(a);
   return hipGetLastError();

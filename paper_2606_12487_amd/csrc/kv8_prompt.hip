@@ -1,0 +1,284 @@
+// kv8_attention for many queries a sequence (the formulas: kv8_attention.hip).
+//
+// A workgroup of four waves takes 128 rows of one KV head of one sequence (row
+// r is query token r / group, head r % group: the heads that share a KV head
+// share its loads), 32 rows a wave, and walks the pages they see.  Pages come
+// into LDS by direct loads, one page ahead; each wave reads the codes from
+// there and converts them as it feeds the matrix cores.
+//
+// The products are those of the decode kernel on 32 x 32 tiles: S^T = K Q^T
+// with the K operand's rows in an order that leaves a lane with 16 consecutive
+// tokens of each half page, O^T = V^T P^T.
+//
+// The softmax keeps a reference m instead of the running maximum: weights are
+// 2^(s - m), and m moves (with the sums and O rescaled) only where a score
+// passes m + 10, then to 4 below it.  A page's v scale goes into the exponent
+// as its ratio to the unit U of O, 2^-4 to 2^4; another unit is taken, with O
+// rescaled, where the ratio leaves that range.  Weights stay below 2^15, within
+// fp16, and are never below their exact size relative to the row's largest:
+// the fp16 rounding is the decode kernel's or finer.
+#include "kv8_attn.h"
+
+namespace dptq {
+namespace {
+
+// 16 bytes per lane from base + voff straight to LDS, at byte lds_off + 16 *
+// lane.  As asm, so that the compiler does not wait for them before each LDS
+// read; wait_loads() and the barrier order them.
+__device__ __forceinline__ void load_lds16(const void* base, uint32_t voff, uint32_t lds_off) {
+  asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1"
+               :
+               : "v"(voff), "s"(base), "s"(lds_off)
+               : "memory");
+}
+
+// What is fetched ahead for a page beside its codes.
+struct Ahead {
+  int page;        // of the list place after
+  float ks, vs;    // the page's own scales
+};
+// Waits for the direct loads and for what was fetched with them.
+__device__ __forceinline__ void wait_loads(Ahead& x) {
+  asm volatile("s_waitcnt vmcnt(0)" : "+v"(x.page), "+v"(x.ks), "+v"(x.vs)::"memory");
+}
+__device__ __forceinline__ float uniform(float x) {
+  return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(x)));
+}
+// Waits for the wave's own LDS reads too: a buffer is refilled behind it.
+__device__ __forceinline__ void barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// The 16-byte slot of a row, moved so that eight lanes with consecutive rows of
+// an operand meet eight different banks.  K rows of token t: lanes hold tokens
+// 4 a + b and 16 + 4 a + b in turn.  V rows of channel d: 64 bytes, two to a
+// line of banks.
+template <int D>
+__device__ __forceinline__ int k_slot(int t, int slot) {
+  return D == 64 ? slot ^ (((t >> 1) & 1) | ((t >> 3) & 2)) : slot ^ ((t & 3) | ((t >> 2) & 4));
+}
+__device__ __forceinline__ int v_slot(int d, int slot) { return slot ^ ((d >> 1) & 3); }
+
+template <int D>
+__global__ void __launch_bounds__(256, D == 256 ? 1 : 2) kv8_prompt_kernel(AttnArgs a) {
+  constexpr int kC = D / 32;               // 32-channel parts of a row
+  constexpr int kBytes = kPage * D;        // codes of a page and head
+  constexpr int kLoads = kBytes / 4096;    // 16-byte loads of a thread for K, and for V
+  extern __shared__ uint8_t lds[];         // two buffers of K, V
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int col = lane & 31, hh = lane >> 5;
+  const int head = (int)blockIdx.x % a.kv_heads, b = (int)blockIdx.x / a.kv_heads;
+  const KvSeq seq = kv_seq(a.cu, a.lengths, b, a.T);
+  const int rows = seq.count * a.group;   // T * heads < 2^30
+  const int tiles = (rows + kPromptRows - 1) / kPromptRows;
+  const int32_t* const table = a.table + (int64_t)b * a.max_pages;
+  const float sign = a.scale_log2 < 0.0f ? -1.0f : 1.0f;
+
+  // Where this thread's 16-byte loads of a page come from (K, then V): slot s
+  // of LDS, in order, takes the row's slot that is moved there.
+  uint32_t from_k[kLoads], from_v[kLoads];
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i) {
+    const int s = i * 256 + tid;
+    const int t = s / (D / 16), ks = s % (D / 16), d = s / 4, vs = s % 4;
+    from_k[i] = (uint32_t)(t * D + 16 * k_slot<D>(t, ks));
+    from_v[i] = (uint32_t)(d * kPage + 16 * v_slot(d, vs));
+  }
+
+  // Tiles from the sequence's end: those that see most come first.
+  for (int tile = tiles - 1 - (int)blockIdx.y; tile >= 0; tile -= (int)gridDim.y) {
+    const int row0 = tile * kPromptRows;
+    const int last_row = min(row0 + kPromptRows, rows) - 1;
+    const int wrow0 = min(row0 + 32 * wave, last_row), wrow1 = min(row0 + 32 * wave + 31, last_row);
+    const int row = min(row0 + 32 * wave + col, last_row);   // lanes past the end repeat the last row
+    const int token = row / a.group, g = row % a.group;
+    const int pos = seq.start + token;
+    const int wmin = __builtin_amdgcn_readfirstlane(seq.start + wrow0 / a.group);
+    const int wmax = __builtin_amdgcn_readfirstlane(seq.start + wrow1 / a.group);
+    const Visible vis = visible_pages(seq.start + row0 / a.group, seq.start + last_row / a.group,
+                                      a.window, a.sinks, a.max_pages);
+    const int begin = (int)((int64_t)vis.total * blockIdx.z / a.splits);
+    const int end = (int)((int64_t)vis.total * (blockIdx.z + 1) / a.splits);
+
+    // Queries: chunk (C, e) gives lane (col, hh) channels 32 C + 16 hh + 8 e and up.
+    half8 qf[kC][2];
+    const __half* const qrow = a.q + (int64_t)(seq.first_row + token) * a.ld_q + (int64_t)(head * a.group + g) * D;
+#pragma unroll
+    for (int C = 0; C < kC; ++C)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        qf[C][e] = *reinterpret_cast<const half8*>(qrow + 32 * C + 16 * hh + 8 * e);
+        qf[C][e] *= (_Float16)sign;
+      }
+
+    float16v o[D / 32];
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[t][e] = 0.0f;
+    float m = -INFINITY, l = 0.0f, unit = 0.0f;   // unit 0: none yet
+
+    // A page's codes into a buffer, with its scales and the table's entry of
+    // the place after it.  Pages that are not there are passed over.
+    const auto there = [&](int page) { return (uint32_t)page < (uint32_t)a.num_pages; };
+    const auto entry = [&](int i) { return i < end ? table[vis.page(i)] : -1; };
+    const auto fetch = [&](int page, int i, int buf) {
+      Ahead x{entry(i + 1), 0.0f, 0.0f};
+      if (!there(page)) return x;
+      const int64_t which = (int64_t)page * a.kv_heads + head, at = which * kBytes;
+      x.ks = a.k_scales[which];
+      x.vs = a.v_scales[which];
+      const uint32_t to = (uint32_t)(buf * 2 * kBytes + wave * 1024);
+#pragma unroll
+      for (int n = 0; n < kLoads; ++n) load_lds16(a.k_pages + at, from_k[n], to + n * 4096);
+#pragma unroll
+      for (int n = 0; n < kLoads; ++n) load_lds16(a.v_pages + at, from_v[n], to + kBytes + n * 4096);
+      return x;
+    };
+
+    int page = __builtin_amdgcn_readfirstlane(entry(begin)), buf = 0;
+    Ahead ahead = fetch(page, begin, 0);
+    for (int i = begin; i < end; ++i, buf ^= 1) {
+      const int j0 = vis.page(i) * kPage;
+      const bool here = there(page);
+      wait_loads(ahead);
+      const float ks = uniform(ahead.ks), vs = uniform(ahead.vs);
+      page = __builtin_amdgcn_readfirstlane(ahead.page);
+      barrier();   // everyone's loads are in, and everyone is done with the other buffer
+      ahead = fetch(page, i + 1, buf ^ 1);
+      const uint8_t* const kb = lds + buf * 2 * kBytes;
+      const uint8_t* const vb = kb + kBytes;
+      if (here && page_any(j0, wmin, wmax, a.window, a.sinks)) {
+        // S^T of the half pages u: row 8 x + 4 h + y of the operand is token
+        // 32 u + 16 h + 4 x + y.
+        float16v s[2];
+        const int ktok = 16 * ((col >> 2) & 1) + 4 * (col >> 3) + (col & 3);
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) s[u][e] = 0.0f;
+          const int t = 32 * u + ktok;
+#pragma unroll
+          for (int C = 0; C < kC; ++C) {
+            const uint4 kc = *reinterpret_cast<const uint4*>(kb + t * D + 16 * k_slot<D>(t, 2 * C + hh));
+            s[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(codes8(kc.x, kc.y), qf[C][0], s[u], 0, 0, 0);
+            s[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(codes8(kc.z, kc.w), qf[C][1], s[u], 0, 0, 0);
+          }
+        }
+        if (!page_whole(j0, wmin, wmax, a.window, a.sinks)) {
+#pragma unroll
+          for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+              s[u][e] = sees(pos, j0 + 32 * u + 16 * hh + e, a.window, a.sinks) ? s[u][e] : -INFINITY;
+        }
+        // c > 0 also where the scale is 0: -inf stays -inf.
+        const float c = fmaxf(fabsf(a.scale_log2) * ks, 1e-37f);
+        float top = s[0][0];
+#pragma unroll
+        for (int e = 1; e < 16; ++e) top = fmaxf(top, s[0][e]);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) top = fmaxf(top, s[1][e]);
+        top *= c;
+        const float ratio = unit > 0.0f ? vs / unit : 0.0f;
+        if (__any(top > m + 10.0f) || !(ratio >= 0.0625f && ratio <= 16.0f)) {
+          // Both lanes of a row (halves of the tokens) move its reference alike.
+          const float row_top = fmaxf(top, __shfl_xor(top, 32));
+          const bool up = row_top > m + 10.0f;
+          const float m_new = up ? row_top - 4.0f : m;
+          const float alpha = m == -INFINITY ? 0.0f : exp2_hw(m - m_new);
+          const bool other_unit = !(ratio >= 0.0625f && ratio <= 16.0f);
+          const float fix = alpha * (other_unit && unit > 0.0f ? unit / vs : 1.0f);
+          if (other_unit) unit = vs;
+          m = m_new;
+          l *= alpha;
+#pragma unroll
+          for (int t = 0; t < D / 32; ++t) o[t] *= fix;
+        }
+        // Weights with the v scale in them; their sum without it.
+        const float base = m == -INFINITY ? 0.0f : m;
+        const float shift = __builtin_amdgcn_logf(vs / unit) - base;
+        float sum = 0.0f;
+        half8 p[2][2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const float x = exp2_hw(fmaf(s[u][e], c, shift));
+            sum += x;
+            p[u][e / 8][e % 8] = (_Float16)x;
+          }
+        l = fmaf(sum, unit / vs, l);
+        // Slots past the sequence's end may hold anything: no NaN of theirs may
+        // meet the zero weight.
+        const bool ends = j0 + kPage > seq.length;
+#pragma unroll
+        for (int t = 0; t < D / 32; ++t) {
+          const int d = 32 * t + col;
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            uint4 vc = *reinterpret_cast<const uint4*>(vb + d * kPage + 16 * v_slot(d, 2 * u + hh));
+            if (ends) {
+              const int held = seq.length - j0 - 32 * u - 16 * hh;
+              vc.x &= held_mask(held, 0);
+              vc.y &= held_mask(held, 4);
+              vc.z &= held_mask(held, 8);
+              vc.w &= held_mask(held, 12);
+            }
+            o[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(codes8(vc.x, vc.y), p[u][0], o[t], 0, 0, 0);
+            o[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(codes8(vc.z, vc.w), p[u][1], o[t], 0, 0, 0);
+          }
+        }
+      }
+    }
+    l += __shfl_xor(l, 32);
+
+    if (row0 + 32 * wave + col < rows) {
+      const int64_t to = ((int64_t)seq.first_row + token) * a.heads + head * a.group + g;
+      if (a.splits == 1) {
+        const float f = l > 0.0f ? unit / l : l;   // 0: nothing seen; NaN stays
+#pragma unroll
+        for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            __half2 h[2];
+            h[0] = __floats2half2_rn(o[t][4 * x] * f, o[t][4 * x + 1] * f);
+            h[1] = __floats2half2_rn(o[t][4 * x + 2] * f, o[t][4 * x + 3] * f);
+            *reinterpret_cast<uint2*>(a.out + to * D + 32 * t + 8 * x + 4 * hh) = *reinterpret_cast<const uint2*>(h);
+          }
+        if (hh == 0) a.lse[to] = m * kLn2 + logf(l);
+      } else {
+        const int64_t slot = (int64_t)blockIdx.z * a.T * a.heads + to;
+#pragma unroll
+        for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+          for (int x = 0; x < 4; ++x)
+            *reinterpret_cast<float4v*>(a.part_o + slot * D + 32 * t + 8 * x + 4 * hh) =
+                float4v{o[t][4 * x], o[t][4 * x + 1], o[t][4 * x + 2], o[t][4 * x + 3]} * unit;
+        if (hh == 0) a.part_ml[slot] = make_float2(m, l);
+      }
+    }
+    barrier();   // the buffers are free for the next tile
+  }
+}
+
+template <int D>
+hipError_t launch(const AttnArgs& a, int64_t B, int64_t max_q, hipStream_t stream) {
+  constexpr int kLds = 4 * kPage * D;
+  const int64_t tiles = (max_q * a.group + kPromptRows - 1) / kPromptRows;
+  const dim3 grid((unsigned)(B * a.kv_heads), (unsigned)(tiles < 65535 ? tiles : 65535), (unsigned)a.splits);
+  kv8_prompt_kernel<D><<<grid, 256, kLds, stream>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_kv8_prompt(const AttnArgs& a, int head_dim, int64_t B, int64_t max_q, hipStream_t stream) {
+  switch (head_dim) {
+    case 64: return launch<64>(a, B, max_q, stream);
+    case 128: return launch<128>(a, B, max_q, stream);
+    case 256: return launch<256>(a, B, max_q, stream);
+    default: return hipErrorInvalidValue;
+  }
+}
+
+}  // namespace dptq
