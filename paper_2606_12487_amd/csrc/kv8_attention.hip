@@ -27,19 +27,31 @@ namespace dptq {
 namespace {
 
 // 16 rows (queries of one KV head of one sequence; row r is query token
-// r / group, head r % group of the group) by one split of the visible pages.
-// Each of the four waves takes every fourth page of the split.
+// r / group, head r % group of the group) by one part of the visible pages.
+// Each of the four waves takes every fourth page of the part, straight from
+// memory into the registers that feed the matrix cores: K of the next page is
+// loaded behind the scores, V behind the second product.
+//
+// The softmax keeps a reference m instead of the running maximum: weights are
+// 2^(s - m), and m moves (with the sums and O rescaled) only where a score
+// passes m + 10, then to 4 below it.  A page's v scale goes into the exponent
+// as its ratio to the unit U of O, 2^-4 to 2^4; another unit is taken, with O
+// rescaled, where the ratio leaves that range.  Weights stay below 2^15, within
+// fp16, and are never below their exact size relative to the row's largest.
 template <int D>
-__global__ void __launch_bounds__(256) kv8_decode_kernel(AttnArgs a) {
+__global__ void __launch_bounds__(256, D == 64 ? 4 : D == 128 ? 3 : 1) kv8_decode_kernel(AttnArgs a) {
   constexpr int kC = D / 64;     // 64-channel parts of a row
   constexpr int kT = D / 16;     // 16-channel tiles of the output
   __shared__ float sum_o[16 * D];
   __shared__ float2 wave_ml[4][16];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int col = lane & 15, quad = lane >> 4;
   const int head = (int)blockIdx.x % a.kv_heads, b = (int)blockIdx.x / a.kv_heads;
   const KvSeq seq = kv_seq(a.cu, a.lengths, b, a.T);
   const int rows = seq.count * a.group;   // T * heads < 2^30
+  const int32_t* const table = a.table + (int64_t)b * a.max_pages;
+  const float sign = a.scale_log2 < 0.0f ? -1.0f : 1.0f;
 
   for (int row0 = (int)blockIdx.y * 16; row0 < rows; row0 += (int)gridDim.y * 16) {
     const int row = min(row0 + col, rows - 1);    // lanes past the end repeat the last row
@@ -48,8 +60,8 @@ __global__ void __launch_bounds__(256) kv8_decode_kernel(AttnArgs a) {
     const int pmin = seq.start + row0 / a.group;
     const int pmax = seq.start + min(row0 + 15, rows - 1) / a.group;
     const Visible vis = visible_pages(pmin, pmax, a.window, a.sinks, a.max_pages);
-    const int begin = (int)((int64_t)vis.total * blockIdx.z / a.splits);
-    const int end = (int)((int64_t)vis.total * (blockIdx.z + 1) / a.splits);
+    const int begin = min((int)blockIdx.z * a.chunk, vis.total);
+    const int end = (int)blockIdx.z == a.splits - 1 ? vis.total : min(begin + a.chunk, vis.total);
 
     // Queries: chunk (C, e) of 32 channels gives lane (col, quad) the channels
     // 64 C + 16 quad + 8 e and up, as K's 16-byte loads hold them.
@@ -58,80 +70,125 @@ __global__ void __launch_bounds__(256) kv8_decode_kernel(AttnArgs a) {
 #pragma unroll
     for (int C = 0; C < kC; ++C)
 #pragma unroll
-      for (int e = 0; e < 2; ++e)
+      for (int e = 0; e < 2; ++e) {
         qf[C][e] = *reinterpret_cast<const half8*>(qrow + 64 * C + 16 * quad + 8 * e);
+        qf[C][e] *= (_Float16)sign;
+      }
 
     float4v o[kT];
 #pragma unroll
     for (int t = 0; t < kT; ++t) o[t] = float4v{0, 0, 0, 0};
-    float m = -INFINITY, l = 0.0f, unit = 1.0f;
+    float m = -INFINITY, l = 0.0f, unit = 0.0f;   // unit 0: none yet
 
-    for (int i = begin + wave; i < end; i += 4) {
-      const int blk = vis.page(i);
-      const int page = a.table[(int64_t)b * a.max_pages + blk];
-      if ((uint32_t)page >= (uint32_t)a.num_pages) continue;
-      const int64_t at = (int64_t)page * a.kv_heads + head;
-      const uint8_t* const kp = a.k_pages + at * (kPage * D);
-      const uint8_t* const vp = a.v_pages + at * (kPage * D);
-      const float ks = a.scale_log2 * a.k_scales[at], vs = a.v_scales[at];
+    // S^T: row x of tile t4 is token 16 (x / 4) + 4 t4 + x % 4, so that lane
+    // (col, quad) ends with tokens 16 quad + 4 t4 + i.
+    uint4 kc[4][kC], vc[kT];
+    const uint32_t k_at = (uint32_t)((16 * (col >> 2) + (col & 3)) * D + 16 * quad);
+    const uint32_t v_at = (uint32_t)(col * kPage + 16 * quad);
+    // A page that is not there: page 0 is read, and all of it is masked.
+    const auto there = [&](int page) { return (uint32_t)page < (uint32_t)a.num_pages; };
+    const auto which = [&](int page) { return (int64_t)(there(page) ? page : 0) * a.kv_heads + head; };
+    const auto load_k = [&](int64_t at) {
+#pragma unroll
+      for (int t4 = 0; t4 < 4; ++t4)
+#pragma unroll
+        for (int C = 0; C < kC; ++C)
+          kc[t4][C] = *reinterpret_cast<const uint4*>(a.k_pages + at * (kPage * D) + k_at + 4 * t4 * D + 64 * C);
+    };
+    const auto load_v = [&](int64_t at) {
+#pragma unroll
+      for (int t = 0; t < kT; ++t)
+        vc[t] = *reinterpret_cast<const uint4*>(a.v_pages + at * (kPage * D) + v_at + 16 * t * kPage);
+    };
 
-      // S^T: row m of tile t4 is token 16 (m / 4) + 4 t4 + m % 4, so that lane
-      // (col, quad) ends with tokens 16 quad + 4 t4 + i.
-      float s[16];
+    int i = begin + wave;
+    if (i < end) {
+      int page = table[vis.page(i)];
+      int page1 = i + 4 < end ? table[vis.page(i + 4)] : -1;
+      load_k(which(page));
+      load_v(which(page));
+      float ks = a.k_scales[which(page)], vs = a.v_scales[which(page)];
+      for (; i < end; i += 4) {
+        const bool more = i + 4 < end;
+        const int page2 = i + 8 < end ? table[vis.page(i + 8)] : -1;
+        float s[16];
 #pragma unroll
-      for (int t4 = 0; t4 < 4; ++t4) {
-        float4v acc = {0, 0, 0, 0};
-        const uint8_t* const krow = kp + (16 * (col >> 2) + 4 * t4 + (col & 3)) * D + 16 * quad;
+        for (int t4 = 0; t4 < 4; ++t4) {
+          float4v acc = {0, 0, 0, 0};
 #pragma unroll
-        for (int C = 0; C < kC; ++C) {
-          const uint4 kc = *reinterpret_cast<const uint4*>(krow + 64 * C);
-          acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8(kc.x, kc.y), qf[C][0], acc, 0, 0, 0);
-          acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8(kc.z, kc.w), qf[C][1], acc, 0, 0, 0);
+          for (int C = 0; C < kC; ++C) {
+            acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8(kc[t4][C].x, kc[t4][C].y), qf[C][0], acc, 0, 0, 0);
+            acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8(kc[t4][C].z, kc[t4][C].w), qf[C][1], acc, 0, 0, 0);
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[4 * t4 + e] = acc[e];
         }
+        const float c = fmaxf(fabsf(a.scale_log2) * ks, 1e-37f);   // > 0 also where the scale is 0: -inf stays -inf
+        const float v_scale = vs;
+        if (more) {
+          load_k(which(page1));
+          ks = a.k_scales[which(page1)];
+          vs = a.v_scales[which(page1)];
+        }
+        const int j0 = there(page) ? vis.page(i) * kPage : 1 << 30;
+        if (!page_whole(j0, pmin, pmax, a.window, a.sinks)) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[4 * t4 + e] = acc[e] * ks;
-      }
-      // Masks, where the page is not visible as a whole to every row.
-      const int j0 = blk * kPage;
-      if (!page_whole(j0, pmin, pmax, a.window, a.sinks)) {
+          for (int e = 0; e < 16; ++e)
+            s[e] = sees(pos, j0 + 16 * quad + e, a.window, a.sinks) ? s[e] : -INFINITY;
+        }
+        float top = s[0];
 #pragma unroll
-        for (int e = 0; e < 16; ++e)
-          s[e] = sees(pos, j0 + 16 * quad + e, a.window, a.sinks) ? s[e] : -INFINITY;
-      }
-      float top = s[0];
+        for (int e = 1; e < 16; ++e) top = fmaxf(top, s[e]);
+        top *= c;
+        const float ratio = unit > 0.0f ? v_scale / unit : 0.0f;
+        const bool other_unit = !(ratio >= 0.0625f && ratio <= 16.0f) && there(page);
+        if (__any(top > m + 10.0f) || other_unit) {
+          // The four lanes of a row move its reference alike.
+          float row_top = fmaxf(top, __shfl_xor(top, 16));
+          row_top = fmaxf(row_top, __shfl_xor(row_top, 32));
+          const float m_new = row_top > m + 10.0f ? row_top - 4.0f : m;
+          const float alpha = m == -INFINITY ? 0.0f : exp2_hw(m - m_new);
+          const float fix = alpha * (other_unit && unit > 0.0f ? unit / v_scale : 1.0f);
+          if (other_unit) unit = v_scale;
+          m = m_new;
+          l *= alpha;
 #pragma unroll
-      for (int e = 1; e < 16; ++e) top = fmaxf(top, s[e]);
-      top = fmaxf(top, __shfl_xor(top, 16));
-      top = fmaxf(top, __shfl_xor(top, 32));
-      const float m_new = fmaxf(m, top);
-      const float base = m_new == -INFINITY ? 0.0f : m_new;
-      const float alpha = exp2_hw(m - base);
-      m = m_new;
-      l *= alpha;
-      half8 p[2];
+          for (int t = 0; t < kT; ++t) o[t] *= fix;
+        }
+        // Weights with the v scale in them; their sum without it.
+        const float base = m == -INFINITY ? 0.0f : m;
+        const float by = there(page) ? v_scale / unit : 1.0f;
+        const float shift = __builtin_amdgcn_logf(by) - base;
+        half8 p[2];
+        float sum = 0.0f;
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const float x = exp2_hw(s[e] - base);
-        l += x;
-        p[e / 8][e % 8] = (_Float16)x;
-      }
-      const float fix = alpha * (unit / vs);
-      unit = vs;
-      // O^T: lane (col, quad) gives channel 16 t + col of tokens 16 quad and
-      // up.  Slots past the sequence's end may hold anything: no NaN of theirs
-      // may meet the zero weight.
-      const int held = seq.length - j0 - 16 * quad;   // valid slots of this lane's 16
-#pragma unroll
-      for (int t = 0; t < kT; ++t) {
-        uint4 vc = *reinterpret_cast<const uint4*>(vp + (16 * t + col) * kPage + 16 * quad);
+        for (int e = 0; e < 16; ++e) {
+          const float x = exp2_hw(fmaf(s[e], c, shift));
+          sum += x;
+          p[e / 8][e % 8] = (_Float16)x;
+        }
+        l = fmaf(sum, 1.0f / by, l);
+        // O^T: lane (col, quad) gives channel 16 t + col of tokens 16 quad and
+        // up.  Slots past the sequence's end may hold anything: no NaN of
+        // theirs may meet the zero weight.
         if (j0 + kPage > seq.length) {
-          uint32_t* const w = &vc.x;
+          const int held = seq.length - j0 - 16 * quad;   // valid slots of this lane's 16
 #pragma unroll
-          for (int d = 0; d < 4; ++d) w[d] &= held_mask(held, 4 * d);
+          for (int t = 0; t < kT; ++t) {
+            vc[t].x &= held_mask(held, 0);
+            vc[t].y &= held_mask(held, 4);
+            vc[t].z &= held_mask(held, 8);
+            vc[t].w &= held_mask(held, 12);
+          }
         }
-        o[t] *= fix;
-        o[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8(vc.x, vc.y), p[0], o[t], 0, 0, 0);
-        o[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8(vc.z, vc.w), p[1], o[t], 0, 0, 0);
+#pragma unroll
+        for (int t = 0; t < kT; ++t) {
+          o[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8(vc[t].x, vc[t].y), p[0], o[t], 0, 0, 0);
+          o[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8(vc[t].z, vc[t].w), p[1], o[t], 0, 0, 0);
+        }
+        if (more) load_v(which(page1));
+        page = page1;
+        page1 = page2;
       }
     }
     l += __shfl_xor(l, 16);
@@ -170,7 +227,7 @@ __global__ void __launch_bounds__(256) kv8_decode_kernel(AttnArgs a) {
         if (d == 0) a.lse[to] = ml.x * kLn2 + logf(ml.y);
       } else {
         const int64_t at = (int64_t)blockIdx.z * a.T * a.heads + to;
-        a.part_o[at * D + d] = sum_o[e];
+        if (begin < end) a.part_o[at * D + d] = sum_o[e];   // parts without pages come last
         if (d == 0) a.part_ml[at] = ml;
       }
     }
@@ -178,27 +235,98 @@ __global__ void __launch_bounds__(256) kv8_decode_kernel(AttnArgs a) {
   }
 }
 
-// Joins the splits of one row: a wave a row.
+// Joins the parts of one row, a wave a row: few parts.
+constexpr int kFewSplits = 8;
+template <int D>
+__global__ void __launch_bounds__(256) kv8_combine_few_kernel(AttnArgs a) {
+  constexpr int kV = D / 64;
+  const int64_t n = (int64_t)a.T * a.heads;
+  const int lane = threadIdx.x & 63;
+  for (int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); row < n; row += (int64_t)gridDim.x * 4) {
+    float2 ml[kFewSplits];
+    float M = -INFINITY, L = 0.0f, o[kV] = {};
+#pragma unroll
+    for (int s = 0; s < kFewSplits; ++s) {
+      ml[s] = s < a.splits ? a.part_ml[s * n + row] : make_float2(-INFINITY, 0.0f);
+      M = fmaxf(M, ml[s].x);
+    }
+    const float ref = M == -INFINITY ? 0.0f : M;
+#pragma unroll
+    for (int s = 0; s < kFewSplits; ++s) {
+      if (ml[s].y == 0.0f) continue;   // it saw nothing
+      const float f = exp2_hw(ml[s].x - ref);
+      L += f * ml[s].y;
+#pragma unroll
+      for (int i = 0; i < kV; ++i) o[i] += f * a.part_o[(s * n + row) * D + 64 * i + lane];
+    }
+#pragma unroll
+    for (int i = 0; i < kV; ++i) a.out[row * D + 64 * i + lane] = __float2half_rn(L > 0.0f ? o[i] / L : L);
+    if (lane == 0) a.lse[row] = M * kLn2 + logf(L);
+  }
+}
+
+// The same, a workgroup a row, each wave every fourth part.
 template <int D>
 __global__ void __launch_bounds__(256) kv8_combine_kernel(AttnArgs a) {
+  constexpr int kV = D / 64;
+  __shared__ float factor[kMaxSplits];
+  __shared__ float wave_max[4], wave_sum[4];
+  __shared__ int wave_used[4];
+  __shared__ float part[4][D];
   const int64_t n = (int64_t)a.T * a.heads;
-  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (row >= n) return;
-  const int lane = threadIdx.x & 63;
-  float M = -INFINITY;
-  for (int s = 0; s < a.splits; ++s) M = fmaxf(M, a.part_ml[s * n + row].x);
-  const float ref = M == -INFINITY ? 0.0f : M;
-  float L = 0.0f, o[D / 64] = {};
-  for (int s = 0; s < a.splits; ++s) {
-    const float2 ml = a.part_ml[s * n + row];
-    const float f = exp2_hw(ml.x - ref);
-    L += f * ml.y;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  for (int64_t row = blockIdx.x; row < n; row += gridDim.x) {
+    float M = -INFINITY;
+    int used = 0;   // parts up to the last that saw anything
+    float2 ml[kMaxSplits / 256];
 #pragma unroll
-    for (int i = 0; i < D / 64; ++i) o[i] += f * a.part_o[(s * n + row) * D + 64 * i + lane];
+    for (int i = 0; i < kMaxSplits / 256; ++i) {
+      const int s = threadIdx.x + 256 * i;
+      ml[i] = s < a.splits ? a.part_ml[s * n + row] : make_float2(-INFINITY, 0.0f);
+      M = fmaxf(M, ml[i].x);
+      if (ml[i].y != 0.0f) used = s + 1;
+    }
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) {
+      M = fmaxf(M, __shfl_xor(M, off));
+      used = max(used, __shfl_xor(used, off));
+    }
+    if (lane == 0) wave_max[wave] = M, wave_used[wave] = used;
+    __syncthreads();
+    used = max(max(wave_used[0], wave_used[1]), max(wave_used[2], wave_used[3]));
+    M = fmaxf(fmaxf(wave_max[0], wave_max[1]), fmaxf(wave_max[2], wave_max[3]));
+    const float ref = M == -INFINITY ? 0.0f : M;
+    float L = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kMaxSplits / 256; ++i) {
+      const int s = threadIdx.x + 256 * i;
+      const float f = exp2_hw(ml[i].x - ref);
+      if (s < a.splits) factor[s] = f;
+      L += f * ml[i].y;
+    }
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) L += __shfl_xor(L, off);
+    if (lane == 0) wave_sum[wave] = L;
+    __syncthreads();
+    L = (wave_sum[0] + wave_sum[1]) + (wave_sum[2] + wave_sum[3]);
+    float o[kV] = {};
+#pragma unroll 4
+    for (int s = wave; s < used; s += 4) {
+      const float* const src = a.part_o + (s * n + row) * D + lane;
+      const float f = factor[s];
+#pragma unroll
+      for (int i = 0; i < kV; ++i) o[i] += f * src[64 * i];
+    }
+#pragma unroll
+    for (int i = 0; i < kV; ++i) part[wave][64 * i + lane] = o[i];
+    __syncthreads();
+    for (int d = threadIdx.x; d < D; d += 256) {
+      const float x = (part[0][d] + part[1][d]) + (part[2][d] + part[3][d]);
+      a.out[row * D + d] = __float2half_rn(L > 0.0f ? x / L : L);
+    }
+    if (threadIdx.x == 0) a.lse[row] = M * kLn2 + logf(L);
+    __syncthreads();
   }
-#pragma unroll
-  for (int i = 0; i < D / 64; ++i) a.out[row * D + 64 * i + lane] = __float2half_rn(L > 0.0f ? o[i] / L : L);
-  if (lane == 0) a.lse[row] = M * kLn2 + logf(L);
 }
 
 // Rows of a sequence's largest count that the tiles of 16 still take; more go
@@ -207,19 +335,28 @@ constexpr int64_t kDecodeRows = 32;
 
 bool is_prompt(const Kv8Attention& c) { return c.max_q * (c.heads / c.cache.kv_heads) > kDecodeRows; }
 
-// Splits of the visible pages: enough workgroups for two on every compute
-// unit, of four pages (one a wave) or more.
-int choose_splits(const Kv8Attention& c) {
+// Parts of the visible pages, and the pages of a part (the last one takes what
+// is left): enough workgroups for kFill on each compute unit, of four pages
+// (one a wave) or more.
+constexpr int64_t kFill = 8;
+struct Split {
+  int chunk, splits;
+};
+Split choose_split(const Kv8Attention& c) {
   const int64_t height = is_prompt(c) ? kPromptRows : 16;
   const int64_t tiles =
       ((c.max_q * (c.heads / c.cache.kv_heads) + height - 1) / height) * c.cache.B * c.cache.kv_heads;
-  int64_t keys = c.max_len;
-  if (c.window > 0 && (int64_t)c.window + c.sinks + c.max_q + 2 * kPage < keys)
-    keys = (int64_t)c.window + c.sinks + c.max_q + 2 * kPage;
-  const int64_t most = (keys + 4 * kPage - 1) / (4 * kPage);
-  const int64_t want = (2 * (int64_t)device_cus() + tiles - 1) / tiles;
-  const int64_t s = want < most ? want : most;
-  return (int)(s < 1 ? 1 : s > 256 ? 256 : s);
+  // What a tile sees: behind a window, that of its tokens, the sinks, and parts of pages at three ends.
+  const int64_t tokens = height / (c.heads / c.cache.kv_heads) + 1;
+  const int64_t seen = c.window > 0 ? c.window + (int64_t)c.sinks + tokens + 3 * kPage : c.max_len;
+  const int64_t pages = ((seen < c.max_len ? seen : c.max_len) + kPage - 1) / kPage;
+  const int64_t fill = (is_prompt(c) ? 2 : kFill) * device_cus();
+  int64_t chunk = (tiles * pages + fill - 1) / fill;
+  chunk = (chunk + 3) / 4 * 4;
+  if (chunk < 4) chunk = 4;
+  if (chunk * kMaxSplits < pages) chunk = (pages + kMaxSplits - 1) / kMaxSplits;
+  const int64_t splits = pages < 1 ? 1 : (pages + chunk - 1) / chunk;
+  return Split{(int)chunk, (int)splits};
 }
 
 template <int D>
@@ -235,14 +372,18 @@ hipError_t launch(const AttnArgs& a, const Kv8Attention& c, hipStream_t stream) 
     e = hipGetLastError();
   }
   if (e != hipSuccess || a.splits == 1) return e;
-  kv8_combine_kernel<D><<<(unsigned)(((int64_t)a.T * a.heads + 3) / 4), 256, 0, stream>>>(a);
+  const int64_t out_rows = (int64_t)a.T * a.heads;
+  const int64_t groups = a.splits <= kFewSplits ? (out_rows + 3) / 4 : out_rows;
+  const unsigned grid = (unsigned)(groups < 65536 ? groups : 65536);
+  if (a.splits <= kFewSplits) kv8_combine_few_kernel<D><<<grid, 256, 0, stream>>>(a);
+  else kv8_combine_kernel<D><<<grid, 256, 0, stream>>>(a);
   return hipGetLastError();
 }
 
 }  // namespace
 
 int64_t kv8_attention_workspace(const Kv8Attention& c) {
-  const int splits = choose_splits(c);
+  const int splits = choose_split(c).splits;
   return splits == 1 ? 0 : (int64_t)splits * c.cache.T * c.heads * (c.cache.head_dim * 4 + 8);
 }
 
@@ -258,7 +399,7 @@ hipError_t launch_kv8_attention(const Kv8Attention& c, hipStream_t stream) {
   a.lengths = c.cache.lengths;
   a.table = c.cache.table;
   a.T = (int)c.cache.T;
-  a.max_pages = (int)c.cache.max_pages;
+  a.max_pages = c.cache.num_pages > 0 ? (int)c.cache.max_pages : 0;   // no pages: nothing is seen
   a.num_pages = (int)c.cache.num_pages;
   a.heads = c.heads;
   a.kv_heads = c.cache.kv_heads;
@@ -266,7 +407,9 @@ hipError_t launch_kv8_attention(const Kv8Attention& c, hipStream_t stream) {
   a.scale_log2 = c.scale * kLog2e;
   a.window = c.window;
   a.sinks = c.sinks;
-  a.splits = choose_splits(c);
+  const Split split = choose_split(c);
+  a.chunk = split.chunk;
+  a.splits = split.splits;
   a.out = static_cast<__half*>(c.out);
   a.lse = c.lse;
   a.part_o = static_cast<float*>(c.workspace);

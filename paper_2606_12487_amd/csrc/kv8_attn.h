@@ -14,6 +14,8 @@ typedef float float16v __attribute__((ext_vector_type(16)));
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
+constexpr int kMaxSplits = 512;
+
 struct AttnArgs {
   const __half* q;
   int64_t ld_q;
@@ -23,7 +25,7 @@ struct AttnArgs {
   int T, max_pages, num_pages, heads, kv_heads, group;
   float scale_log2;        // scale * log2(e)
   int window, sinks;       // window 0: none
-  int splits;
+  int chunk, splits;       // pages of a part; the last part takes what is left
   __half* out;
   float* lse;
   float* part_o;           // [splits][T * heads][D], relative to their maxima
@@ -55,7 +57,7 @@ struct Visible {
 };
 
 __device__ __forceinline__ Visible visible_pages(int pmin, int pmax, int window, int sinks, int max_pages) {
-  if (pmax < 0) return Visible{0, 0, 0};
+  if (pmax < 0 || max_pages == 0) return Visible{0, 0, 0};
   const int low = window > 0 ? max(pmin - window + 1, 0) : 0;
   const int last = min(pmax / kPage, max_pages - 1);
   const int sink_pages = window > 0 ? min((min(sinks, low) + kPage - 1) / kPage, last + 1) : 0;

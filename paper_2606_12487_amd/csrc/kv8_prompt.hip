@@ -96,8 +96,8 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) kv8_prompt_kernel(AttnA
     const int wmax = __builtin_amdgcn_readfirstlane(seq.start + wrow1 / a.group);
     const Visible vis = visible_pages(seq.start + row0 / a.group, seq.start + last_row / a.group,
                                       a.window, a.sinks, a.max_pages);
-    const int begin = (int)((int64_t)vis.total * blockIdx.z / a.splits);
-    const int end = (int)((int64_t)vis.total * (blockIdx.z + 1) / a.splits);
+    const int begin = min((int)blockIdx.z * a.chunk, vis.total);
+    const int end = (int)blockIdx.z == a.splits - 1 ? vis.total : min(begin + a.chunk, vis.total);
 
     // Queries: chunk (C, e) gives lane (col, hh) channels 32 C + 16 hh + 8 e and up.
     half8 qf[kC][2];
@@ -248,12 +248,14 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) kv8_prompt_kernel(AttnA
         if (hh == 0) a.lse[to] = m * kLn2 + logf(l);
       } else {
         const int64_t slot = (int64_t)blockIdx.z * a.T * a.heads + to;
+        if (begin < end) {   // parts without pages come last
 #pragma unroll
-        for (int t = 0; t < D / 32; ++t)
+          for (int t = 0; t < D / 32; ++t)
 #pragma unroll
-          for (int x = 0; x < 4; ++x)
-            *reinterpret_cast<float4v*>(a.part_o + slot * D + 32 * t + 8 * x + 4 * hh) =
-                float4v{o[t][4 * x], o[t][4 * x + 1], o[t][4 * x + 2], o[t][4 * x + 3]} * unit;
+            for (int x = 0; x < 4; ++x)
+              *reinterpret_cast<float4v*>(a.part_o + slot * D + 32 * t + 8 * x + 4 * hh) =
+                  float4v{o[t][4 * x], o[t][4 * x + 1], o[t][4 * x + 2], o[t][4 * x + 3]} * unit;
+        }
         if (hh == 0) a.part_ml[slot] = make_float2(m, l);
       }
     }

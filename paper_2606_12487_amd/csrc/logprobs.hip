@@ -35,7 +35,7 @@ struct LogprobArgs {
   float *logprobs, *entropy, *top_logprobs;
   int64_t* top_ids;
   float4* part;   // [M][splits] (m, l, u, -)
-  int2* list;     // [M][splits][top] (bits of x, index)
+  unsigned long long* list;   // [M][splits][top] keys
 };
 
 // Sums relative to the maximum m: l = sum exp(x - m), u = sum exp(x - m) (x - m).
@@ -78,32 +78,32 @@ __device__ __forceinline__ Stats block_join(Stats s, Stats* part) {
   return join(join(part[0], part[1]), join(part[2], part[3]));
 }
 
-// (x, i) comes before (y, j).
-__device__ __forceinline__ bool before(float x, int i, float y, int j) { return x > y || (x == y && i < j); }
+// A logit and its index as one number: larger ones come first, equal logits by
+// index.  0: none.
+using Key = unsigned long long;
 
-// The best `top` values so far, in order; places that nothing has taken hold
-// (-inf, INT_MAX).
-struct TopList {
-  float x[kMaxTop];
-  int i[kMaxTop];
-};
+__device__ __forceinline__ uint32_t ordered(float x) {
+  const uint32_t u = __float_as_uint(x + 0.0f);   // -0 is 0
+  return u ^ (u >> 31 ? 0xFFFFFFFFu : 0x80000000u);
+}
+__device__ __forceinline__ float unordered(uint32_t o) { return __uint_as_float(o ^ (o >> 31 ? 0x80000000u : 0xFFFFFFFFu)); }
+__device__ __forceinline__ Key key_of(float x, int i) { return (Key)ordered(x) << 32 | (uint32_t)~i; }
+__device__ __forceinline__ float key_value(Key k) { return k ? unordered((uint32_t)(k >> 32)) : -INFINITY; }
+__device__ __forceinline__ int key_index(Key k) { return k ? (int)~(uint32_t)k : 0x7FFFFFFF; }
+
+constexpr uint32_t kOrderedLowest = 0x007FFFFFu;   // of -inf
 
 struct TopScratch {
-  TopList best, next;
-  float x[kCap + kMaxTop];
-  int i[kCap + kMaxTop];
-  float group[kThreads];
-  float wave_x[4];
-  int wave_i[4];
+  Key best[kMaxTop];   // the list so far, in order, 0 where it has room
+  Key next[kMaxTop];
+  Key found[kCap + kMaxTop];
+  uint32_t group[kThreads];
+  Key wave_best[4];
   int count;
-  float threshold;
 };
 
 __device__ __forceinline__ void clear_list(TopScratch& t, int top) {
-  if ((int)threadIdx.x < top) {
-    t.best.x[threadIdx.x] = -INFINITY;
-    t.best.i[threadIdx.x] = 0x7FFFFFFF;
-  }
+  if ((int)threadIdx.x < top) t.best[threadIdx.x] = 0;
   if (threadIdx.x == 0) t.count = 0;
   __syncthreads();
 }
@@ -112,122 +112,117 @@ __device__ __forceinline__ void clear_list(TopScratch& t, int top) {
 // negative where it has none.  Indices of later chunks are larger, so a value
 // enters only if it is larger than the list's last, or if the list has room.
 //
-// Where too many are larger (the first chunk of a row), the `top`-th largest of
-// the threads' maxima is a bound that at least `top` values reach, and few more
-// do in ordinary data.  Where that is too many as well (ties), the entries are
-// taken out one by one.
+// Where too many would (the first chunk of a row), the `top`-th largest of the
+// threads' maxima, to 16 bits, is a bound that at least `top` values reach, and
+// few more do in ordinary data.  Where that is too many as well (ties), the
+// entries are taken out one by one.
 // whole: the thread has all its values.
 template <typename Index>
 __device__ __forceinline__ void merge_chunk(const float (&v)[kPer], const Index& index, bool whole, int top,
                                             TopScratch& t) {
-  const float last = t.best.x[top - 1];
-  const bool room = t.best.i[top - 1] == 0x7FFFFFFF;
+  const Key last = t.best[top - 1];
+  const bool room = last == 0;
+  // Larger than the last: at least the next float.
+  const float least = room ? -INFINITY : unordered((uint32_t)(last >> 32) + 1);
   uint32_t mine = 0;
 #pragma unroll
-  for (int k = 0; k < kPer; ++k) mine |= v[k] > last || (room && v[k] == v[k]) ? 1u << k : 0u;
+  for (int k = 0; k < kPer; ++k) mine |= v[k] >= least ? 1u << k : 0u;
   if (!whole) {
 #pragma unroll
     for (int k = 0; k < kPer; ++k)
       if (index(k) < 0) mine &= ~(1u << k);
   }
-  const auto gather = [&](uint32_t mask) {
-    if (mask) {
-      int at = atomicAdd(&t.count, __popc(mask));
+  const auto gather = [&]() {
+    if (__any(mine != 0)) {
+      int at = mine ? atomicAdd(&t.count, __popc(mine)) : 0;
 #pragma unroll
       for (int k = 0; k < kPer; ++k)
-        if (mask >> k & 1) {
-          if (at < kCap) t.x[at] = v[k], t.i[at] = index(k);
-          ++at;
-        }
+        if (__any(mine >> k & 1))   // few are: a branch each
+          if (mine >> k & 1) {
+            if (at < kCap) t.found[at] = key_of(v[k], index(k));
+            ++at;
+          }
     }
     __syncthreads();
     return t.count;
   };
   int n = 0;
-  if (!room) n = gather(mine);
+  if (!room) n = gather();
   if (room || n > kCap) {   // the same for every thread
     float top_of_mine = -INFINITY;
 #pragma unroll
     for (int k = 0; k < kPer; ++k)
       if (mine >> k & 1) top_of_mine = fmaxf(top_of_mine, v[k]);
-    t.group[threadIdx.x] = top_of_mine;
+    t.group[threadIdx.x] = mine ? ordered(top_of_mine) : 0;
     __syncthreads();
     if (threadIdx.x == 0) t.count = 0;
-    int rank = 0;
-    for (int k = 0; k < kThreads; k += 4) {
-      const float4 g = *reinterpret_cast<const float4*>(t.group + k);
-      rank += before(g.x, k, top_of_mine, (int)threadIdx.x) + before(g.y, k + 1, top_of_mine, (int)threadIdx.x) +
-              before(g.z, k + 2, top_of_mine, (int)threadIdx.x) + before(g.w, k + 3, top_of_mine, (int)threadIdx.x);
+    const uint4 g = *reinterpret_cast<const uint4*>(t.group + 4 * (threadIdx.x & 63));
+    uint32_t bound = 0;
+    for (int bit = 31; bit >= 16; --bit) {
+      const uint32_t b = bound | 1u << bit;
+      const int reach = __popcll(__ballot(g.x >= b)) + __popcll(__ballot(g.y >= b)) + __popcll(__ballot(g.z >= b)) +
+                        __popcll(__ballot(g.w >= b));
+      if (reach >= top) bound = b;
     }
-    if (rank == top - 1) t.threshold = top_of_mine;
-    __syncthreads();
-    const float bound = t.threshold;
+    const float x = unordered(bound > kOrderedLowest ? bound : kOrderedLowest);
 #pragma unroll
     for (int k = 0; k < kPer; ++k)
-      if (!(v[k] >= bound)) mine &= ~(1u << k);
-    n = gather(mine);
+      if (!(v[k] >= x)) mine &= ~(1u << k);
+    __syncthreads();
+    n = gather();
   }
   if (n == 0) {   // and so is count
     __syncthreads();
     return;
   }
   if (n <= kCap) {
-    // Rank of each candidate and of each list entry among all of them.
+    // Ranks of the candidates and of the list's entries among all of them.
     if ((int)threadIdx.x < top) {
-      t.x[n + threadIdx.x] = t.best.x[threadIdx.x];
-      t.i[n + threadIdx.x] = t.best.i[threadIdx.x];
+      t.found[n + threadIdx.x] = t.best[threadIdx.x];
+      t.next[threadIdx.x] = 0;
     }
     __syncthreads();
     const int all = n + top;
     for (int c = threadIdx.x; c < all; c += kThreads) {
-      const float x = t.x[c];
-      const int i = t.i[c];
+      const Key mine_key = t.found[c];
       int rank = 0;
-      for (int o = 0; o < all; ++o)
-        rank += before(t.x[o], t.i[o], x, i) || (t.x[o] == x && t.i[o] == i && o < c);
-      if (rank < top) t.next.x[rank] = x, t.next.i[rank] = i;
+#pragma unroll 8
+      for (int o = 0; o < all; ++o) rank += t.found[o] > mine_key;
+      if (mine_key && rank < top) t.next[rank] = mine_key;
     }
     __syncthreads();
   } else {
-    // One by one: the best of the chunk that comes after the last one taken,
-    // against the head of the list.
-    float last_x = INFINITY;
-    int last_i = -1, head = 0;
+    // One by one: the best of the chunk after the last one taken, against the
+    // head of the list.
+    Key taken = ~(Key)0;
+    int head = 0;
     for (int out = 0; out < top; ++out) {
-      float bx = -INFINITY;
-      int bi = 0x7FFFFFFF;
+      Key best = 0;
 #pragma unroll
       for (int k = 0; k < kPer; ++k)
         if (mine >> k & 1) {
-          const int i = index(k);
-          if (before(last_x, last_i, v[k], i) && before(v[k], i, bx, bi)) bx = v[k], bi = i;
+          float x = v[k];
+          asm volatile("" : "+v"(x));   // the keys are formed again in each turn rather than held in registers
+          const Key c = key_of(x, index(k));
+          if (c < taken && c > best) best = c;
         }
 #pragma unroll
       for (int off = 32; off > 0; off >>= 1) {
-        const float ox = __shfl_xor(bx, off);
-        const int oi = __shfl_xor(bi, off);
-        if (before(ox, oi, bx, bi)) bx = ox, bi = oi;
+        const Key other = __shfl_xor(best, off);
+        if (other > best) best = other;
       }
-      if ((threadIdx.x & 63) == 0) t.wave_x[threadIdx.x >> 6] = bx, t.wave_i[threadIdx.x >> 6] = bi;
+      if ((threadIdx.x & 63) == 0) t.wave_best[threadIdx.x >> 6] = best;
       __syncthreads();
       for (int w = 0; w < 4; ++w)
-        if (before(t.wave_x[w], t.wave_i[w], bx, bi)) bx = t.wave_x[w], bi = t.wave_i[w];
-      const float hx = t.best.x[head];
-      const int hi = t.best.i[head];
-      const bool from_list = !before(bx, bi, hx, hi);
-      if (threadIdx.x == 0) {
-        t.next.x[out] = from_list ? hx : bx;
-        t.next.i[out] = from_list ? hi : bi;
-      }
-      if (from_list) ++head;
-      else last_x = bx, last_i = bi;
+        if (t.wave_best[w] > best) best = t.wave_best[w];
+      const Key old = t.best[head];
+      if (threadIdx.x == 0) t.next[out] = old > best ? old : best;
+      if (old > best) ++head;
+      else taken = best;
       __syncthreads();
     }
   }
-  if ((int)threadIdx.x < top) {
-    t.best.x[threadIdx.x] = t.next.x[threadIdx.x];
-    t.best.i[threadIdx.x] = t.next.i[threadIdx.x];
-  }
+  if ((int)threadIdx.x < top) t.best[threadIdx.x] = t.next[threadIdx.x];
   if (threadIdx.x == 0) t.count = 0;
   __syncthreads();
 }
@@ -252,7 +247,7 @@ __device__ __forceinline__ void unpack(const uint4 r, const float*, float* v) {
 
 // The row's results from its sums and list (thread 0, and a thread an entry).
 template <typename T>
-__device__ __forceinline__ void finish(const LogprobArgs& a, int64_t row, Stats s, const TopList* best) {
+__device__ __forceinline__ void finish(const LogprobArgs& a, int64_t row, Stats s, const Key* best) {
   const float log_l = logf(s.l);
   if (threadIdx.x == 0) {
     const int64_t t = a.tokens[row];
@@ -267,9 +262,9 @@ __device__ __forceinline__ void finish(const LogprobArgs& a, int64_t row, Stats 
     a.entropy[row] = s.l == 0.0f ? 0.0f : log_l - s.u / s.l;   // 0: all masked
   }
   if ((int)threadIdx.x < a.top) {
-    const float x = best->x[threadIdx.x];
+    const float x = key_value(best[threadIdx.x]);
     a.top_logprobs[row * a.top + threadIdx.x] = x == -INFINITY ? x : (x - s.m) - log_l;
-    a.top_ids[row * a.top + threadIdx.x] = min(best->i[threadIdx.x], a.V - 1);   // NaN takes no place
+    a.top_ids[row * a.top + threadIdx.x] = min(key_index(best[threadIdx.x]), a.V - 1);   // NaN takes no place
   }
 }
 
@@ -277,7 +272,7 @@ __device__ __forceinline__ void finish(const LogprobArgs& a, int64_t row, Stats 
 // before its first element: units that reach over an end are loaded element by
 // element.
 template <typename T, bool TOP>
-__global__ void __launch_bounds__(kThreads) token_logprobs_kernel(LogprobArgs a) {
+__global__ void __launch_bounds__(kThreads, 4) token_logprobs_kernel(LogprobArgs a) {
   constexpr int E = 16 / sizeof(T), kUnits = kPer / E;
   __shared__ Stats part[4];
   __shared__ TopScratch scratch;
@@ -291,10 +286,11 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_kernel(LogprobArgs a)
     if constexpr (TOP) clear_list(scratch, a.top);
     for (int c = begin; c < end; ++c) {
       float v[kPer];
-      const int64_t first = (int64_t)c * kChunk - skew;   // of the chunk; may be negative, may pass 2^31
+      const int first = c * kChunk - skew;   // of the chunk; may be negative
+      const int mine = first + (int)threadIdx.x * E;
 #pragma unroll
       for (int n = 0; n < kUnits; ++n) {
-        const int64_t i = first + (n * kThreads + (int)threadIdx.x) * E;
+        const int i = mine + n * kThreads * E;
         if (i >= 0 && i + E <= a.V) {
           unpack(*reinterpret_cast<const uint4*>(x + i), x, v + n * E);
         } else {
@@ -305,21 +301,20 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_kernel(LogprobArgs a)
       s = join(s, stats_of(v));
       if constexpr (TOP) {
         const auto index = [&](int k) {
-          const int64_t i = first + ((k / E) * kThreads + (int)threadIdx.x) * E + k % E;
-          return i < a.V ? (int)i : -1;
+          const int i = mine + (k / E) * kThreads * E + k % E;
+          return i < a.V ? i : -1;
         };
         merge_chunk(v, index, first >= 0 && first + kChunk <= a.V, a.top, scratch);
       }
     }
     s = block_join(s, part);
     if (a.splits == 1) {
-      finish<T>(a, row, s, TOP ? &scratch.best : nullptr);
+      finish<T>(a, row, s, TOP ? scratch.best : nullptr);
     } else {
       const int64_t at = row * a.splits + blockIdx.x;
       if (threadIdx.x == 0) a.part[at] = make_float4(s.m, s.l, s.u, 0.0f);
       if (TOP && (int)threadIdx.x < a.top)
-        a.list[at * a.top + threadIdx.x] =
-            make_int2(__float_as_int(scratch.best.x[threadIdx.x]), scratch.best.i[threadIdx.x]);
+        a.list[at * a.top + threadIdx.x] = scratch.best[threadIdx.x];
     }
     __syncthreads();   // part and the list are free again
   }
@@ -327,7 +322,7 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_kernel(LogprobArgs a)
 
 // Joins a row's parts, which lie in the order of their indices.
 template <typename T, bool TOP>
-__global__ void __launch_bounds__(kThreads) join_logprobs_kernel(LogprobArgs a) {
+__global__ void __launch_bounds__(kThreads, 4) join_logprobs_kernel(LogprobArgs a) {
   __shared__ Stats part[4];
   __shared__ TopScratch scratch;
   for (int64_t row = blockIdx.x; row < a.M; row += gridDim.x) {
@@ -340,21 +335,21 @@ __global__ void __launch_bounds__(kThreads) join_logprobs_kernel(LogprobArgs a) 
     if constexpr (TOP) {
       clear_list(scratch, a.top);
       const int n = a.splits * a.top;
-      const int2* const list = a.list + row * n;
+      const Key* const list = a.list + row * n;
       for (int c = 0; c < n; c += kChunk) {
         float v[kPer];
         int id[kPer];
 #pragma unroll
         for (int k = 0; k < kPer; ++k) {
           const int i = c + k * kThreads + (int)threadIdx.x;
-          const int2 e = i < n ? list[i] : make_int2(0, 0x7FFFFFFF);
-          id[k] = e.y == 0x7FFFFFFF ? -1 : e.y;
-          v[k] = id[k] < 0 ? -INFINITY : __int_as_float(e.x);
+          const Key e = i < n ? list[i] : 0;
+          id[k] = e ? key_index(e) : -1;
+          v[k] = key_value(e);
         }
         merge_chunk(v, [&](int k) { return id[k]; }, false, a.top, scratch);
       }
     }
-    finish<T>(a, row, s, TOP ? &scratch.best : nullptr);
+    finish<T>(a, row, s, TOP ? scratch.best : nullptr);
     __syncthreads();
   }
 }
@@ -388,7 +383,7 @@ hipError_t launch_token_logprobs(const TokenLogprobs& c, hipStream_t stream) {
   LogprobArgs a{c.logits, c.ld, c.M, c.V, c.top, choose_splits(c), c.tokens, c.logprobs, c.entropy,
                 c.top_logprobs, c.top_ids, nullptr, nullptr};
   a.part = static_cast<float4*>(c.workspace);
-  a.list = reinterpret_cast<int2*>(a.part + a.M * a.splits);
+  a.list = reinterpret_cast<Key*>(a.part + a.M * a.splits);
   if (c.fp32) return c.top ? launch<float, true>(a, stream) : launch<float, false>(a, stream);
   return c.top ? launch<__half, true>(a, stream) : launch<__half, false>(a, stream);
 }
