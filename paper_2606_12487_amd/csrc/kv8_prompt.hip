@@ -115,7 +115,7 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) kv8_prompt_kernel(AttnA
     for (int t = 0; t < D / 32; ++t)
 #pragma unroll
       for (int e = 0; e < 16; ++e) o[t][e] = 0.0f;
-    float m = -INFINITY, l = 0.0f, unit = 0.0f;   // unit 0: none yet
+    float m = -INFINITY, l = 0.0f, unit = 0.0f, inv_unit = 0.0f;   // unit 0: none yet
 
     // A page's codes into a buffer, with its scales and the table's entry of
     // the place after it.  Pages that are not there are passed over.
@@ -145,8 +145,21 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) kv8_prompt_kernel(AttnA
       page = __builtin_amdgcn_readfirstlane(ahead.page);
       barrier();   // everyone's loads are in, and everyone is done with the other buffer
       ahead = fetch(page, i + 1, buf ^ 1);
-      const uint8_t* const kb = lds + buf * 2 * kBytes;
-      const uint8_t* const vb = kb + kBytes;
+      uint8_t* const kb = lds + buf * 2 * kBytes;
+      uint8_t* const vb = kb + kBytes;
+      // V's slots past the sequence's end may hold anything: they are cleared,
+      // so that no NaN of theirs meets the zero weight.
+      if (here && j0 + kPage > seq.length) {
+#pragma unroll
+        for (int n = 0; n < kLoads; ++n) {
+          const int slot = n * 256 + tid, d = slot / 4;
+          const int held = seq.length - j0 - 16 * v_slot(d, slot % 4);
+          uint4* const w = reinterpret_cast<uint4*>(vb + 16 * slot);
+          *w = make_uint4(w->x & held_mask(held, 0), w->y & held_mask(held, 4), w->z & held_mask(held, 8),
+                          w->w & held_mask(held, 12));
+        }
+        barrier();
+      }
       if (here && page_any(j0, wmin, wmax, a.window, a.sinks)) {
         // S^T of the half pages u: row 8 x + 4 h + y of the operand is token
         // 32 u + 16 h + 4 x + y.
@@ -179,16 +192,22 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) kv8_prompt_kernel(AttnA
 #pragma unroll
         for (int e = 0; e < 16; ++e) top = fmaxf(top, s[1][e]);
         top *= c;
-        const float ratio = unit > 0.0f ? vs / unit : 0.0f;
-        if (__any(top > m + 10.0f) || !(ratio >= 0.0625f && ratio <= 16.0f)) {
+        float ratio = vs * inv_unit;
+        const bool other_unit = !(ratio >= 0.0625f && ratio <= 16.0f);
+        if (__any(top > m + 10.0f) || other_unit) {
           // Both lanes of a row (halves of the tokens) move its reference alike.
           const float row_top = fmaxf(top, __shfl_xor(top, 32));
           const bool up = row_top > m + 10.0f;
           const float m_new = up ? row_top - 4.0f : m;
           const float alpha = m == -INFINITY ? 0.0f : exp2_hw(m - m_new);
-          const bool other_unit = !(ratio >= 0.0625f && ratio <= 16.0f);
-          const float fix = alpha * (other_unit && unit > 0.0f ? unit / vs : 1.0f);
-          if (other_unit) unit = vs;
+          float fix = alpha;
+          if (other_unit) {
+            const float inv = __builtin_amdgcn_rcpf(vs);
+            fix = alpha * (unit * inv);
+            unit = vs;
+            inv_unit = inv;
+            ratio = 1.0f;
+          }
           m = m_new;
           l *= alpha;
 #pragma unroll
@@ -196,7 +215,7 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) kv8_prompt_kernel(AttnA
         }
         // Weights with the v scale in them; their sum without it.
         const float base = m == -INFINITY ? 0.0f : m;
-        const float shift = __builtin_amdgcn_logf(vs / unit) - base;
+        const float shift = __builtin_amdgcn_logf(ratio) - base;
         float sum = 0.0f;
         half8 p[2][2];
 #pragma unroll
@@ -207,23 +226,13 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) kv8_prompt_kernel(AttnA
             sum += x;
             p[u][e / 8][e % 8] = (_Float16)x;
           }
-        l = fmaf(sum, unit / vs, l);
-        // Slots past the sequence's end may hold anything: no NaN of theirs may
-        // meet the zero weight.
-        const bool ends = j0 + kPage > seq.length;
+        l = fmaf(sum, __builtin_amdgcn_rcpf(ratio), l);
 #pragma unroll
         for (int t = 0; t < D / 32; ++t) {
           const int d = 32 * t + col;
 #pragma unroll
           for (int u = 0; u < 2; ++u) {
-            uint4 vc = *reinterpret_cast<const uint4*>(vb + d * kPage + 16 * v_slot(d, 2 * u + hh));
-            if (ends) {
-              const int held = seq.length - j0 - 32 * u - 16 * hh;
-              vc.x &= held_mask(held, 0);
-              vc.y &= held_mask(held, 4);
-              vc.z &= held_mask(held, 8);
-              vc.w &= held_mask(held, 12);
-            }
+            const uint4 vc = *reinterpret_cast<const uint4*>(vb + d * kPage + 16 * v_slot(d, 2 * u + hh));
             o[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(codes8(vc.x, vc.y), p[u][0], o[t], 0, 0, 0);
             o[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(codes8(vc.z, vc.w), p[u][1], o[t], 0, 0, 0);
           }
