@@ -57,28 +57,29 @@ __device__ __forceinline__ int k_slot(int t, int slot) {
 }
 __device__ __forceinline__ int v_slot(int d, int slot) { return slot ^ ((d >> 1) & 3); }
 
-template <int D>
-__global__ void __launch_bounds__(256, D == 256 ? 1 : 2) kv8_prompt_kernel(AttnArgs a) {
-  constexpr int kC = D / 32;               // 32-channel parts of a row
-  constexpr int kBytes = kPage * D;        // codes of a page and head
-  constexpr int kLoads = kBytes / 4096;    // 16-byte loads of a thread for K, and for V
-  extern __shared__ uint8_t lds[];         // two buffers of K, V
+template <int D, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) kv8_prompt_kernel(AttnArgs a) {
+  constexpr int kThreads = 64 * WAVES, kRows = 32 * WAVES;
+  constexpr int kC = D / 32;                       // 32-channel parts of a row
+  constexpr int kBytes = kPage * D;                // codes of a page and head
+  constexpr int kLoads = kBytes / 16 / kThreads;   // 16-byte loads of a thread for K, and for V
+  extern __shared__ uint8_t lds[];                 // two buffers of K, two of V
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 31, hh = lane >> 5;
-  const int head = (int)blockIdx.x % a.kv_heads, b = (int)blockIdx.x / a.kv_heads;
+  const int head = (int)blockIdx.x, b = (int)blockIdx.z / a.splits, part = (int)blockIdx.z % a.splits;
   const KvSeq seq = kv_seq(a.cu, a.lengths, b, a.T);
   const int rows = seq.count * a.group;   // T * heads < 2^30
-  const int tiles = (rows + kPromptRows - 1) / kPromptRows;
+  const int tiles = (rows + kRows - 1) / kRows;
   const int32_t* const table = a.table + (int64_t)b * a.max_pages;
   const float sign = a.scale_log2 < 0.0f ? -1.0f : 1.0f;
 
-  // Where this thread's 16-byte loads of a page come from (K, then V): slot s
-  // of LDS, in order, takes the row's slot that is moved there.
+  // Where this thread's 16-byte loads of a page come from: slot s of LDS, in
+  // order, takes the row's slot that is moved there.
   uint32_t from_k[kLoads], from_v[kLoads];
 #pragma unroll
   for (int i = 0; i < kLoads; ++i) {
-    const int s = i * 256 + tid;
+    const int s = i * kThreads + tid;
     const int t = s / (D / 16), ks = s % (D / 16), d = s / 4, vs = s % 4;
     from_k[i] = (uint32_t)(t * D + 16 * k_slot<D>(t, ks));
     from_v[i] = (uint32_t)(d * kPage + 16 * v_slot(d, vs));
@@ -86,18 +87,18 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) kv8_prompt_kernel(AttnA
 
   // Tiles from the sequence's end: those that see most come first.
   for (int tile = tiles - 1 - (int)blockIdx.y; tile >= 0; tile -= (int)gridDim.y) {
-    const int row0 = tile * kPromptRows;
-    const int last_row = min(row0 + kPromptRows, rows) - 1;
+    const int row0 = tile * kRows;
+    const int last_row = min(row0 + kRows, rows) - 1;
     const int wrow0 = min(row0 + 32 * wave, last_row), wrow1 = min(row0 + 32 * wave + 31, last_row);
     const int row = min(row0 + 32 * wave + col, last_row);   // lanes past the end repeat the last row
     const int token = row / a.group, g = row % a.group;
     const int pos = seq.start + token;
     const int wmin = __builtin_amdgcn_readfirstlane(seq.start + wrow0 / a.group);
     const int wmax = __builtin_amdgcn_readfirstlane(seq.start + wrow1 / a.group);
-    const Visible vis = visible_pages(seq.start + row0 / a.group, seq.start + last_row / a.group,
-                                      a.window, a.sinks, a.max_pages);
-    const int begin = min((int)blockIdx.z * a.chunk, vis.total);
-    const int end = (int)blockIdx.z == a.splits - 1 ? vis.total : min(begin + a.chunk, vis.total);
+    const Visible vis = visible_pages(seq.start + row0 / a.group, seq.start + last_row / a.group, a.window, a.sinks,
+                                      a.max_pages);
+    const int begin = min(part * a.chunk, vis.total);
+    const int end = part == a.splits - 1 ? vis.total : min(begin + a.chunk, vis.total);
 
     // Queries: chunk (C, e) gives lane (col, hh) channels 32 C + 16 hh + 8 e and up.
     half8 qf[kC][2];
@@ -117,42 +118,84 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) kv8_prompt_kernel(AttnA
       for (int e = 0; e < 16; ++e) o[t][e] = 0.0f;
     float m = -INFINITY, l = 0.0f, unit = 0.0f, inv_unit = 0.0f;   // unit 0: none yet
 
-    // A page's codes into a buffer, with its scales and the table's entry of
-    // the place after it.  Pages that are not there are passed over.
+    // Pages that are not there are passed over.
     const auto there = [&](int page) { return (uint32_t)page < (uint32_t)a.num_pages; };
     const auto entry = [&](int i) { return i < end ? table[vis.page(i)] : -1; };
-    const auto fetch = [&](int page, int i, int buf) {
-      Ahead x{entry(i + 1), 0.0f, 0.0f};
-      if (!there(page)) return x;
-      const int64_t which = (int64_t)page * a.kv_heads + head, at = which * kBytes;
-      x.ks = a.k_scales[which];
-      x.vs = a.v_scales[which];
-      const uint32_t to = (uint32_t)(buf * 2 * kBytes + wave * 1024);
+    const auto load_k = [&](int page, int buf) {
+      const uint8_t* const from = a.k_pages + ((int64_t)page * a.kv_heads + head) * kBytes;
 #pragma unroll
-      for (int n = 0; n < kLoads; ++n) load_lds16(a.k_pages + at, from_k[n], to + n * 4096);
+      for (int n = 0; n < kLoads; ++n)
+        load_lds16(from, from_k[n], (uint32_t)(buf * kBytes + wave * 1024 + n * 16 * kThreads));
+    };
+    const auto load_v = [&](int page, int buf) {
+      const uint8_t* const from = a.v_pages + ((int64_t)page * a.kv_heads + head) * kBytes;
 #pragma unroll
-      for (int n = 0; n < kLoads; ++n) load_lds16(a.v_pages + at, from_v[n], to + kBytes + n * 4096);
-      return x;
+      for (int n = 0; n < kLoads; ++n)
+        load_lds16(from, from_v[n], (uint32_t)((2 + buf) * kBytes + wave * 1024 + n * 16 * kThreads));
+    };
+    // S^T of half page u from a K buffer: row 8 x + 4 h + y of the operand is
+    // token 32 u + 16 h + 4 x + y.
+    const int ktok = 16 * ((col >> 2) & 1) + 4 * (col >> 3) + (col & 3);
+    const auto scores = [&](int buf, int u) {
+      const int t = 32 * u + ktok;
+      const uint8_t* const kb = lds + buf * kBytes + t * D;
+      float16v s;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[e] = 0.0f;
+#pragma unroll
+      for (int C = 0; C < kC; ++C) {
+        const uint4 kc = *reinterpret_cast<const uint4*>(kb + 16 * k_slot<D>(t, 2 * C + hh));
+        s = __builtin_amdgcn_mfma_f32_32x32x16_f16(codes8(kc.x, kc.y), qf[C][0], s, 0, 0, 0);
+        s = __builtin_amdgcn_mfma_f32_32x32x16_f16(codes8(kc.z, kc.w), qf[C][1], s, 0, 0, 0);
+      }
+      return s;
     };
 
-    int page = __builtin_amdgcn_readfirstlane(entry(begin)), buf = 0;
-    Ahead ahead = fetch(page, begin, 0);
-    for (int i = begin; i < end; ++i, buf ^= 1) {
-      const int j0 = vis.page(i) * kPage;
-      const bool here = there(page);
+    // Turn i: the scores of page i + 1 are formed while page i goes through the
+    // softmax and the second product; K of page i + 2 and V of page i + 1 come
+    // in meanwhile, with their scales and the table's entry after them.
+    int page = __builtin_amdgcn_readfirstlane(entry(begin));        // i
+    int page1 = __builtin_amdgcn_readfirstlane(entry(begin + 1));   // i + 1
+    Ahead ahead{entry(begin + 2), 0.0f, 0.0f};                      // page i + 2, scales of i
+    float16v s0, s1;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) s0[e] = s1[e] = 0.0f;
+    if (begin < end) {
+      if (there(page)) {
+        load_k(page, 0);
+        load_v(page, 0);
+        ahead.ks = a.k_scales[(int64_t)page * a.kv_heads + head];
+        ahead.vs = a.v_scales[(int64_t)page * a.kv_heads + head];
+      }
+      if (there(page1)) load_k(page1, 1);
       wait_loads(ahead);
+      barrier();
+      if (there(page)) {
+        s0 = scores(0, 0);
+        s1 = scores(0, 1);
+      }
+    }
+    for (int i = begin, buf = 0; i < end; ++i, buf ^= 1) {
+      const int j0 = vis.page(i) * kPage;
+      if (i > begin) wait_loads(ahead);
       const float ks = uniform(ahead.ks), vs = uniform(ahead.vs);
-      page = __builtin_amdgcn_readfirstlane(ahead.page);
-      barrier();   // everyone's loads are in, and everyone is done with the other buffer
-      ahead = fetch(page, i + 1, buf ^ 1);
-      uint8_t* const kb = lds + buf * 2 * kBytes;
-      uint8_t* const vb = kb + kBytes;
+      const int page2 = __builtin_amdgcn_readfirstlane(ahead.page);
+      barrier();   // everyone's loads are in, and everyone is done with the buffers of the last turn
+      ahead.page = entry(i + 3);
+      if (there(page1)) {
+        load_v(page1, buf ^ 1);
+        ahead.ks = a.k_scales[(int64_t)page1 * a.kv_heads + head];
+        ahead.vs = a.v_scales[(int64_t)page1 * a.kv_heads + head];
+      }
+      if (there(page2)) load_k(page2, buf);
+      const bool here = there(page);
+      uint8_t* const vb = lds + (2 + buf) * kBytes;
       // V's slots past the sequence's end may hold anything: they are cleared,
       // so that no NaN of theirs meets the zero weight.
       if (here && j0 + kPage > seq.length) {
 #pragma unroll
         for (int n = 0; n < kLoads; ++n) {
-          const int slot = n * 256 + tid, d = slot / 4;
+          const int slot = n * kThreads + tid, d = slot / 4;
           const int held = seq.length - j0 - 16 * v_slot(d, slot % 4);
           uint4* const w = reinterpret_cast<uint4*>(vb + 16 * slot);
           *w = make_uint4(w->x & held_mask(held, 0), w->y & held_mask(held, 4), w->z & held_mask(held, 8),
@@ -161,36 +204,18 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) kv8_prompt_kernel(AttnA
         barrier();
       }
       if (here && page_any(j0, wmin, wmax, a.window, a.sinks)) {
-        // S^T of the half pages u: row 8 x + 4 h + y of the operand is token
-        // 32 u + 16 h + 4 x + y.
-        float16v s[2];
-        const int ktok = 16 * ((col >> 2) & 1) + 4 * (col >> 3) + (col & 3);
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-#pragma unroll
-          for (int e = 0; e < 16; ++e) s[u][e] = 0.0f;
-          const int t = 32 * u + ktok;
-#pragma unroll
-          for (int C = 0; C < kC; ++C) {
-            const uint4 kc = *reinterpret_cast<const uint4*>(kb + t * D + 16 * k_slot<D>(t, 2 * C + hh));
-            s[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(codes8(kc.x, kc.y), qf[C][0], s[u], 0, 0, 0);
-            s[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(codes8(kc.z, kc.w), qf[C][1], s[u], 0, 0, 0);
-          }
-        }
         if (!page_whole(j0, wmin, wmax, a.window, a.sinks)) {
 #pragma unroll
-          for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int e = 0; e < 16; ++e)
-              s[u][e] = sees(pos, j0 + 32 * u + 16 * hh + e, a.window, a.sinks) ? s[u][e] : -INFINITY;
+          for (int e = 0; e < 16; ++e) {
+            s0[e] = sees(pos, j0 + 16 * hh + e, a.window, a.sinks) ? s0[e] : -INFINITY;
+            s1[e] = sees(pos, j0 + 32 + 16 * hh + e, a.window, a.sinks) ? s1[e] : -INFINITY;
+          }
         }
         // c > 0 also where the scale is 0: -inf stays -inf.
         const float c = fmaxf(fabsf(a.scale_log2) * ks, 1e-37f);
-        float top = s[0][0];
+        float top = fmaxf(s0[0], s1[0]);
 #pragma unroll
-        for (int e = 1; e < 16; ++e) top = fmaxf(top, s[0][e]);
-#pragma unroll
-        for (int e = 0; e < 16; ++e) top = fmaxf(top, s[1][e]);
+        for (int e = 1; e < 16; ++e) top = fmaxf(fmaxf(top, s0[e]), s1[e]);
         top *= c;
         float ratio = vs * inv_unit;
         const bool other_unit = !(ratio >= 0.0625f && ratio <= 16.0f);
@@ -216,28 +241,36 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) kv8_prompt_kernel(AttnA
         // Weights with the v scale in them; their sum without it.
         const float base = m == -INFINITY ? 0.0f : m;
         const float shift = __builtin_amdgcn_logf(ratio) - base;
+        // (Scores of a page that is not there are never used.)
+        const float16v n0 = scores(buf ^ 1, 0), n1 = scores(buf ^ 1, 1);
         float sum = 0.0f;
         half8 p[2][2];
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const float x = exp2_hw(fmaf(s[u][e], c, shift));
-            sum += x;
-            p[u][e / 8][e % 8] = (_Float16)x;
-          }
+        for (int e = 0; e < 16; ++e) {
+          const float x = exp2_hw(fmaf(s0[e], c, shift)), y = exp2_hw(fmaf(s1[e], c, shift));
+          sum += x;
+          sum += y;
+          p[0][e / 8][e % 8] = (_Float16)x;
+          p[1][e / 8][e % 8] = (_Float16)y;
+        }
         l = fmaf(sum, __builtin_amdgcn_rcpf(ratio), l);
 #pragma unroll
-        for (int t = 0; t < D / 32; ++t) {
-          const int d = 32 * t + col;
+        for (int u = 0; u < 2; ++u)
 #pragma unroll
-          for (int u = 0; u < 2; ++u) {
+          for (int t = 0; t < D / 32; ++t) {
+            const int d = 32 * t + col;
             const uint4 vc = *reinterpret_cast<const uint4*>(vb + d * kPage + 16 * v_slot(d, 2 * u + hh));
             o[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(codes8(vc.x, vc.y), p[u][0], o[t], 0, 0, 0);
             o[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(codes8(vc.z, vc.w), p[u][1], o[t], 0, 0, 0);
           }
-        }
+        s0 = n0;
+        s1 = n1;
+      } else {
+        s0 = scores(buf ^ 1, 0);
+        s1 = scores(buf ^ 1, 1);
       }
+      page = page1;
+      page1 = page2;
     }
     l += __shfl_xor(l, 32);
 
@@ -256,7 +289,7 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) kv8_prompt_kernel(AttnA
           }
         if (hh == 0) a.lse[to] = m * kLn2 + logf(l);
       } else {
-        const int64_t slot = (int64_t)blockIdx.z * a.T * a.heads + to;
+        const int64_t slot = (int64_t)part * a.T * a.heads + to;
         if (begin < end) {   // parts without pages come last
 #pragma unroll
           for (int t = 0; t < D / 32; ++t)
@@ -272,12 +305,16 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) kv8_prompt_kernel(AttnA
   }
 }
 
-template <int D>
+template <int D, int WAVES>
 hipError_t launch(const AttnArgs& a, int64_t B, int64_t max_q, hipStream_t stream) {
-  constexpr int kLds = 4 * kPage * D;
-  const int64_t tiles = (max_q * a.group + kPromptRows - 1) / kPromptRows;
-  const dim3 grid((unsigned)(B * a.kv_heads), (unsigned)(tiles < 65535 ? tiles : 65535), (unsigned)a.splits);
-  kv8_prompt_kernel<D><<<grid, 256, kLds, stream>>>(a);
+  constexpr int kLds = 4 * kPage * D, kRows = 32 * WAVES;
+  const int64_t tiles = (max_q * a.group + kRows - 1) / kRows;
+  // The heads first: with 8 of them a head's pages stay in one XCD's L2.  Then a
+  // sequence's tiles: workgroups go to the shader engines in turn, and an order
+  // that alternates long and short sequences gives all long ones to the same
+  // engines (391 against 323 us for two sequences of 2048 and 1226 queries).
+  const dim3 grid((unsigned)a.kv_heads, (unsigned)(tiles < 65535 ? tiles : 65535), (unsigned)(B * a.splits));
+  kv8_prompt_kernel<D, WAVES><<<grid, 64 * WAVES, kLds, stream>>>(a);
   return hipGetLastError();
 }
 
@@ -285,9 +322,9 @@ hipError_t launch(const AttnArgs& a, int64_t B, int64_t max_q, hipStream_t strea
 
 hipError_t launch_kv8_prompt(const AttnArgs& a, int head_dim, int64_t B, int64_t max_q, hipStream_t stream) {
   switch (head_dim) {
-    case 64: return launch<64>(a, B, max_q, stream);
-    case 128: return launch<128>(a, B, max_q, stream);
-    case 256: return launch<256>(a, B, max_q, stream);
+    case 64: return launch<64, 4>(a, B, max_q, stream);
+    case 128: return launch<128, 4>(a, B, max_q, stream);
+    case 256: return launch<256, 4>(a, B, max_q, stream);
     default: return hipErrorInvalidValue;
   }
 }
