@@ -47,15 +47,17 @@ __device__ __forceinline__ float uniform(float x) {
 // Waits for the wave's own LDS reads too: a buffer is refilled behind it.
 __device__ __forceinline__ void barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
-// The 16-byte slot of a row, moved so that eight lanes with consecutive rows of
-// an operand meet eight different banks.  K rows of token t: lanes hold tokens
-// 4 a + b and 16 + 4 a + b in turn.  V rows of channel d: 64 bytes, two to a
-// line of banks.
+// The 16-byte slot of a row, moved so that the 16 lanes of an operand that are
+// read together meet 16 different groups of four of the 64 banks.  K rows, token
+// t: those lanes hold tokens 4 x + 16 h + y, y < 4, with four different
+// (x & 1, h); 256 bytes of banks take 4, 2 or 1 rows.
 template <int D>
 __device__ __forceinline__ int k_slot(int t, int slot) {
-  return D == 64 ? slot ^ (((t >> 1) & 1) | ((t >> 3) & 2)) : slot ^ ((t & 3) | ((t >> 2) & 4));
+  const int xh = ((t >> 2) & 1) | ((t >> 3) & 2);
+  return slot ^ (D == 64 ? xh : D == 128 ? ((t >> 1) & 1) | xh << 1 : (t & 3) | xh << 2);
 }
-__device__ __forceinline__ int v_slot(int d, int slot) { return slot ^ ((d >> 1) & 3); }
+// V rows, channel d: 64 bytes, four to a line of banks.
+__device__ __forceinline__ int v_slot(int d, int slot) { return slot ^ ((d >> 2) & 3); }
 
 template <int D, int WAVES>
 __global__ void __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) kv8_prompt_kernel(AttnArgs a) {
@@ -312,7 +314,7 @@ hipError_t launch(const AttnArgs& a, int64_t B, int64_t max_q, hipStream_t strea
   // The heads first: with 8 of them a head's pages stay in one XCD's L2.  Then a
   // sequence's tiles: workgroups go to the shader engines in turn, and an order
   // that alternates long and short sequences gives all long ones to the same
-  // engines (391 against 323 us for two sequences of 2048 and 1226 queries).
+  // engines (391 against 356 us for two sequences of 2048 and 1226 queries).
   const dim3 grid((unsigned)a.kv_heads, (unsigned)(tiles < 65535 ? tiles : 65535), (unsigned)(B * a.splits));
   kv8_prompt_kernel<D, WAVES><<<grid, 64 * WAVES, kLds, stream>>>(a);
   return hipGetLastError();
