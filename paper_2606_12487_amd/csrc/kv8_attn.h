@@ -78,8 +78,8 @@ __device__ __forceinline__ bool sees(int pos, int j, int window, int sinks) {
   return j <= pos && (window == 0 || j > pos - window || j < sinks);
 }
 
-// Defined in kv8_prompt.hip.
-hipError_t launch_kv8_prompt(const AttnArgs& a, int head_dim, int64_t B, int64_t max_q, hipStream_t stream);
-constexpr int kPromptRows = 128;   // rows (query tokens x heads of a group) of a workgroup there
+// Defined in kv8_prompt.hip; rows (query tokens x heads of a group) of a workgroup: 128 or 64.
+hipError_t launch_kv8_prompt(const AttnArgs& a, int head_dim, int rows, int64_t B, int64_t max_q,
+                             hipStream_t stream);
 
 }  // namespace dptq

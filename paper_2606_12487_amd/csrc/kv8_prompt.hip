@@ -1,6 +1,6 @@
 // kv8_attention for many queries a sequence (the formulas: kv8_attention.hip).
 //
-// A workgroup of four waves takes 128 rows of one KV head of one sequence (row
+// A workgroup of four (or two) waves takes 128 (64) rows of one KV head of one sequence (row
 // r is query token r / group, head r % group: the heads that share a KV head
 // share its loads), 32 rows a wave, and walks the pages they see.  Pages come
 // into LDS by direct loads, one page ahead; each wave reads the codes from
@@ -322,11 +322,13 @@ hipError_t launch(const AttnArgs& a, int64_t B, int64_t max_q, hipStream_t strea
 
 }  // namespace
 
-hipError_t launch_kv8_prompt(const AttnArgs& a, int head_dim, int64_t B, int64_t max_q, hipStream_t stream) {
+hipError_t launch_kv8_prompt(const AttnArgs& a, int head_dim, int rows, int64_t B, int64_t max_q,
+                             hipStream_t stream) {
+  const bool four = rows == 128;
   switch (head_dim) {
-    case 64: return launch<64, 4>(a, B, max_q, stream);
-    case 128: return launch<128, 4>(a, B, max_q, stream);
-    case 256: return launch<256, 4>(a, B, max_q, stream);
+    case 64: return four ? launch<64, 4>(a, B, max_q, stream) : launch<64, 2>(a, B, max_q, stream);
+    case 128: return four ? launch<128, 4>(a, B, max_q, stream) : launch<128, 2>(a, B, max_q, stream);
+    case 256: return four ? launch<256, 4>(a, B, max_q, stream) : launch<256, 2>(a, B, max_q, stream);
     default: return hipErrorInvalidValue;
   }
 }
