@@ -17,6 +17,7 @@
 // cleared.  Bound by bytes: 2 read and 1 written per element.
 #include "internal.h"
 #include "kv8_device.h"
+#include "wave_device.h"
 
 namespace dptq {
 namespace {
@@ -52,7 +53,7 @@ __device__ __forceinline__ int scale_exp(float a) {
   return max(e, kKv8MinExp);
 }
 
-// Bytes of word w that lie in slots [lo, hi) of the eight from slot `first`.
+// Bytes of the dword of slots [first, first + 4) that lie in [lo, hi).
 __device__ __forceinline__ uint32_t slot_mask(int first, int lo, int hi) {
   uint32_t m = 0;
 #pragma unroll
@@ -63,16 +64,23 @@ __device__ __forceinline__ uint32_t slot_mask(int first, int lo, int hi) {
 
 template <int D>
 __global__ void __launch_bounds__(kThreads) kv8_append_kernel(AppendArgs a) {
-  constexpr int kUnits = kPage * D / 8;            // 8 codes each
-  constexpr int kPer = kUnits / kThreads;
+  constexpr int kOctets = D / 8;                       // of channels
+  constexpr int kPer = kPage * kOctets / kThreads;     // tokens x octets of a thread
+  constexpr int kRow = kPage + 4;                      // of the staged V codes, a channel a row
   __shared__ float part[kThreads / 64];
-  __shared__ uint8_t stage[D * (kPage + 8)];       // V codes, transposed
+  __shared__ __align__(8) uint8_t stage[D * kRow];
   const int b = blockIdx.z, head = blockIdx.y >> 1;
   const bool is_v = blockIdx.y & 1;
   const KvSeq q = kv_seq(a.cu, a.lengths, b, a.T);
   if (q.count == 0 || q.length == 0) return;
   const int begin = max(q.start, 0);
   const int last_block = min((q.length - 1) / kPage, a.max_pages - 1);
+  const int tid = threadIdx.x;
+  // A thread's tokens of one octet of channels: for K every (64 / kPer)th, so
+  // that a row's octets are stored by consecutive threads; for V consecutive
+  // ones, which make one LDS store of a channel.
+  const int octet = tid % kOctets, first_slot = tid / kOctets * (is_v ? kPer : 1);
+  const int slot_step = is_v ? 1 : kPage / kPer;
   for (int blk = begin / kPage + blockIdx.x; blk <= last_block; blk += gridDim.x) {
     const int page = a.table[(int64_t)b * a.max_pages + blk];
     if ((uint32_t)page >= (uint32_t)a.num_pages) continue;
@@ -81,20 +89,23 @@ __global__ void __launch_bounds__(kThreads) kv8_append_kernel(AppendArgs a) {
     const bool fresh = lo == 0;
     const int64_t at = (int64_t)page * a.heads + head;
     uint8_t* const codes = a.pages[is_v] + at * (kPage * D);
-    const __half* const rows = a.x[is_v] + (int64_t)head * D;
+    const __half* const rows = a.x[is_v] + (int64_t)head * D + 8 * octet;
+    const float had = fresh ? 0.0f : a.scales[is_v][at];
 
-    // The new tokens' values and their largest magnitude.  Unit u: slot
-    // u / (D / 8), channels 8 (u % (D / 8)) and up.
+    // The new tokens' values and their largest magnitude.
     uint4 v[kPer];
     float top = 0.0f;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-      const int u = (int)threadIdx.x + i * kThreads, slot = u / (D / 8);
+      const int slot = first_slot + i * slot_step;
       v[i] = make_uint4(0, 0, 0, 0);
       if (slot >= lo && slot < hi) {
         const int64_t t = (int64_t)q.first_row + ((int64_t)blk * kPage + slot - q.start);
-        v[i] = *reinterpret_cast<const uint4*>(rows + t * a.ld[is_v] + 8 * (u % (D / 8)));
+        v[i] = *reinterpret_cast<const uint4*>(rows + t * a.ld[is_v]);
       }
+    }
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
       const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -102,67 +113,75 @@ __global__ void __launch_bounds__(kThreads) kv8_append_kernel(AppendArgs a) {
         top = fmaxf(top, fmaxf(fabsf(__low2float(h)), fabsf(__high2float(h))));
       }
     }
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
-    if ((threadIdx.x & 63) == 0) part[threadIdx.x / 64] = top;
-    __syncthreads();
+    top = wave_max(top);
+    if ((tid & 63) == 0) part[tid / 64] = top;
+    __syncthreads();   // and everyone has read the scale
 #pragma unroll
     for (int i = 0; i < kThreads / 64; ++i) top = fmaxf(top, part[i]);
-    const int e = scale_exp(top);
-    const float need = __uint_as_float((uint32_t)(e + 127) << 23);
-    const float had = fresh ? 0.0f : a.scales[is_v][at];
+    const float need = __uint_as_float((uint32_t)(scale_exp(top) + 127) << 23);
     const float s = fmaxf(need, had);
     const bool grew = !fresh && s > had;
     const float ratio = had / s, inv = 1.0f / s;   // exact for powers of two
-    __syncthreads();                                // everyone has read the scale
-    if (threadIdx.x == 0) a.scales[is_v][at] = s;
+    if (tid == 0) a.scales[is_v][at] = s;
 
+    float f[kPer][8];
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-      const int u = (int)threadIdx.x + i * kThreads, slot = u / (D / 8), c = u % (D / 8);
       const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
-      float f[8];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const __half2 h = *reinterpret_cast<const __half2*>(&w[j]);
-        f[2 * j] = __low2float(h) * inv;
-        f[2 * j + 1] = __high2float(h) * inv;
+        f[i][2 * j] = __low2float(h) * inv;
+        f[i][2 * j + 1] = __high2float(h) * inv;
       }
-      const uint32_t c0 = to_e4m3<true>(f[2], f[3], to_e4m3<false>(f[0], f[1], 0));
-      const uint32_t c1 = to_e4m3<true>(f[6], f[7], to_e4m3<false>(f[4], f[5], 0));
-      if (!is_v) {
-        uint2* const dst = reinterpret_cast<uint2*>(codes + slot * D + 8 * c);
+    }
+    if (!is_v) {
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        const int slot = first_slot + i * slot_step;
+        uint2* const dst = reinterpret_cast<uint2*>(codes + slot * D + 8 * octet);
         if ((slot >= lo && slot < hi) || (fresh && slot >= hi)) {
-          *dst = make_uint2(c0, c1);
+          *dst = make_uint2(to_e4m3<true>(f[i][2], f[i][3], to_e4m3<false>(f[i][0], f[i][1], 0)),
+                            to_e4m3<true>(f[i][6], f[i][7], to_e4m3<false>(f[i][4], f[i][5], 0)));
         } else if (slot < lo && grew) {
           const uint2 o = *dst;
           *dst = make_uint2(rescale4(o.x, ratio), rescale4(o.y, ratio));
         }
-      } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-          stage[(8 * c + j) * (kPage + 8) + slot] = (uint8_t)((j < 4 ? c0 : c1) >> (8 * (j & 3)));
       }
-    }
-    if (is_v) {
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        uint8_t* const to = stage + (8 * octet + j) * kRow + first_slot;
+        if constexpr (kPer == 2) {
+          *reinterpret_cast<uint16_t*>(to) = (uint16_t)to_e4m3<false>(f[0][j], f[1][j], 0);
+        } else {
+#pragma unroll
+          for (int i = 0; i < kPer; i += 4)
+            *reinterpret_cast<uint32_t*>(to + i) =
+                to_e4m3<true>(f[i + 2][j], f[i + 3][j], to_e4m3<false>(f[i][j], f[i + 1][j], 0));
+        }
+      }
       __syncthreads();
       // Unit u: channel u / 8, slots 8 (u % 8) and up.
 #pragma unroll
       for (int i = 0; i < kPer; ++i) {
-        const int u = (int)threadIdx.x + i * kThreads, d = u / 8, first = 8 * (u % 8);
-        const uint2 n = *reinterpret_cast<const uint2*>(stage + d * (kPage + 8) + first);
-        uint2* const dst = reinterpret_cast<uint2*>(codes + d * kPage + first);
-        if (fresh) {
-          *dst = n;
-        } else if ((first + 8 > lo && first < hi) || (grew && first < lo)) {
-          uint2 o = *dst;
-          if (grew) {
-            const uint32_t m0 = slot_mask(first, 0, lo), m1 = slot_mask(first + 4, 0, lo);
-            o.x = (rescale4(o.x, ratio) & m0) | (o.x & ~m0);
-            o.y = (rescale4(o.y, ratio) & m1) | (o.y & ~m1);
-          }
-          const uint32_t m0 = slot_mask(first, lo, hi), m1 = slot_mask(first + 4, lo, hi);
-          *dst = make_uint2((n.x & m0) | (o.x & ~m0), (n.y & m1) | (o.y & ~m1));
+        const int u = tid + i * kThreads, d = u / 8, first = 8 * (u % 8);
+        const uint32_t* const from = reinterpret_cast<const uint32_t*>(stage + d * kRow + first);
+        uint8_t* const dst = codes + d * kPage + first;
+        const uint2 n = make_uint2(from[0], from[1]);
+        if (fresh || (first >= lo && first + 8 <= hi)) {
+          *reinterpret_cast<uint2*>(dst) = n;
+        } else if (grew && first < lo) {
+          const uint2 o = *reinterpret_cast<const uint2*>(dst);
+          const uint32_t old0 = slot_mask(first, 0, lo), old1 = slot_mask(first + 4, 0, lo);
+          const uint32_t new0 = slot_mask(first, lo, hi), new1 = slot_mask(first + 4, lo, hi);
+          *reinterpret_cast<uint2*>(dst) =
+              make_uint2((rescale4(o.x, ratio) & old0) | (n.x & new0) | (o.x & ~(old0 | new0)),
+                         (rescale4(o.y, ratio) & old1) | (n.y & new1) | (o.y & ~(old1 | new1)));
+        } else {
+          // Single slots, without reading the page.
+          for (int slot = max(lo, first); slot < min(hi, first + 8); ++slot)
+            dst[slot - first] = (uint8_t)((slot - first < 4 ? n.x : n.y) >> (8 * ((slot - first) & 3)));
         }
       }
     }

@@ -11,19 +11,23 @@
 // 0 and log probabilities -inf.
 //
 // One read of the logits.  A workgroup walks a part of a row in chunks of 8192
-// logits, 32 a thread in registers, from which it takes the sums and, against
-// the running list of the best `top`, the few logits that enter it.  Rows are
-// split over workgroups while there are too few of them; a second launch then
-// joins the parts.
+// logits in registers, from which it takes the sums and, against the running
+// list of the best `top`, the few logits that enter it.  Rows are split over
+// workgroups while there are too few of them; a second launch then joins the
+// parts.  Without alternatives 256 threads hold 32 logits each; with them 1024
+// hold 8: what a workgroup runs once per row is then short code, whose fetch
+// would otherwise take longer than the logits do.
 #include "internal.h"
+#include "wave_device.h"
 
 namespace dptq {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr int kThreads = 256;
-constexpr int kPer = 32;                        // logits of a thread in a chunk
-constexpr int kChunk = kThreads * kPer;
+constexpr int kChunk = 8192;
+constexpr int kTopThreads = 1024, kSumThreads = 256;
+constexpr int kTopPer = kChunk / kTopThreads;   // logits of a thread in a chunk
+constexpr int kGroups = 256;                    // whose maxima bound the list
 constexpr int kCap = 512;                       // candidates of a chunk that are ranked at once
 constexpr int kMaxTop = 64;
 
@@ -53,14 +57,15 @@ __device__ __forceinline__ Stats join(Stats a, Stats b) {
 }
 
 // The sums of a thread's values; -inf weighs nothing, NaN makes them NaN.
-__device__ __forceinline__ Stats stats_of(const float (&v)[kPer]) {
+template <int PER>
+__device__ __forceinline__ Stats stats_of(const float (&v)[PER]) {
   float m = v[0];
 #pragma unroll
-  for (int i = 1; i < kPer; ++i) m = fmaxf(m, v[i]);
+  for (int i = 1; i < PER; ++i) m = fmaxf(m, v[i]);
   const float base = m == -INFINITY ? 0.0f : m;
   float l[2] = {0.0f, 0.0f}, u[2] = {0.0f, 0.0f};
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) {
+  for (int i = 0; i < PER; ++i) {
     const float d = v[i] - base;
     const float e = __builtin_amdgcn_exp2f(d * kLog2e);
     l[i & 1] += e;
@@ -69,13 +74,19 @@ __device__ __forceinline__ Stats stats_of(const float (&v)[kPer]) {
   return Stats{m, l[0] + l[1], u[0] + u[1]};
 }
 
+// Over a workgroup of WAVES waves; every thread has the result.  The maximum
+// first, then the sums relative to it.
+template <int WAVES>
 __device__ __forceinline__ Stats block_join(Stats s, Stats* part) {
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1)
-    s = join(s, Stats{__shfl_xor(s.m, off), __shfl_xor(s.l, off), __shfl_xor(s.u, off)});
+  const auto wave_join = [](Stats s) {
+    s = join(s, Stats{wave_max(s.m), 0.0f, 0.0f});
+    return Stats{s.m, wave_sum(s.l), wave_sum(s.u)};
+  };
+  s = wave_join(s);
+  if (WAVES == 1) return s;
   if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = s;
   __syncthreads();
-  return join(join(part[0], part[1]), join(part[2], part[3]));
+  return wave_join((int)(threadIdx.x & 63) < WAVES ? part[threadIdx.x & 63] : Stats{-INFINITY, 0.0f, 0.0f});
 }
 
 // A logit and its index as one number: larger ones come first, equal logits by
@@ -97,8 +108,9 @@ struct TopScratch {
   Key best[kMaxTop];   // the list so far, in order, 0 where it has room
   Key next[kMaxTop];
   Key found[kCap + kMaxTop];
-  uint32_t group[kThreads];
-  Key wave_best[4];
+  uint32_t group[kGroups];
+  Key wave_best[kTopThreads / 64];
+  uint32_t bound;
   int count;
 };
 
@@ -109,66 +121,76 @@ __device__ __forceinline__ void clear_list(TopScratch& t, int top) {
 }
 
 // Merges a chunk into the list: index(k) is that of the thread's value v[k],
-// negative where it has none.  Indices of later chunks are larger, so a value
+// negative where it has none (whole: it has all); mine_top the largest of them,
+// of what has no index also.  Indices of later chunks are larger, so a value
 // enters only if it is larger than the list's last, or if the list has room.
 //
 // Where too many would (the first chunk of a row), the `top`-th largest of the
-// threads' maxima, to 16 bits, is a bound that at least `top` values reach, and
-// few more do in ordinary data.  Where that is too many as well (ties), the
-// entries are taken out one by one.
-// whole: the thread has all its values.
+// maxima of 256 groups of four threads, to 16 bits, is a bound that at least
+// `top` values reach, and few more do in ordinary data.  Where that is too many
+// as well (ties), the entries are taken out one by one.
 template <typename Index>
-__device__ __forceinline__ void merge_chunk(const float (&v)[kPer], const Index& index, bool whole, int top,
-                                            TopScratch& t) {
+__device__ __forceinline__ void merge_chunk(const float (&v)[kTopPer], float mine_top, const Index& index,
+                                            bool whole, int top, TopScratch& t) {
   const Key last = t.best[top - 1];
   const bool room = last == 0;
   // Larger than the last: at least the next float.
   const float least = room ? -INFINITY : unordered((uint32_t)(last >> 32) + 1);
   uint32_t mine = 0;
+  const auto choose = [&](float bound) {
+    mine = 0;
+    if (!__any(mine_top >= bound)) return;   // most waves, in most chunks
 #pragma unroll
-  for (int k = 0; k < kPer; ++k) mine |= v[k] >= least ? 1u << k : 0u;
-  if (!whole) {
-#pragma unroll
-    for (int k = 0; k < kPer; ++k)
-      if (index(k) < 0) mine &= ~(1u << k);
-  }
+    for (int k = 0; k < kTopPer; ++k) mine |= v[k] >= bound && (whole || index(k) >= 0) ? 1u << k : 0u;
+  };
   const auto gather = [&]() {
-    if (__any(mine != 0)) {
-      int at = mine ? atomicAdd(&t.count, __popc(mine)) : 0;
+    if (mine) {
+      int at = atomicAdd(&t.count, __popc(mine));
 #pragma unroll
-      for (int k = 0; k < kPer; ++k)
-        if (__any(mine >> k & 1))   // few are: a branch each
-          if (mine >> k & 1) {
-            if (at < kCap) t.found[at] = key_of(v[k], index(k));
-            ++at;
-          }
+      for (int k = 0; k < kTopPer; ++k)
+        if (mine >> k & 1) {
+          if (at < kCap) t.found[at] = key_of(v[k], index(k));
+          ++at;
+        }
     }
     __syncthreads();
     return t.count;
   };
   int n = 0;
-  if (!room) n = gather();
+  if (!room) {
+    choose(least);
+    n = gather();
+  }
   if (room || n > kCap) {   // the same for every thread
-    float top_of_mine = -INFINITY;
+    // In a chunk with places that have no index only the others count.
+    uint32_t high = 0;
+    if (whole) {
+      high = mine_top >= least ? ordered(mine_top) : 0;
+    } else {
 #pragma unroll
-    for (int k = 0; k < kPer; ++k)
-      if (mine >> k & 1) top_of_mine = fmaxf(top_of_mine, v[k]);
-    t.group[threadIdx.x] = mine ? ordered(top_of_mine) : 0;
-    __syncthreads();
-    if (threadIdx.x == 0) t.count = 0;
-    const uint4 g = *reinterpret_cast<const uint4*>(t.group + 4 * (threadIdx.x & 63));
-    uint32_t bound = 0;
-    for (int bit = 31; bit >= 16; --bit) {
-      const uint32_t b = bound | 1u << bit;
-      const int reach = __popcll(__ballot(g.x >= b)) + __popcll(__ballot(g.y >= b)) + __popcll(__ballot(g.z >= b)) +
-                        __popcll(__ballot(g.w >= b));
-      if (reach >= top) bound = b;
+      for (int k = 0; k < kTopPer; ++k)
+        if (v[k] >= least && index(k) >= 0) high = max(high, ordered(v[k]));
     }
-    const float x = unordered(bound > kOrderedLowest ? bound : kOrderedLowest);
-#pragma unroll
-    for (int k = 0; k < kPer; ++k)
-      if (!(v[k] >= x)) mine &= ~(1u << k);
+    high = max(high, (uint32_t)__shfl_xor((int)high, 1));
+    high = max(high, (uint32_t)__shfl_xor((int)high, 2));
+    if (threadIdx.x % 4 == 0) t.group[threadIdx.x / 4] = high;
     __syncthreads();
+    if (threadIdx.x < 64) {
+      const uint4 g = *reinterpret_cast<const uint4*>(t.group + 4 * threadIdx.x);
+      uint32_t bound = 0;
+      for (int bit = 31; bit >= 16; --bit) {
+        const uint32_t b = bound | 1u << bit;
+        const int reach = __popcll(__ballot(g.x >= b)) + __popcll(__ballot(g.y >= b)) +
+                          __popcll(__ballot(g.z >= b)) + __popcll(__ballot(g.w >= b));
+        if (reach >= top) bound = b;
+      }
+      if (threadIdx.x == 0) {
+        t.bound = bound > kOrderedLowest ? bound : kOrderedLowest;
+        t.count = 0;
+      }
+    }
+    __syncthreads();
+    choose(fmaxf(least, unordered(t.bound)));
     n = gather();
   }
   if (n == 0) {   // and so is count
@@ -176,19 +198,21 @@ __device__ __forceinline__ void merge_chunk(const float (&v)[kPer], const Index&
     return;
   }
   if (n <= kCap) {
-    // Ranks of the candidates and of the list's entries among all of them.
+    // Ranks of the candidates and of the list's entries among all of them: 16
+    // threads count for one.
     if ((int)threadIdx.x < top) {
       t.found[n + threadIdx.x] = t.best[threadIdx.x];
       t.next[threadIdx.x] = 0;
     }
     __syncthreads();
     const int all = n + top;
-    for (int c = threadIdx.x; c < all; c += kThreads) {
+    for (int c = threadIdx.x / 16; c < all; c += kTopThreads / 16) {
       const Key mine_key = t.found[c];
       int rank = 0;
-#pragma unroll 8
-      for (int o = 0; o < all; ++o) rank += t.found[o] > mine_key;
-      if (mine_key && rank < top) t.next[rank] = mine_key;
+      for (int o = threadIdx.x % 16; o < all; o += 16) rank += t.found[o] > mine_key;
+#pragma unroll
+      for (int off = 8; off > 0; off >>= 1) rank += __shfl_xor(rank, off);
+      if (threadIdx.x % 16 == 0 && mine_key && rank < top) t.next[rank] = mine_key;
     }
     __syncthreads();
   } else {
@@ -199,11 +223,9 @@ __device__ __forceinline__ void merge_chunk(const float (&v)[kPer], const Index&
     for (int out = 0; out < top; ++out) {
       Key best = 0;
 #pragma unroll
-      for (int k = 0; k < kPer; ++k)
+      for (int k = 0; k < kTopPer; ++k)
         if (mine >> k & 1) {
-          float x = v[k];
-          asm volatile("" : "+v"(x));   // the keys are formed again in each turn rather than held in registers
-          const Key c = key_of(x, index(k));
+          const Key c = key_of(v[k], index(k));
           if (c < taken && c > best) best = c;
         }
 #pragma unroll
@@ -213,7 +235,7 @@ __device__ __forceinline__ void merge_chunk(const float (&v)[kPer], const Index&
       }
       if ((threadIdx.x & 63) == 0) t.wave_best[threadIdx.x >> 6] = best;
       __syncthreads();
-      for (int w = 0; w < 4; ++w)
+      for (int w = 0; w < kTopThreads / 64; ++w)
         if (t.wave_best[w] > best) best = t.wave_best[w];
       const Key old = t.best[head];
       if (threadIdx.x == 0) t.next[out] = old > best ? old : best;
@@ -245,19 +267,28 @@ __device__ __forceinline__ void unpack(const uint4 r, const float*, float* v) {
   v[3] = __uint_as_float(r.w);
 }
 
-// The row's results from its sums and list (thread 0, and a thread an entry).
+// The row's token and its logit, for thread 0; fetched ahead of the row.
+struct Picked {
+  int64_t token;
+  float x;
+};
 template <typename T>
-__device__ __forceinline__ void finish(const LogprobArgs& a, int64_t row, Stats s, const Key* best) {
+__device__ __forceinline__ Picked pick(const LogprobArgs& a, int64_t row) {
+  Picked p{-1, 0.0f};
+  if (threadIdx.x == 0) {
+    p.token = a.tokens[row];
+    if (p.token >= 0 && p.token < a.V) p.x = value(static_cast<const T*>(a.x) + row * a.ld + p.token);
+  }
+  return p;
+}
+
+// The row's results from its sums and list (thread 0, and a thread an entry).
+__device__ __forceinline__ void finish(const LogprobArgs& a, int64_t row, Picked p, Stats s, const Key* best) {
   const float log_l = logf(s.l);
   if (threadIdx.x == 0) {
-    const int64_t t = a.tokens[row];
     float lp = 0.0f;
-    if (t >= a.V) {
-      lp = NAN;
-    } else if (t >= 0) {
-      const float v = value(static_cast<const T*>(a.x) + row * a.ld + t);
-      lp = v == -INFINITY ? v : (v - s.m) - log_l;
-    }
+    if (p.token >= a.V) lp = NAN;
+    else if (p.token >= 0) lp = p.x == -INFINITY ? p.x : (p.x - s.m) - log_l;
     a.logprobs[row] = lp;
     a.entropy[row] = s.l == 0.0f ? 0.0f : log_l - s.u / s.l;   // 0: all masked
   }
@@ -272,9 +303,10 @@ __device__ __forceinline__ void finish(const LogprobArgs& a, int64_t row, Stats 
 // before its first element: units that reach over an end are loaded element by
 // element.
 template <typename T, bool TOP>
-__global__ void __launch_bounds__(kThreads, 4) token_logprobs_kernel(LogprobArgs a) {
+__global__ void __launch_bounds__(TOP ? kTopThreads : kSumThreads, 8) token_logprobs_kernel(LogprobArgs a) {
+  constexpr int kThreads = TOP ? kTopThreads : kSumThreads, kPer = kChunk / kThreads;
   constexpr int E = 16 / sizeof(T), kUnits = kPer / E;
-  __shared__ Stats part[4];
+  __shared__ Stats part[kThreads / 64];
   __shared__ TopScratch scratch;
   for (int64_t row = blockIdx.y; row < a.M; row += gridDim.y) {
     const T* const x = static_cast<const T*>(a.x) + row * a.ld;
@@ -282,6 +314,7 @@ __global__ void __launch_bounds__(kThreads, 4) token_logprobs_kernel(LogprobArgs
     const int chunks = (int)(((int64_t)a.V + skew + kChunk - 1) / kChunk);
     const int begin = (int)((int64_t)chunks * blockIdx.x / a.splits);
     const int end = (int)((int64_t)chunks * (blockIdx.x + 1) / a.splits);
+    const Picked picked = a.splits == 1 ? pick<T>(a, row) : Picked{-1, 0.0f};
     Stats s{-INFINITY, 0.0f, 0.0f};
     if constexpr (TOP) clear_list(scratch, a.top);
     for (int c = begin; c < end; ++c) {
@@ -298,23 +331,23 @@ __global__ void __launch_bounds__(kThreads, 4) token_logprobs_kernel(LogprobArgs
           for (int j = 0; j < E; ++j) v[n * E + j] = i + j >= 0 && i + j < a.V ? value(x + i + j) : -INFINITY;
         }
       }
-      s = join(s, stats_of(v));
+      const Stats here = stats_of(v);
+      s = join(s, here);
       if constexpr (TOP) {
         const auto index = [&](int k) {
           const int i = mine + (k / E) * kThreads * E + k % E;
           return i < a.V ? i : -1;
         };
-        merge_chunk(v, index, first >= 0 && first + kChunk <= a.V, a.top, scratch);
+        merge_chunk(v, here.m, index, first >= 0 && first + kChunk <= a.V, a.top, scratch);
       }
     }
-    s = block_join(s, part);
+    s = block_join<kThreads / 64>(s, part);
     if (a.splits == 1) {
-      finish<T>(a, row, s, TOP ? scratch.best : nullptr);
+      finish(a, row, picked, s, TOP ? scratch.best : nullptr);
     } else {
       const int64_t at = row * a.splits + blockIdx.x;
       if (threadIdx.x == 0) a.part[at] = make_float4(s.m, s.l, s.u, 0.0f);
-      if (TOP && (int)threadIdx.x < a.top)
-        a.list[at * a.top + threadIdx.x] = scratch.best[threadIdx.x];
+      if (TOP && (int)threadIdx.x < a.top) a.list[at * a.top + threadIdx.x] = scratch.best[threadIdx.x];
     }
     __syncthreads();   // part and the list are free again
   }
@@ -322,53 +355,59 @@ __global__ void __launch_bounds__(kThreads, 4) token_logprobs_kernel(LogprobArgs
 
 // Joins a row's parts, which lie in the order of their indices.
 template <typename T, bool TOP>
-__global__ void __launch_bounds__(kThreads, 4) join_logprobs_kernel(LogprobArgs a) {
-  __shared__ Stats part[4];
+__global__ void __launch_bounds__(TOP ? kTopThreads : 64) join_logprobs_kernel(LogprobArgs a) {
+  constexpr int kThreads = TOP ? kTopThreads : 64;
+  __shared__ Stats part[kThreads / 64];
   __shared__ TopScratch scratch;
   for (int64_t row = blockIdx.x; row < a.M; row += gridDim.x) {
+    const Picked picked = pick<T>(a, row);
     Stats s{-INFINITY, 0.0f, 0.0f};
     for (int i = threadIdx.x; i < a.splits; i += kThreads) {
       const float4 p = a.part[row * a.splits + i];
       s = join(s, Stats{p.x, p.y, p.z});
     }
-    s = block_join(s, part);
+    s = block_join<kThreads / 64>(s, part);
     if constexpr (TOP) {
       clear_list(scratch, a.top);
       const int n = a.splits * a.top;
       const Key* const list = a.list + row * n;
       for (int c = 0; c < n; c += kChunk) {
-        float v[kPer];
-        int id[kPer];
+        float v[kTopPer];
+        int id[kTopPer];
 #pragma unroll
-        for (int k = 0; k < kPer; ++k) {
+        for (int k = 0; k < kTopPer; ++k) {
           const int i = c + k * kThreads + (int)threadIdx.x;
           const Key e = i < n ? list[i] : 0;
           id[k] = e ? key_index(e) : -1;
           v[k] = key_value(e);
         }
-        merge_chunk(v, [&](int k) { return id[k]; }, false, a.top, scratch);
+        float most = v[0];
+#pragma unroll
+        for (int k = 1; k < kTopPer; ++k) most = fmaxf(most, v[k]);
+        merge_chunk(v, most, [&](int k) { return id[k]; }, false, a.top, scratch);
       }
     }
-    finish<T>(a, row, s, TOP ? scratch.best : nullptr);
+    finish(a, row, picked, s, TOP ? scratch.best : nullptr);
     __syncthreads();
   }
 }
 
-// Parts of a row: enough workgroups for a few on each compute unit, of one
-// chunk or more.
+// Parts of a row: enough workgroups for 8 of 256 threads, or the two of 1024
+// that it holds, on each compute unit, of one chunk or more.
 int choose_splits(const TokenLogprobs& c) {
   const int64_t chunks = ((int64_t)c.V + kChunk - 1) / kChunk;
-  const int64_t want = (8 * (int64_t)device_cus() + c.M - 1) / c.M;
+  const int64_t want = ((c.top ? 2 : 8) * (int64_t)device_cus() + c.M - 1) / c.M;
   return (int)(want < chunks ? want : chunks);
 }
 
 template <typename T, bool TOP>
 hipError_t launch(const LogprobArgs& a, hipStream_t stream) {
   const unsigned rows = (unsigned)(a.M < 65535 ? a.M : 65535);
+  constexpr int kThreads = TOP ? kTopThreads : kSumThreads, kJoinThreads = TOP ? kTopThreads : 64;
   token_logprobs_kernel<T, TOP><<<dim3((unsigned)a.splits, rows), kThreads, 0, stream>>>(a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.splits == 1) return e;
-  join_logprobs_kernel<T, TOP><<<rows, kThreads, 0, stream>>>(a);
+  join_logprobs_kernel<T, TOP><<<rows, kJoinThreads, 0, stream>>>(a);
   return hipGetLastError();
 }
 

@@ -13,6 +13,7 @@
 // codes: x, the residual and the weight are read once, h and the codes written
 // once.
 #include "internal.h"
+#include "wave_device.h"
 
 namespace dptq {
 namespace {
@@ -78,11 +79,8 @@ rms_norm_quant_kernel(const uint4* x, const uint4* residual, const uint4* __rest
       }
     }
   }
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) {
-    sq += __shfl_xor(sq, off);
-    top = fmaxf(top, __shfl_xor(top, off));
-  }
+  sq = wave_sum(sq);
+  top = wave_max(top);
   if ((threadIdx.x & 63) == 0) part[threadIdx.x / 64] = make_float2(sq, top);
   __syncthreads();
   sq = 0.0f;
