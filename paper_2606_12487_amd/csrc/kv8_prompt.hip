@@ -1,10 +1,12 @@
 // kv8_attention for many queries a sequence (the formulas: kv8_attention.hip).
 //
-// A workgroup of four (or two) waves takes 128 (64) rows of one KV head of one sequence (row
+// A workgroup of four waves takes 128 rows of one KV head of one sequence (row
 // r is query token r / group, head r % group: the heads that share a KV head
 // share its loads), 32 rows a wave, and walks the pages they see.  Pages come
 // into LDS by direct loads, one page ahead; each wave reads the codes from
-// there and converts them as it feeds the matrix cores.
+// there and converts them as it feeds the matrix cores.  Where that makes too
+// few workgroups, one takes 64 rows, two waves on every other page each, and
+// joins the two halves at the end (KEYS = 2).
 //
 // The products are those of the decode kernel on 32 x 32 tiles: S^T = K Q^T
 // with the K operand's rows in an order that leaves a lane with 16 consecutive
@@ -59,15 +61,18 @@ __device__ __forceinline__ int k_slot(int t, int slot) {
 // V rows, channel d: 64 bytes, four to a line of banks.
 __device__ __forceinline__ int v_slot(int d, int slot) { return slot ^ ((d >> 2) & 3); }
 
-template <int D, int WAVES>
-__global__ void __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) kv8_prompt_kernel(AttnArgs a) {
-  constexpr int kThreads = 64 * WAVES, kRows = 32 * WAVES;
+template <int D, int KEYS>
+__global__ void __launch_bounds__(256, D == 256 ? 1 : 2) kv8_prompt_kernel(AttnArgs a) {
+  constexpr int kThreads = 256 / KEYS, kRows = 128 / KEYS;   // of the waves that share pages
   constexpr int kC = D / 32;                       // 32-channel parts of a row
   constexpr int kBytes = kPage * D;                // codes of a page and head
   constexpr int kLoads = kBytes / 16 / kThreads;   // 16-byte loads of a thread for K, and for V
-  extern __shared__ uint8_t lds[];                 // two buffers of K, two of V
-  const int tid = threadIdx.x, lane = tid & 63;
+  extern __shared__ uint8_t all_lds[];
+  const int keys = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kThreads);   // which of the pages
+  const int tid = threadIdx.x % kThreads, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const uint32_t lds_at = (uint32_t)keys * 4 * kBytes;
+  uint8_t* const lds = all_lds + lds_at;           // two buffers of K, two of V
   const int col = lane & 31, hh = lane >> 5;
   const int head = (int)blockIdx.x, b = (int)blockIdx.z / a.splits, part = (int)blockIdx.z % a.splits;
   const KvSeq seq = kv_seq(a.cu, a.lengths, b, a.T);
@@ -127,13 +132,13 @@ __global__ void __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) kv8_prompt_kerne
       const uint8_t* const from = a.k_pages + ((int64_t)page * a.kv_heads + head) * kBytes;
 #pragma unroll
       for (int n = 0; n < kLoads; ++n)
-        load_lds16(from, from_k[n], (uint32_t)(buf * kBytes + wave * 1024 + n * 16 * kThreads));
+        load_lds16(from, from_k[n], lds_at + (uint32_t)(buf * kBytes + wave * 1024 + n * 16 * kThreads));
     };
     const auto load_v = [&](int page, int buf) {
       const uint8_t* const from = a.v_pages + ((int64_t)page * a.kv_heads + head) * kBytes;
 #pragma unroll
       for (int n = 0; n < kLoads; ++n)
-        load_lds16(from, from_v[n], (uint32_t)((2 + buf) * kBytes + wave * 1024 + n * 16 * kThreads));
+        load_lds16(from, from_v[n], lds_at + (uint32_t)((2 + buf) * kBytes + wave * 1024 + n * 16 * kThreads));
     };
     // S^T of half page u from a K buffer: row 8 x + 4 h + y of the operand is
     // token 32 u + 16 h + 4 x + y.
@@ -153,12 +158,13 @@ __global__ void __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) kv8_prompt_kerne
       return s;
     };
 
-    // Turn i: the scores of page i + 1 are formed while page i goes through the
-    // softmax and the second product; K of page i + 2 and V of page i + 1 come
+    // The scores of the next page are formed while a page goes through the
+    // softmax and the second product; K of the one after and V of the next come
     // in meanwhile, with their scales and the table's entry after them.
-    int page = __builtin_amdgcn_readfirstlane(entry(begin));        // i
-    int page1 = __builtin_amdgcn_readfirstlane(entry(begin + 1));   // i + 1
-    Ahead ahead{entry(begin + 2), 0.0f, 0.0f};                      // page i + 2, scales of i
+    const int first = begin + keys;
+    int page = __builtin_amdgcn_readfirstlane(entry(first));           // of place i
+    int page1 = __builtin_amdgcn_readfirstlane(entry(first + KEYS));   // the next
+    Ahead ahead{entry(first + 2 * KEYS), 0.0f, 0.0f};                  // the one after; scales of place i
     float16v s0, s1;
 #pragma unroll
     for (int e = 0; e < 16; ++e) s0[e] = s1[e] = 0.0f;
@@ -177,13 +183,13 @@ __global__ void __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) kv8_prompt_kerne
         s1 = scores(0, 1);
       }
     }
-    for (int i = begin, buf = 0; i < end; ++i, buf ^= 1) {
-      const int j0 = vis.page(i) * kPage;
-      if (i > begin) wait_loads(ahead);
+    for (int turn = begin, buf = 0; turn < end; turn += KEYS, buf ^= 1) {
+      const int i = turn + keys, j0 = vis.page(i) * kPage;   // past the end: no page
+      if (turn > begin) wait_loads(ahead);
       const float ks = uniform(ahead.ks), vs = uniform(ahead.vs);
       const int page2 = __builtin_amdgcn_readfirstlane(ahead.page);
       barrier();   // everyone's loads are in, and everyone is done with the buffers of the last turn
-      ahead.page = entry(i + 3);
+      ahead.page = entry(i + 3 * KEYS);
       if (there(page1)) {
         load_v(page1, buf ^ 1);
         ahead.ks = a.k_scales[(int64_t)page1 * a.kv_heads + head];
@@ -194,7 +200,7 @@ __global__ void __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) kv8_prompt_kerne
       uint8_t* const vb = lds + (2 + buf) * kBytes;
       // V's slots past the sequence's end may hold anything: they are cleared,
       // so that no NaN of theirs meets the zero weight.
-      if (here && j0 + kPage > seq.length) {
+      if (vis.page(min(turn + KEYS, end) - 1) * kPage + kPage > seq.length) {   // the same for every wave
 #pragma unroll
         for (int n = 0; n < kLoads; ++n) {
           const int slot = n * kThreads + tid, d = slot / 4;
@@ -276,7 +282,35 @@ __global__ void __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) kv8_prompt_kerne
     }
     l += __shfl_xor(l, 32);
 
-    if (row0 + 32 * wave + col < rows) {
+    if constexpr (KEYS == 2) {
+      // The two halves' sums, relative to the larger reference, in units of 1.
+      float* const o_of = reinterpret_cast<float*>(all_lds);
+      float* const ml_of = o_of + 16 * (D / 32) * kThreads;
+      barrier();   // the pages are done with
+      if (keys == 1) {
+#pragma unroll
+        for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) o_of[(16 * t + e) * kThreads + tid] = o[t][e] * unit;
+        ml_of[tid] = m;
+        ml_of[kThreads + tid] = l;
+      }
+      barrier();
+      if (keys == 0) {
+        const float m1 = ml_of[tid], both = fmaxf(m, m1), ref = both == -INFINITY ? 0.0f : both;
+        const float f0 = exp2_hw(m - ref), f1 = exp2_hw(m1 - ref);
+#pragma unroll
+        for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            o[t][e] = o[t][e] * (f0 * unit) + f1 * o_of[(16 * t + e) * kThreads + tid];
+        l = f0 * l + f1 * ml_of[kThreads + tid];
+        m = both;
+        unit = 1.0f;
+      }
+    }
+
+    if (keys == 0 && row0 + 32 * wave + col < rows) {
       const int64_t to = ((int64_t)seq.first_row + token) * a.heads + head * a.group + g;
       if (a.splits == 1) {
         const float f = l > 0.0f ? unit / l : l;   // 0: nothing seen; NaN stays
@@ -307,16 +341,22 @@ __global__ void __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) kv8_prompt_kerne
   }
 }
 
-template <int D, int WAVES>
+template <int D, int KEYS>
 hipError_t launch(const AttnArgs& a, int64_t B, int64_t max_q, hipStream_t stream) {
-  constexpr int kLds = 4 * kPage * D, kRows = 32 * WAVES;
+  constexpr int kPages = KEYS * 4 * kPage * D, kJoin = (16 * (D / 32) + 2) * 4 * (256 / KEYS);
+  constexpr int kLds = KEYS == 2 && kJoin > kPages ? kJoin : kPages, kRows = 128 / KEYS;
   const int64_t tiles = (max_q * a.group + kRows - 1) / kRows;
   // The heads first: with 8 of them a head's pages stay in one XCD's L2.  Then a
   // sequence's tiles: workgroups go to the shader engines in turn, and an order
   // that alternates long and short sequences gives all long ones to the same
   // engines (391 against 356 us for two sequences of 2048 and 1226 queries).
   const dim3 grid((unsigned)a.kv_heads, (unsigned)(tiles < 65535 ? tiles : 65535), (unsigned)(B * a.splits));
-  kv8_prompt_kernel<D, WAVES><<<grid, 64 * WAVES, kLds, stream>>>(a);
+  if constexpr (kLds > 65536) {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kv8_prompt_kernel<D, KEYS>),
+                                             hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
+    if (e != hipSuccess) return e;
+  }
+  kv8_prompt_kernel<D, KEYS><<<grid, 256, kLds, stream>>>(a);
   return hipGetLastError();
 }
 
@@ -324,11 +364,10 @@ hipError_t launch(const AttnArgs& a, int64_t B, int64_t max_q, hipStream_t strea
 
 hipError_t launch_kv8_prompt(const AttnArgs& a, int head_dim, int rows, int64_t B, int64_t max_q,
                              hipStream_t stream) {
-  const bool four = rows == 128;
   switch (head_dim) {
-    case 64: return four ? launch<64, 4>(a, B, max_q, stream) : launch<64, 2>(a, B, max_q, stream);
-    case 128: return four ? launch<128, 4>(a, B, max_q, stream) : launch<128, 2>(a, B, max_q, stream);
-    case 256: return four ? launch<256, 4>(a, B, max_q, stream) : launch<256, 2>(a, B, max_q, stream);
+    case 64: return rows == 128 ? launch<64, 1>(a, B, max_q, stream) : launch<64, 2>(a, B, max_q, stream);
+    case 128: return rows == 128 ? launch<128, 1>(a, B, max_q, stream) : launch<128, 2>(a, B, max_q, stream);
+    case 256: return rows == 128 ? launch<256, 1>(a, B, max_q, stream) : launch<256, 2>(a, B, max_q, stream);
     default: return hipErrorInvalidValue;
   }
 }
