@@ -210,8 +210,9 @@ hipError_t launch_kv8_append(const Kv8Cache& c, const void* k, int64_t ld_k, con
   a.num_pages = (int)c.num_pages;
   a.heads = c.kv_heads;
   // Pages that max_new tokens can touch; a sequence with more loops.
-  const int64_t blocks = (max_new + kPage - 2) / kPage + 1;
-  const dim3 grid((unsigned)(blocks < c.max_pages ? blocks : c.max_pages), (unsigned)(2 * c.kv_heads), (unsigned)c.B);
+  int64_t blocks = (max_new + kPage - 2) / kPage + 1;
+  blocks = blocks < c.max_pages ? blocks : c.max_pages;
+  const dim3 grid((unsigned)(blocks < 65535 ? blocks : 65535), (unsigned)(2 * c.kv_heads), (unsigned)c.B);
   switch (c.head_dim) {
     case 64: kv8_append_kernel<64><<<grid, kThreads, 0, stream>>>(a); break;
     case 128: kv8_append_kernel<128><<<grid, kThreads, 0, stream>>>(a); break;

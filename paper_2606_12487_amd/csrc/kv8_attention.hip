@@ -55,7 +55,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 4 : D == 128 ? 2 : 1) kv8_decod
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int col = lane & 15, quad = lane >> 4;
-  const int head = (int)blockIdx.x % a.kv_heads, b = (int)blockIdx.x / a.kv_heads;
+  const int head = (int)blockIdx.x, b = (int)blockIdx.z / a.splits, part = (int)blockIdx.z % a.splits;
   const KvSeq seq = kv_seq(a.cu, a.lengths, b, a.T);
   const int rows = seq.count * a.group;   // T * heads < 2^30
   const int32_t* const table = a.table + (int64_t)b * a.max_pages;
@@ -68,8 +68,8 @@ __global__ void __launch_bounds__(256, D == 64 ? 4 : D == 128 ? 2 : 1) kv8_decod
     const int pmin = seq.start + row0 / a.group;
     const int pmax = seq.start + min(row0 + 15, rows - 1) / a.group;
     const Visible vis = visible_pages(pmin, pmax, a.window, a.sinks, a.max_pages);
-    const int begin = min((int)blockIdx.z * a.chunk, vis.total);
-    const int end = (int)blockIdx.z == a.splits - 1 ? vis.total : min(begin + a.chunk, vis.total);
+    const int begin = min(part * a.chunk, vis.total);
+    const int end = part == a.splits - 1 ? vis.total : min(begin + a.chunk, vis.total);
 
     // Queries: chunk (C, e) of 32 channels gives lane (col, quad) the channels
     // 64 C + 16 quad + 8 e and up, as K's 16-byte loads hold them.
@@ -234,7 +234,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 4 : D == 128 ? 2 : 1) kv8_decod
         a.out[to * D + d] = __float2half_rn(ml.y > 0.0f ? sum_o[e] / ml.y : ml.y);
         if (d == 0) a.lse[to] = ml.x * kLn2 + logf(ml.y);
       } else {
-        const int64_t at = (int64_t)blockIdx.z * a.T * a.heads + to;
+        const int64_t at = (int64_t)part * a.T * a.heads + to;
         if (begin < end) a.part_o[at * D + d] = sum_o[e];   // parts without pages come last
         if (d == 0) a.part_ml[at] = ml;
       }
@@ -346,9 +346,12 @@ struct Layout {
 Layout choose_layout(const Kv8Attention& c) {
   const int64_t group = c.heads / c.cache.kv_heads, heads = c.cache.B * c.cache.kv_heads, cus = device_cus();
   const auto tiles = [&](int64_t rows) { return (c.max_q * group + rows - 1) / rows * heads; };
-  // Up to 32 rows of a sequence go to tiles of 16.  More go to tiles of 128, or
-  // of 64 while those are fewer than two on a compute unit.
-  const int rows = c.max_q * group <= 32 ? 16 : tiles(128) >= 2 * cus ? 128 : 64;
+  // The rows of a sequence that fit one tile of 16 go there (32 rows in two of
+  // them take 42 us against 33 in one of 64: 16 sequences of 4096 tokens, 4
+  // queries, 64 / 8 heads).  More go to tiles of 128, or of 64 while those are
+  // fewer than two on a compute unit (256 tiles of 128 behind a window of 1024:
+  // 29 us against 25 in 512 of 64).
+  const int rows = c.max_q * group <= 16 ? 16 : tiles(128) >= 2 * cus ? 128 : 64;
   // What a tile sees: behind a window, that of its tokens, the sinks, and parts of pages at three ends.
   const int64_t seen = c.window > 0 ? c.window + (int64_t)c.sinks + rows / group + 1 + 3 * kPage : c.max_len;
   const int64_t pages = ((seen < c.max_len ? seen : c.max_len) + kPage - 1) / kPage;
@@ -372,8 +375,9 @@ hipError_t launch(const AttnArgs& a, const Kv8Attention& c, int rows, hipStream_
     e = launch_kv8_prompt(a, D, rows, c.cache.B, c.max_q, stream);
   } else {
     const int64_t tiles = (c.max_q * a.group + 15) / 16;
-    const dim3 grid((unsigned)(c.cache.B * a.kv_heads), (unsigned)(tiles < 65535 ? tiles : 65535),
-                    (unsigned)a.splits);
+    // (There is more than one part only where there are few sequences: z fits.)
+    const dim3 grid((unsigned)a.kv_heads, (unsigned)(tiles < 65535 ? tiles : 65535),
+                    (unsigned)(c.cache.B * a.splits));
     kv8_decode_kernel<D><<<grid, 256, 0, stream>>>(a);
     e = hipGetLastError();
   }

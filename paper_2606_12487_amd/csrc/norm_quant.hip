@@ -48,71 +48,74 @@ __device__ __forceinline__ uint32_t code8(float t, float s, float rc) {
 
 template <int THREADS, int VPT>
 __global__ void __launch_bounds__(THREADS)
-rms_norm_quant_kernel(const uint4* x, const uint4* residual, const uint4* __restrict__ weight, int n8,
-                      float inv_k, float eps, uint4* sum, uint2* __restrict__ codes,
+rms_norm_quant_kernel(const uint4* x, const uint4* residual, const uint4* __restrict__ weight, int64_t M,
+                      int n8, float inv_k, float eps, uint4* sum, uint2* __restrict__ codes,
                       float* __restrict__ scales) {
   __shared__ float2 part[THREADS / 64];
-  const int64_t row = blockIdx.x;
-  const int64_t base = row * n8;
-  Row8 h[VPT];
-  float sq = 0.0f, top = 0.0f;
+  for (int64_t row = blockIdx.x; row < M; row += gridDim.x) {
+    const int64_t base = row * n8;
+    Row8 h[VPT];
+    float sq = 0.0f, top = 0.0f;
 #pragma unroll
-  for (int v = 0; v < VPT; ++v) {
-    const int c = (int)threadIdx.x + v * THREADS;
-    h[v] = Row8{{0, 0, 0, 0}};
-    if (c < n8) {
-      h[v] = load8(x + base + c);
-      if (residual) {
-        const Row8 r = load8(residual + base + c);
+    for (int v = 0; v < VPT; ++v) {
+      const int c = (int)threadIdx.x + v * THREADS;
+      h[v] = Row8{{0, 0, 0, 0}};
+      if (c < n8) {
+        h[v] = load8(x + base + c);
+        if (residual) {
+          const Row8 r = load8(residual + base + c);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          h[v].w[i] = pack_halves(lo_half(h[v].w[i]) + lo_half(r.w[i]), hi_half(h[v].w[i]) + hi_half(r.w[i]));
-        sum[base + c] = make_uint4(h[v].w[0], h[v].w[1], h[v].w[2], h[v].w[3]);
-      }
-      const Row8 w = load8(weight + c);
+          for (int i = 0; i < 4; ++i)
+            h[v].w[i] = pack_halves(lo_half(h[v].w[i]) + lo_half(r.w[i]), hi_half(h[v].w[i]) + hi_half(r.w[i]));
+          sum[base + c] = make_uint4(h[v].w[0], h[v].w[1], h[v].w[2], h[v].w[3]);
+        }
+        const Row8 w = load8(weight + c);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float a = lo_half(h[v].w[i]), b = hi_half(h[v].w[i]);
-        sq = fmaf(a, a, sq);
-        sq = fmaf(b, b, sq);
-        top = fmaxf(top, fmaxf(fabsf(a * lo_half(w.w[i])), fabsf(b * hi_half(w.w[i]))));
+        for (int i = 0; i < 4; ++i) {
+          const float a = lo_half(h[v].w[i]), b = hi_half(h[v].w[i]);
+          sq = fmaf(a, a, sq);
+          sq = fmaf(b, b, sq);
+          top = fmaxf(top, fmaxf(fabsf(a * lo_half(w.w[i])), fabsf(b * hi_half(w.w[i]))));
+        }
       }
     }
-  }
-  sq = wave_sum(sq);
-  top = wave_max(top);
-  if ((threadIdx.x & 63) == 0) part[threadIdx.x / 64] = make_float2(sq, top);
-  __syncthreads();
-  sq = 0.0f;
+    sq = wave_sum(sq);
+    top = wave_max(top);
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x / 64] = make_float2(sq, top);
+    __syncthreads();
+    sq = 0.0f;
 #pragma unroll
-  for (int i = 0; i < THREADS / 64; ++i) {
-    sq += part[i].x;
-    top = fmaxf(top, part[i].y);
-  }
-  const float s = top / 127.0f;
-  const float rc = s > 0.0f ? 1.0f / s : 0.0f;   // a row of zeros: codes 0
-#pragma unroll
-  for (int v = 0; v < VPT; ++v) {
-    const int c = (int)threadIdx.x + v * THREADS;
-    if (c < n8) {
-      const Row8 w = load8(weight + c);
-      uint32_t out[2] = {0, 0};
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        out[i / 2] |= code8(lo_half(h[v].w[i]) * lo_half(w.w[i]), s, rc) << (16 * (i & 1));
-        out[i / 2] |= code8(hi_half(h[v].w[i]) * hi_half(w.w[i]), s, rc) << (16 * (i & 1) + 8);
-      }
-      codes[base + c] = make_uint2(out[0], out[1]);
+    for (int i = 0; i < THREADS / 64; ++i) {
+      sq += part[i].x;
+      top = fmaxf(top, part[i].y);
     }
+    const float s = top / 127.0f;
+    const float rc = s > 0.0f ? 1.0f / s : 0.0f;   // a row of zeros: codes 0
+#pragma unroll
+    for (int v = 0; v < VPT; ++v) {
+      const int c = (int)threadIdx.x + v * THREADS;
+      if (c < n8) {
+        const Row8 w = load8(weight + c);
+        uint32_t out[2] = {0, 0};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          out[i / 2] |= code8(lo_half(h[v].w[i]) * lo_half(w.w[i]), s, rc) << (16 * (i & 1));
+          out[i / 2] |= code8(hi_half(h[v].w[i]) * hi_half(w.w[i]), s, rc) << (16 * (i & 1) + 8);
+        }
+        codes[base + c] = make_uint2(out[0], out[1]);
+      }
+    }
+    if (threadIdx.x == 0) scales[row] = s > 0.0f ? s * (1.0f / sqrtf(sq * inv_k + eps)) : 0.0f;
+    __syncthreads();   // part is free again
   }
-  if (threadIdx.x == 0) scales[row] = s > 0.0f ? s * (1.0f / sqrtf(sq * inv_k + eps)) : 0.0f;
 }
 
 template <int THREADS, int VPT>
 hipError_t launch(const void* x, const void* residual, const void* weight, int64_t M, int K, float eps,
                   void* sum, int8_t* codes, float* scales, hipStream_t stream) {
-  rms_norm_quant_kernel<THREADS, VPT><<<(unsigned)M, THREADS, 0, stream>>>(
-      static_cast<const uint4*>(x), static_cast<const uint4*>(residual), static_cast<const uint4*>(weight),
+  const unsigned grid = (unsigned)(M < 1 << 20 ? M : 1 << 20);
+  rms_norm_quant_kernel<THREADS, VPT><<<grid, THREADS, 0, stream>>>(
+      static_cast<const uint4*>(x), static_cast<const uint4*>(residual), static_cast<const uint4*>(weight), M,
       K / 8, 1.0f / (float)K, eps, static_cast<uint4*>(sum), reinterpret_cast<uint2*>(codes), scales);
   return hipGetLastError();
 }

@@ -40,7 +40,8 @@ def _check(x, tokens, top, xd=None):
 
 
 CASES = [(1, 1, 0), (1, 1, 1), (3, 2, 2), (5, 7, 7), (1, 63, 5), (2, 64, 64), (4, 1000, 20), (1, 32768, 20),
-         (9, 50001, 1), (2, 131072, 64), (300, 257, 3), (17, 4097, 0), (3, 8191, 33), (1, 300007, 20)]
+         (9, 50001, 1), (2, 131072, 64), (300, 257, 3), (17, 4097, 0), (3, 8191, 33), (1, 300007, 20),
+         (65537, 5, 2), (70001, 3, 0), (1, 1200000, 64), (3000, 9000, 0)]
 
 
 @pytest.mark.parametrize("M,V,top", CASES)

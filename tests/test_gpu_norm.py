@@ -29,7 +29,8 @@ def _check(x, w, eps, res):
 
 
 @pytest.mark.parametrize("M,K", [(1, 8), (3, 16), (1, 4096), (5, 2048), (2, 2056), (7, 5120), (33, 8192), (2, 8200),
-                                 (3, 32768), (2, 32776), (2, 65536), (513, 1032), (1030, 4096)])
+                                 (3, 32768), (2, 32776), (2, 65536), (513, 1032), (1030, 4096),
+                                 (2 ** 20 + 3, 8)])
 @pytest.mark.parametrize("add", [True, False])
 def test_norm_matches_oracle(M, K, add):
     rng = np.random.default_rng(M * 31 + K)
