@@ -14,7 +14,10 @@
 // factor of two of a floating-point format's range, which e4m3 does not feel.
 //
 // A page that is new (its first slot is written now) has its other slots
-// cleared.  Bound by bytes: 2 read and 1 written per element.
+// cleared.  2 bytes read and 1 written per element; bound by the chain of loads
+// (offsets, table, rows) and the reduction between them: a token for each of 64
+// sequences (8 heads of 128) takes 7.4 us, 4500 tokens of three prompts 10.1 us
+// (2.6 TB/s).
 #include "internal.h"
 #include "kv8_device.h"
 #include "wave_device.h"

@@ -15,8 +15,10 @@
 // list of the best `top`, the few logits that enter it.  Rows are split over
 // workgroups while there are too few of them; a second launch then joins the
 // parts.  Without alternatives 256 threads hold 32 logits each; with them 1024
-// hold 8: what a workgroup runs once per row is then short code, whose fetch
-// would otherwise take longer than the logits do.
+// hold 8, in which the work that a row needs once (bound, ranks, join) is
+// spread wider (27.6 us against 28.9 for 64 x 131072 fp16 with 20 alternatives:
+// latency of those chains).  2047 x 100003 fp32 without alternatives: 143 us,
+// 5.7 TB/s, bound by bytes.
 #include "internal.h"
 #include "wave_device.h"
 

@@ -11,7 +11,8 @@
 //
 // One workgroup a row, the row held in registers between the reduction and the
 // codes: x, the residual and the weight are read once, h and the codes written
-// once.
+// once.  Bound by those 7 bytes an element: 4001 rows of 8192 take 44.6 us, 5.15
+// TB/s, as a large copy does; one row of 4096 takes 3 us, a launch.
 #include "internal.h"
 #include "wave_device.h"
 
