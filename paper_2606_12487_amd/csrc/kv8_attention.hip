@@ -54,7 +54,8 @@ template <int D>
 __global__ void __launch_bounds__(256, D == 64 ? 4 : D == 128 ? 2 : 1) kv8_decode_kernel(AttnArgs a) {
   constexpr int kC = D / 64;     // 64-channel parts of a row
   constexpr int kT = D / 16;     // 16-channel tiles of the output
-  __shared__ float sum_o[16 * D];
+  constexpr int kSlots = D == 256 ? 2 : 4;   // waves whose outputs stand in LDS at once
+  __shared__ float sum_o[kSlots][16 * D];
   __shared__ float2 wave_ml[4][16];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -216,12 +217,13 @@ __global__ void __launch_bounds__(256, D == 64 ? 4 : D == 128 ? 2 : 1) kv8_decod
 #pragma unroll
     for (int w = 0; w < 4; ++w) L += wave_ml[w][col].y * exp2_hw(wave_ml[w][col].x - ref);
     const float mine = exp2_hw(m - ref) * unit;
-    for (int w = 0; w < 4; ++w) {
-      if (w == wave) {
+#pragma unroll
+    for (int first = 0; first < 4; first += kSlots) {
+      if (wave >= first && wave < first + kSlots) {
 #pragma unroll
         for (int t = 0; t < kT; ++t) {
-          float4v* const dst = reinterpret_cast<float4v*>(sum_o + col * D + 16 * t + 4 * quad);
-          *dst = w == 0 ? o[t] * mine : *dst + o[t] * mine;
+          float4v* const dst = reinterpret_cast<float4v*>(sum_o[wave % kSlots] + col * D + 16 * t + 4 * quad);
+          *dst = first == 0 ? o[t] * mine : *dst + o[t] * mine;
         }
       }
       __syncthreads();
@@ -233,13 +235,16 @@ __global__ void __launch_bounds__(256, D == 64 ? 4 : D == 128 ? 2 : 1) kv8_decod
       if (r >= rows) break;
       const int d = e % D;
       const float2 ml = wave_ml[0][e / D];
+      float x = 0.0f;
+#pragma unroll
+      for (int w = 0; w < kSlots; ++w) x += sum_o[w][e];
       const int64_t to = ((int64_t)seq.first_row + r / a.group) * a.heads + head * a.group + r % a.group;
       if (a.splits == 1) {
-        a.out[to * D + d] = __float2half_rn(ml.y > 0.0f ? sum_o[e] / ml.y : ml.y);
+        a.out[to * D + d] = __float2half_rn(ml.y > 0.0f ? x / ml.y : ml.y);
         if (d == 0) a.lse[to] = ml.x * kLn2 + logf(ml.y);
       } else {
         const int64_t at = (int64_t)part * a.T * a.heads + to;
-        if (begin < end) a.part_o[at * D + d] = sum_o[e];   // parts without pages come last
+        if (begin < end) a.part_o[at * D + d] = x;   // parts without pages come last
         if (d == 0) a.part_ml[at] = ml;
       }
     }

@@ -14,11 +14,11 @@
 // logits in registers, from which it takes the sums and, against the running
 // list of the best `top`, the few logits that enter it.  Rows are split over
 // workgroups while there are too few of them; a second launch then joins the
-// parts.  Without alternatives 256 threads hold 32 logits each; with them 1024
-// hold 8, in which the work that a row needs once (bound, ranks, join) is
-// spread wider (27.6 us against 28.9 for 64 x 131072 fp16 with 20 alternatives:
-// latency of those chains).  2047 x 100003 fp32 without alternatives: 143 us,
-// 5.7 TB/s, bound by bytes.
+// parts.  Without alternatives 256 threads hold 32 logits each: 2047 x 100003
+// fp32 take 143 us, 5.7 TB/s, bound by bytes.  With them 512 hold 16, so that
+// the work that a row needs once (bound, ranks, join) is spread wider: 64 x
+// 131072 fp16 with 20 alternatives take 22.3 us, bound by the latency of those
+// chains in two launches (27 us with 256 threads, 27.6 with 1024).
 #include "internal.h"
 #include "wave_device.h"
 
@@ -27,7 +27,7 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kChunk = 8192;
-constexpr int kTopThreads = 1024, kSumThreads = 256;
+constexpr int kTopThreads = 512, kSumThreads = 256;
 constexpr int kTopPer = kChunk / kTopThreads;   // logits of a thread in a chunk
 constexpr int kGroups = 256;                    // whose maxima bound the list
 constexpr int kCap = 512;                       // candidates of a chunk that are ranked at once
@@ -128,7 +128,7 @@ __device__ __forceinline__ void clear_list(TopScratch& t, int top) {
 // enters only if it is larger than the list's last, or if the list has room.
 //
 // Where too many would (the first chunk of a row), the `top`-th largest of the
-// maxima of 256 groups of four threads, to 16 bits, is a bound that at least
+// maxima of 256 groups of threads, to 16 bits, is a bound that at least
 // `top` values reach, and few more do in ordinary data.  Where that is too many
 // as well (ties), the entries are taken out one by one.
 template <typename Index>
@@ -173,9 +173,10 @@ __device__ __forceinline__ void merge_chunk(const float (&v)[kTopPer], float min
       for (int k = 0; k < kTopPer; ++k)
         if (v[k] >= least && index(k) >= 0) high = max(high, ordered(v[k]));
     }
-    high = max(high, (uint32_t)__shfl_xor((int)high, 1));
-    high = max(high, (uint32_t)__shfl_xor((int)high, 2));
-    if (threadIdx.x % 4 == 0) t.group[threadIdx.x / 4] = high;
+    constexpr int kMates = kTopThreads / kGroups;
+#pragma unroll
+    for (int off = 1; off < kMates; off *= 2) high = max(high, (uint32_t)__shfl_xor((int)high, off));
+    if (threadIdx.x % kMates == 0) t.group[threadIdx.x / kMates] = high;
     __syncthreads();
     if (threadIdx.x < 64) {
       const uint4 g = *reinterpret_cast<const uint4*>(t.group + 4 * threadIdx.x);
@@ -305,7 +306,7 @@ __device__ __forceinline__ void finish(const LogprobArgs& a, int64_t row, Picked
 // before its first element: units that reach over an end are loaded element by
 // element.
 template <typename T, bool TOP>
-__global__ void __launch_bounds__(TOP ? kTopThreads : kSumThreads, 8) token_logprobs_kernel(LogprobArgs a) {
+__global__ void __launch_bounds__(TOP ? kTopThreads : kSumThreads, TOP ? kTopThreads / 128 : 8) token_logprobs_kernel(LogprobArgs a) {
   constexpr int kThreads = TOP ? kTopThreads : kSumThreads, kPer = kChunk / kThreads;
   constexpr int E = 16 / sizeof(T), kUnits = kPer / E;
   __shared__ Stats part[kThreads / 64];
