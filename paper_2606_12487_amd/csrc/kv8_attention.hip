@@ -364,13 +364,14 @@ Layout choose_layout(const Kv8Attention& c) {
   // What a tile sees: behind a window, that of its tokens, the sinks, and parts of pages at three ends.
   const int64_t seen = c.window > 0 ? c.window + (int64_t)c.sinks + rows / group + 1 + 3 * kPage : c.max_len;
   const int64_t pages = ((seen < c.max_len ? seen : c.max_len) + kPage - 1) / kPage;
-  // Parts: for decode enough workgroups for the two that a compute unit holds
-  // (3, 4 and 8 took 1 to 15 % longer on the large batches), of four pages (one
-  // a wave) or more, and none of what has up to eight pages (the second launch
+  // Parts: for decode one round of the workgroups that a compute unit holds, 4,
+  // 2 or 1 by the head size (at 128 two: 3, 4 and 8 took 1 to 15 % longer on the
+  // large batches; at 256 one: 34 us against 42 for 65536 tokens), of four pages
+  // (one a wave) or more, and none of what has up to eight pages (the second launch
   // costs more: 500 tokens 9.1 us against 10.7, while 777 take 11.4 against
   // 10.6); for prompts, whose partial outputs are large, only while there are
   // fewer tiles than compute units.
-  const int64_t fill = rows == 16 ? 2 * cus : cus;
+  const int64_t fill = rows == 16 ? 256 / c.cache.head_dim * cus : cus;
   int64_t chunk = (tiles(rows) * pages + fill - 1) / fill;
   chunk = (chunk + 3) / 4 * 4;
   const int64_t least = pages <= 8 ? 8 : 4;
