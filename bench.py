@@ -45,10 +45,10 @@ HEADLINE = "llama2_70b_layer"
 TRAFFIC_FILE = os.path.join(ROOT, "profiles", "traffic_qgemm_fp6_llama2_70b_stack.txt")
 # The sources of the kernels that a summary describes, and of the rule that picks them.
 _CSRC = os.path.join(ROOT, "paper_2606_12487_amd", "csrc")
-TRAFFIC_SOURCE = tuple(os.path.join(_CSRC, f) for f in ("qgemm_fp6.hip", "fp6_device.h"))
+TRAFFIC_SOURCE = tuple(os.path.join(_CSRC, f) for f in ("qgemm_fp6.hip", "fp6_device.h", "lds_load.h"))
 DECODE_TRAFFIC_FILE = os.path.join(ROOT, "profiles", "traffic_qgemm_decode_llama2_70b_M8.txt")
 DECODE_TRAFFIC_SOURCE = tuple(os.path.join(_CSRC, f) for f in (
-    "qgemm_ksplit.hip", "qgemm_decode.hip", "qgemm_device.h", "gemm_rules.h"))
+    "qgemm_ksplit.hip", "qgemm_decode.hip", "qgemm_device.h", "lds_load.h", "gemm_rules.h"))
 
 
 def parse():

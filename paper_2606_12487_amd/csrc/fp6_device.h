@@ -1,10 +1,12 @@
 // Device helpers shared by the FP6 GEMM kernels (the layout is described in
-// qgemm_fp6.hip): direct loads, the MFMA step and the dequantization epilogue.
+// qgemm_fp6.hip): the MFMA step and the dequantization epilogue.
 #pragma once
 
 #include <hip/hip_runtime.h>
 #include <hip/hip_fp16.h>
 #include <stdint.h>
+
+#include "lds_load.h"
 
 namespace dptq {
 namespace f6 {
@@ -15,14 +17,6 @@ typedef __attribute__((address_space(3))) uint8_t* lds_ptr_t;
 
 constexpr int kF6Block = 3072;   // bytes of one 32-row x 128-k block
 
-// Wavefront-wide direct load of 1 KiB (16 bytes per lane) from sbase + voff
-// into LDS at lds_off + 16 * lane.
-__device__ __forceinline__ void f6_dma16(const void* sbase, uint32_t voff, uint32_t lds_off) {
-  asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1"
-               :
-               : "v"(voff), "s"(sbase), "s"(lds_off)
-               : "memory", "m0");
-}
 __device__ __forceinline__ int f6_xcd_remap(int bid, int total) {
   const int per = total >> 3, rem = total & 7;
   const int x = bid & 7, idx = bid >> 3;

@@ -26,19 +26,10 @@
 // 128) take 333 to 349 us, 0.88 to 0.92 PFLOP/s; 1000 queries behind a window of 1024
 // (32 heads on 8, head size 64) 25 us.
 #include "kv8_attn.h"
+#include "lds_load.h"
 
 namespace dptq {
 namespace {
-
-// 16 bytes per lane from base + voff straight to LDS, at byte lds_off + 16 *
-// lane.  As asm, so that the compiler does not wait for them before each LDS
-// read; wait_loads() and the barrier order them.
-__device__ __forceinline__ void load_lds16(const void* base, uint32_t voff, uint32_t lds_off) {
-  asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1"
-               :
-               : "v"(voff), "s"(base), "s"(lds_off)
-               : "memory", "m0");
-}
 
 // What is fetched ahead for a page beside its codes.
 struct Ahead {

@@ -22,6 +22,7 @@
 
 #include "dptq.h"
 #include "internal.h"
+#include "lds_load.h"
 #include "qgemm_device.h"
 
 namespace dptq {
@@ -45,37 +46,6 @@ constexpr int kBK = 256;
 
 typedef __attribute__((address_space(3))) uint8_t* lds_ptr;
 typedef int v16i __attribute__((ext_vector_type(16)));
-
-// One wavefront-wide 16-byte-per-lane direct load from global memory into LDS
-// at byte offset lds_off (+ 16 * lane).  Issued as asm so that the compiler's
-// conservative wait (it cannot tell the ring buffers apart) does not drain
-// the loads before every LDS read; completion is tracked with wait_vmcnt.
-// Address = wavefront-uniform base + 32-bit per-lane offset.
-__device__ __forceinline__ void dma16(const void* sbase, uint32_t voff, uint32_t lds_off) {
-  asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1"
-               :
-               : "v"(voff), "s"(sbase), "s"(lds_off)
-               : "memory", "m0");
-}
-
-// The same with the LDS destination given as a wavefront-uniform base plus a
-// compile-time offset, formed in M0 by one scalar add (the global address is
-// sbase + voff, the per-lane offset carrying the row).
-template <uint32_t OFF>
-__device__ __forceinline__ void dma16_at(const void* sbase, uint32_t voff, uint32_t lds_base) {
-  asm volatile("s_add_u32 m0, %2, %3\n\tglobal_load_lds_dwordx4 %0, %1"
-               :
-               : "v"(voff), "s"(sbase), "s"(lds_base), "i"(OFF)
-               : "memory", "m0", "scc");
-}
-
-// The same with 4 bytes per lane (LDS byte offset lds_off + 4 * lane).
-__device__ __forceinline__ void dma4(const void* sbase, uint32_t voff, uint32_t lds_off) {
-  asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dword %0, %1"
-               :
-               : "v"(voff), "s"(sbase), "s"(lds_off)
-               : "memory", "m0");
-}
 
 // Workgroup barrier without the release/acquire fences of __syncthreads(): the
 // fences would drain every outstanding direct-to-LDS load.  Callers wait for
@@ -205,7 +175,7 @@ qgemm_prefill(const uint8_t* __restrict__ a_codes, const float* __restrict__ a_s
     if (w_full && !tail) {
 #pragma unroll
       for (int i = 0; i < C::kWLoads; ++i)
-        dma16(wt + (size_t)((i * kWaves + wave_u) * 8) * wrow, wlane[i & 1], base + i * kWaves * 1024);
+        load_lds16(wt + (size_t)((i * kWaves + wave_u) * 8) * wrow, wlane[i & 1], base + i * kWaves * 1024);
     } else {
 #pragma unroll
       for (int i = 0; i < C::kWLoads; ++i) {
@@ -213,7 +183,7 @@ qgemm_prefill(const uint8_t* __restrict__ a_codes, const float* __restrict__ a_s
         int c = (lane & 7) ^ swz8(r);
         if (tail) c &= 3;
         const int rc = min(r, N - 1 - n0);
-        dma16(wt, (uint32_t)(rc * wrow + c * 16), base + i * kWaves * 1024);
+        load_lds16(wt, (uint32_t)(rc * wrow + c * 16), base + i * kWaves * 1024);
       }
     }
   };
@@ -224,7 +194,7 @@ qgemm_prefill(const uint8_t* __restrict__ a_codes, const float* __restrict__ a_s
     if (a_full && !tail) {
 #pragma unroll
       for (int i = 0; i < C::kALoads; ++i)
-        dma16(at + (size_t)((i * kWaves + wave_u) * kARows) * arow, alane[i & 1],
+        load_lds16(at + (size_t)((i * kWaves + wave_u) * kARows) * arow, alane[i & 1],
               base + C::kW + i * kWaves * 1024);
     } else {
 #pragma unroll
@@ -240,7 +210,7 @@ qgemm_prefill(const uint8_t* __restrict__ a_codes, const float* __restrict__ a_s
           if (tail) c &= 7;
         }
         const int rc = min(r, M - 1 - m0);
-        dma16(at, (uint32_t)(rc * arow + c * 16), base + C::kW + i * kWaves * 1024);
+        load_lds16(at, (uint32_t)(rc * arow + c * 16), base + C::kW + i * kWaves * 1024);
       }
     }
   };
@@ -585,10 +555,10 @@ qgemm_prefill_wide(const uint8_t* __restrict__ a_codes, const float* __restrict_
     const uint8_t* wt = wtile + (size_t)st * C::kWRow;
     const uint8_t* at = atile + (size_t)st * C::kARow;
     [&]<int... I>(std::integer_sequence<int, I...>) {
-      (dma16_at<(uint32_t)(I * 4096)>(wt, wofs[I], base), ...);
+      (load_lds16_at<(uint32_t)(I * 4096)>(wt, wofs[I], base), ...);
     }(std::make_integer_sequence<int, C::kWLoads>{});
     [&]<int... I>(std::integer_sequence<int, I...>) {
-      (dma16_at<(uint32_t)(C::kW + I * 4096)>(at, aofs[I], base), ...);
+      (load_lds16_at<(uint32_t)(C::kW + I * 4096)>(at, aofs[I], base), ...);
     }(std::make_integer_sequence<int, C::kALoads>{});
   };
   // Loads [I0, I1) of one stage (weights first, then activations), so that a
@@ -605,9 +575,9 @@ qgemm_prefill_wide(const uint8_t* __restrict__ a_codes, const float* __restrict_
           [&] {
             if constexpr (I >= I0 && I < I1) {
               if constexpr (I < C::kWLoads)
-                dma16_at<(uint32_t)(I * 4096)>(wt, wofs[I], base);
+                load_lds16_at<(uint32_t)(I * 4096)>(wt, wofs[I], base);
               else
-                dma16_at<(uint32_t)(C::kW + (I - C::kWLoads) * 4096)>(at, aofs[I - C::kWLoads], base);
+                load_lds16_at<(uint32_t)(C::kW + (I - C::kWLoads) * 4096)>(at, aofs[I - C::kWLoads], base);
             }
           }(),
           ...);
@@ -625,11 +595,11 @@ qgemm_prefill_wide(const uint8_t* __restrict__ a_codes, const float* __restrict_
       const uint32_t base = smem_base + C::kRing + q * C::kScaleSlot;
       if (wave == 0) {
 #pragma unroll
-        for (int i = 0; i < C::kBM / 64; ++i) dma4(a_scales + m0 + 64 * i, (uint32_t)lane * 4, base + 256 * i);
+        for (int i = 0; i < C::kBM / 64; ++i) load_lds4(a_scales + m0 + 64 * i, (uint32_t)lane * 4, base + 256 * i);
       } else if (wave == 1) {
 #pragma unroll
         for (int i = 0; i < C::kBN / 64; ++i)
-          dma4(w_scales + n0 + 64 * i, (uint32_t)lane * 4, base + 1024 + 256 * i);
+          load_lds4(w_scales + n0 + 64 * i, (uint32_t)lane * 4, base + 1024 + 256 * i);
       }
     }
   };

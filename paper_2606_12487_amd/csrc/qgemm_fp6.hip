@@ -120,22 +120,6 @@ struct F6 {
   static constexpr int nl(int w) { return w < 2 ? 11 : 10; }
 };
 
-// The same with the LDS destination a wavefront-uniform base plus a
-// compile-time offset, formed in M0 by one scalar add; the global address is
-// sbase + voff.
-template <uint32_t OFF>
-__device__ __forceinline__ void f6_dma16_at(const void* sbase, uint32_t voff, uint32_t lds_base) {
-  asm volatile("s_add_u32 m0, %2, %3\n\tglobal_load_lds_dwordx4 %0, %1"
-               :
-               : "v"(voff), "s"(sbase), "s"(lds_base), "i"(OFF)
-               : "memory", "m0", "scc");
-}
-__device__ __forceinline__ void f6_dma4(const void* sbase, uint32_t voff, uint32_t lds_off) {
-  asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dword %0, %1"
-               :
-               : "v"(voff), "s"(sbase), "s"(lds_off)
-               : "memory", "m0");
-}
 __device__ __forceinline__ void f6_barrier() { asm volatile("s_barrier" ::: "memory"); }
 
 template <int N>
@@ -246,7 +230,7 @@ __device__ __forceinline__ void qgemm_fp6_body(const uint8_t* __restrict__ a6,
         // The block offset travels in the per-lane offset (one vector
         // instruction) and the LDS offset in M0's add, so a load costs one
         // scalar instruction beside it.
-        f6_dma16_at<(uint32_t)(q * 1024)>(q < C::kWLoads ? wst : ast, lane16 + (uint32_t)(rel * 1024), base);
+        load_lds16_at<(uint32_t)(q * 1024)>(q < C::kWLoads ? wst : ast, lane16 + (uint32_t)(rel * 1024), base);
       };
       [&]<int... I>(std::integer_sequence<int, I...>) __attribute__((always_inline)) {
         (one(std::integral_constant<int, Q0 + P0 + I>{}), ...);
@@ -261,7 +245,7 @@ __device__ __forceinline__ void qgemm_fp6_body(const uint8_t* __restrict__ a6,
         const int rb = isa ? min(rba + b, mblk - 1) : min(rbw + b, nblk - 1);
         const uint8_t* src = (isa ? a6 + (size_t)kb * astride : w6 + (size_t)kb * wstride) +
                              (size_t)rb * kF6Block + (qq - 3 * b) * 1024;
-        f6_dma16(src, lane16, base + q * 1024);
+        load_lds16(src, lane16, base + q * 1024);
       }
     }
   };
@@ -281,13 +265,13 @@ __device__ __forceinline__ void qgemm_fp6_body(const uint8_t* __restrict__ a6,
 #pragma unroll
         for (int i = 0; i < C::kBM / 64; ++i) {
           const int m = min(m0 + 64 * i + lane, M - 1);
-          f6_dma4(a_scales, (uint32_t)m * 4, base + 256 * i);
+          load_lds4(a_scales, (uint32_t)m * 4, base + 256 * i);
         }
       } else {
 #pragma unroll
         for (int i = 0; i < C::kBN / 64; ++i) {
           const int n = min(n0 + 64 * i + lane, N - 1);
-          f6_dma4(w_scales, (uint32_t)n * 4, base + 1024 + 256 * i);
+          load_lds4(w_scales, (uint32_t)n * 4, base + 1024 + 256 * i);
         }
       }
     }

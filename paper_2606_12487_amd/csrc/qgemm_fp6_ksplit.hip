@@ -83,11 +83,11 @@ qgemm_fp6_ksplit(const uint8_t* __restrict__ a6, const float* __restrict__ a_sca
 #pragma unroll
     for (int i = 0; i < TI; ++i)
 #pragma unroll
-      for (int c = 0; c < 3; ++c) f6_dma16(wk, wofs[i] + c * 1024, b + (3 * i + c) * 1024);
+      for (int c = 0; c < 3; ++c) load_lds16(wk, wofs[i] + c * 1024, b + (3 * i + c) * 1024);
 #pragma unroll
     for (int j = 0; j < TJ; ++j)
 #pragma unroll
-      for (int c = 0; c < 3; ++c) f6_dma16(ak, aofs[j] + c * 1024, b + (3 * (TI + j) + c) * 1024);
+      for (int c = 0; c < 3; ++c) load_lds16(ak, aofs[j] + c * 1024, b + (3 * (TI + j) + c) * 1024);
   };
   struct Frag {
     uint32_t w[2][TI][6], a[2][TJ][6];

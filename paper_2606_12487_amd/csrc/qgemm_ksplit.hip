@@ -25,6 +25,7 @@
 #include <type_traits>
 
 #include "internal.h"
+#include "lds_load.h"
 #include "qgemm_device.h"
 
 namespace dptq {
@@ -34,14 +35,6 @@ using namespace qg;
 
 typedef __attribute__((address_space(3))) uint8_t* lds_ptr;
 
-// Wavefront-wide direct load of 1 KiB (16 bytes per lane) from sbase + voff
-// into LDS at lds_off + 16 * lane.
-__device__ __forceinline__ void dma16(const void* sbase, uint32_t voff, uint32_t lds_off) {
-  asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1"
-               :
-               : "v"(voff), "s"(sbase), "s"(lds_off)
-               : "memory", "m0");
-}
 // Waits that no memory access moves across.
 template <int N>
 __device__ __forceinline__ void wait_vmcnt_fence() {
@@ -145,7 +138,7 @@ qgemm_ksplit(const uint8_t* __restrict__ a_codes, const float* __restrict__ a_sc
 #pragma unroll
       for (int q = 0; q < 2; ++q) {
         const uint32_t o = !TAIL ? wofs[2 * i + q] : WDEC ? wofs[2 * i] : wofs[2 * i + q] - hi[q];
-        dma16(wc, o, base + (2 * i + q) * 1024);
+        load_lds16(wc, o, base + (2 * i + q) * 1024);
       }
   };
   auto load_a = [&](auto tail, int s, int j) __attribute__((always_inline)) {
@@ -155,10 +148,10 @@ qgemm_ksplit(const uint8_t* __restrict__ a_codes, const float* __restrict__ a_sc
     for (int q = 0; q < 2; ++q) {
       const uint32_t la = base + (2 * TI + kAB * j + q) * 1024;
       if constexpr (BITS == 4) {
-        dma16(ac, TAIL ? aofs[2 * j + q] - hi[q] : aofs[2 * j + q], la);
+        load_lds16(ac, TAIL ? aofs[2 * j + q] - hi[q] : aofs[2 * j + q], la);
       } else {
-        dma16(ac, aofs[2 * j + q], la);
-        dma16(TAIL ? ac : ac + 128, aofs[2 * j + q], la + 2048);
+        load_lds16(ac, aofs[2 * j + q], la);
+        load_lds16(TAIL ? ac : ac + 128, aofs[2 * j + q], la + 2048);
       }
     }
   };
