@@ -549,7 +549,8 @@ def kv8_cache(pages, kv_heads, head_dim, device="cuda"):
     f8 = torch.float8_e4m3fn
     return KV8Cache(torch.empty((pages, kv_heads, KV8_PAGE, head_dim), dtype=f8, device=device),
                     torch.empty((pages, kv_heads, head_dim, KV8_PAGE), dtype=f8, device=device),
-                    torch.ones((pages, kv_heads), device=device), torch.ones((pages, kv_heads), device=device))
+                    torch.ones((pages, kv_heads), dtype=torch.float32, device=device),
+                    torch.ones((pages, kv_heads), dtype=torch.float32, device=device))
 
 
 def kv8_append(k, v, cu_seqlens, lengths, page_table, cache, max_new=None):
