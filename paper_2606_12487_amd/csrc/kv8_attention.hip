@@ -143,18 +143,19 @@ __global__ void __launch_bounds__(256, D == 64 ? 4 : D == 128 ? 2 : 1) kv8_decod
           ks = a.k_scales[which(page1)];
           vs = a.v_scales[which(page1)];
         }
-        const int j0 = there(page) ? vis.page(i) * kPage : 1 << 30;
-        if (!page_whole(j0, pmin, pmax, a.window, a.sinks)) {
+        const bool here = there(page);
+        const int j0 = vis.page(i) * kPage;
+        if (!here || !page_whole(j0, pmin, pmax, a.window, a.sinks)) {
 #pragma unroll
           for (int e = 0; e < 16; ++e)
-            s[e] = sees(pos, j0 + 16 * quad + e, a.window, a.sinks) ? s[e] : -INFINITY;
+            s[e] = here && sees(pos, j0 + 16 * quad + e, a.window, a.sinks) ? s[e] : -INFINITY;
         }
         float top = s[0];
 #pragma unroll
         for (int e = 1; e < 16; ++e) top = fmaxf(top, s[e]);
         top *= c;
         const float ratio = unit > 0.0f ? v_scale / unit : 0.0f;
-        const bool other_unit = !(ratio >= 0.0625f && ratio <= 16.0f) && there(page);
+        const bool other_unit = !(ratio >= 0.0625f && ratio <= 16.0f) && here;
         if (__any(top > m + 10.0f) || other_unit) {
           // The four lanes of a row move its reference alike.
           float row_top = fmaxf(top, __shfl_xor(top, 16));
@@ -170,7 +171,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 4 : D == 128 ? 2 : 1) kv8_decod
         }
         // Weights with the v scale in them; their sum without it.
         const float base = m == -INFINITY ? 0.0f : m;
-        const float by = there(page) ? v_scale / unit : 1.0f;
+        const float by = here ? v_scale / unit : 1.0f;
         const float shift = __builtin_amdgcn_logf(by) - base;
         half8 p[2];
         float sum = 0.0f;
@@ -182,10 +183,10 @@ __global__ void __launch_bounds__(256, D == 64 ? 4 : D == 128 ? 2 : 1) kv8_decod
         }
         l = fmaf(sum, 1.0f / by, l);
         // O^T: lane (col, quad) gives channel 16 t + col of tokens 16 quad and
-        // up.  Slots past the sequence's end may hold anything: no NaN of
-        // theirs may meet the zero weight.
-        if (j0 + kPage > seq.length) {
-          const int held = seq.length - j0 - 16 * quad;   // valid slots of this lane's 16
+        // up.  Slots past the sequence's end, and page 0 in place of one that is
+        // not there, may hold anything: no NaN of theirs may meet the zero weight.
+        if (!here || j0 + kPage > seq.length) {
+          const int held = here ? seq.length - j0 - 16 * quad : 0;   // valid slots of this lane's 16
 #pragma unroll
           for (int t = 0; t < kT; ++t) {
             vc[t].x &= held_mask(held, 0);

@@ -61,8 +61,8 @@ __device__ __forceinline__ Visible visible_pages(int pmin, int pmax, int window,
   const int low = window > 0 ? max(pmin - window + 1, 0) : 0;
   const int last = min(pmax / kPage, max_pages - 1);
   const int sink_pages = window > 0 ? min((min(sinks, low) + kPage - 1) / kPage, last + 1) : 0;
-  const int first = max(low / kPage, sink_pages);
-  return Visible{sink_pages, first, sink_pages + max(last - first + 1, 0)};
+  const int first = min(max(low / kPage, sink_pages), last + 1);   // last + 1: none (low may lie beyond the table)
+  return Visible{sink_pages, first, sink_pages + last + 1 - first};
 }
 
 // Whether every row with positions in [pmin, pmax] sees the whole page from
