@@ -405,7 +405,9 @@ int dptq_rms_norm_quant(const void* x, const void* residual, const void* weight,
  *
  * These three are read on the device when the call's work runs; offsets and
  * lengths out of range are clamped.  k_pages, v_pages and the activations must
- * be 16-byte aligned, all else to its elements.
+ * be 16-byte aligned, all else to its elements.  Where num_pages or max_pages
+ * is 0 nothing is written or seen, and the pages, their scales and the table
+ * may be NULL.
  */
 #define DPTQ_KV8_PAGE 64
 

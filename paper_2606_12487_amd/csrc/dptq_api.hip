@@ -77,10 +77,12 @@ int check_kv8_shape(int64_t T, int64_t B, int64_t max_pages, int64_t num_pages, 
   return DPTQ_OK;
 }
 
+// Without pages, in the cache or in the table, nothing of either is read.
 bool kv8_pointers(const dptq::Kv8Cache& c) {
-  return c.k_pages && c.v_pages && c.k_scales && c.v_scales && c.cu && c.lengths && c.table &&
-         aligned16(c.k_pages) && aligned16(c.v_pages) && aligned4(c.k_scales) && aligned4(c.v_scales) &&
-         aligned4(c.cu) && aligned4(c.lengths) && aligned4(c.table);
+  const bool pages = c.num_pages > 0 && c.max_pages > 0;
+  if (pages && !(c.k_pages && c.v_pages && c.k_scales && c.v_scales && c.table)) return false;
+  return c.cu && c.lengths && aligned16(c.k_pages) && aligned16(c.v_pages) && aligned4(c.k_scales) &&
+         aligned4(c.v_scales) && aligned4(c.cu) && aligned4(c.lengths) && aligned4(c.table);
 }
 
 // Rows of n elements, ld apart, that 16-byte loads take.

@@ -1,4 +1,5 @@
-"""The 8-bit paged cache and its attention where sizes and lengths end: lengths beyond any page table."""
+"""The 8-bit paged cache and its attention where sizes and lengths end: lengths beyond any page table, and caches and
+tables without pages."""
 
 import numpy as np
 import pytest
@@ -29,3 +30,20 @@ def test_lengths_beyond_2_to_the_30_see_no_missing_page(new, window, sinks):
     assert np.isneginf(want[1][:new]).all()
     for hints in ({}, dict(max_q=new, max_len=500)):
         _matches(dptq.kv8_attention(_d(q), _d(cu), _d(lengths), _d(table), cache, 0.1, window, sinks, **hints), want)
+
+
+@pytest.mark.parametrize("counts", [[1, 1], [40, 3]])
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_caches_and_tables_without_pages(counts, D):
+    # Nothing is written and nothing is seen.
+    T, H, Hkv = sum(counts), 4, 2
+    q = torch.ones((T, H, D), dtype=torch.float16, device="cuda")
+    k = torch.ones((T, Hkv, D), dtype=torch.float16, device="cuda")
+    cu, n = _d(_cu(counts)), _d(np.array(counts, np.int32))
+    for pages, width in ((0, 3), (2, 0), (0, 0)):
+        cache = dptq.kv8_cache(pages, Hkv, D)
+        table = torch.zeros((2, width), dtype=torch.int32, device="cuda")
+        assert dptq.kv8_append(k, k, cu, n, table, cache) is cache
+        out, lse = torch.full_like(q, 7), torch.full((T, H), 7.0, device="cuda")
+        dptq.kv8_attention(q, cu, n, table, cache, out=out, lse=lse)
+        assert bool((out == 0).all()) and bool(torch.isneginf(lse).all())
