@@ -49,19 +49,66 @@ def test_sources_wait_for_m0():
     assert loads > 0
 
 
-def test_built_library_waits_for_m0(tmp_path):
+@pytest.fixture(scope="module")
+def listings(tmp_path_factory):
+    """The instructions of each device image in the built library."""
     objdump = shutil.which("llvm-objdump") or "/opt/rocm/llvm/bin/llvm-objdump"
     if not os.path.exists(objdump):
         pytest.skip("no llvm-objdump")
     if not os.path.exists(dptq.library_path()):
         B.build()
-    lib = shutil.copy(dptq.library_path(), tmp_path)
-    subprocess.run([objdump, "--offloading", lib], cwd=tmp_path, check=True, stdout=subprocess.DEVNULL)
-    loads = 0
-    for image in sorted(glob.glob(str(tmp_path / f"*{B.ARCH}*"))):
+    path = tmp_path_factory.mktemp("images")
+    lib = shutil.copy(dptq.library_path(), path)
+    subprocess.run([objdump, "--offloading", lib], cwd=path, check=True, stdout=subprocess.DEVNULL)
+    images = []
+    for image in sorted(glob.glob(str(path / f"*{B.ARCH}*"))):
         out = subprocess.run([objdump, "-d", "--no-show-raw-insn", "--no-leading-addr", image], check=True,
                              capture_output=True, text=True).stdout
-        n, bad = missing_waits([line.split("//")[0].strip() for line in out.splitlines()])
+        images.append([line.split("//")[0].strip() for line in out.splitlines()])
+    return images
+
+
+def test_built_library_waits_for_m0(listings):
+    loads = 0
+    for listing in listings:
+        n, bad = missing_waits(listing)
         loads += n
         assert not bad, (len(bad), bad[:3])
     assert loads > 0
+
+
+def scalars(operand):
+    """The scalar registers that an operand names."""
+    m = re.match(r"s(?:(\d+)|\[(\d+):(\d+)\])$", operand)
+    return set() if not m else {int(m[1])} if m[1] else set(range(int(m[2]), int(m[3]) + 1))
+
+
+def late_bases(listing):
+    """Direct loads less than five wait states behind a vector instruction's write of their scalar base."""
+    window, bad = [], []
+    for i in listing:
+        parts = i.replace(",", " ").split()
+        if not parts or i.endswith(":"):
+            continue
+        if "_load_lds_" in parts[0]:
+            base, states = set().union(*map(scalars, parts[1:])), 0
+            for p in reversed(window):
+                if p[0].startswith("v_") and len(p) > 1 and scalars(p[1]) & base:
+                    bad.append((p[0], i))
+                states += int(p[1], 0) + 1 if p[0] == "s_nop" else 1
+                if states >= 5:
+                    break
+        window = (window + [parts])[-5:]
+    return bad
+
+
+def test_built_library_waits_for_scalar_bases(listings):
+    # The other wait that the compiler leaves out of an asm statement: a scalar register that a vector instruction
+    # writes (a lane that is read) is a load's base five wait states later at the earliest.
+    load = "global_load_lds_dwordx4 v1, s[2:3]"
+    write = "v_readlane_b32 s3, v9, 1"
+    assert late_bases([write, "s_mov_b32 m0, s4", "s_nop 0", load]) == [("v_readlane_b32", load)]
+    assert late_bases([write, "s_mov_b32 m0, s4", "s_nop 3", load]) == []
+    for listing in listings:
+        bad = late_bases(listing)
+        assert not bad, (len(bad), bad[:3])
