@@ -454,7 +454,8 @@ int dptq_kv8_append(const void* k, int64_t ld_k, const void* v, int64_t ld_v, in
  *   out = fl16(sum_j P_j * v_scale * v_code_j),   lse = log sum_j exp(S_j)
  *
  * Products and sums in fp32, P rounded to fp16.  A query that sees nothing
- * gives out 0 and lse -inf.  What a masked slot past the sequence's end holds
+ * gives out 0 and lse -inf; rows of q that cu_seqlens gives to no sequence have
+ * unspecified out and lse.  What a masked slot past the sequence's end holds
  * does not matter, NaN included.
  *
  *   q           device, fp16 [T, heads, head_dim], ld_q elements from a token to
@@ -463,8 +464,10 @@ int dptq_kv8_append(const void* k, int64_t ld_k, const void* v, int64_t ld_v, in
  *   scale       finite
  *   window      >= 0 (0: none), sinks >= 0; both < 2^30
  *   max_q       the most queries of a sequence, max_len the longest sequence, as
- *               far as the caller knows: they size the launch and change no
- *               result beyond the order of fp32 sums (0: T, and 64 * max_pages)
+ *               far as the caller knows: they lay out the launch and change no
+ *               result beyond the order of fp32 sums (0: T, and 64 * max_pages;
+ *               a batch of single tokens then runs as prompts do, and short
+ *               sequences in few parts: pass them where time matters)
  *   out         device, fp16 [T, heads, head_dim] output, dense
  *   lse         device, float [T, heads] output
  *   workspace   device, 16-byte aligned, dptq_kv8_attention_workspace bytes for

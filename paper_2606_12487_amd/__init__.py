@@ -568,8 +568,10 @@ def kv8_attention(q, cu_seqlens, lengths, page_table, cache, scale=None, window=
     over the cache, which holds their keys and values already (kv8_append with the same cu_seqlens, lengths and
     page_table) -> (out fp16 [T, heads, head_dim], lse fp32 [T, heads], the log of each row's sum of exponentials).
     scale: of the scores, head_dim ** -0.5 by default.  window > 0: a query sees only the last `window` positions up
-    to its own, and the first `sinks` ones.  max_q, max_len: the most queries and the longest length of a sequence
-    if known (they size the launch)."""
+    to its own, and the first `sinks` ones.  max_q, max_len: the most queries and the longest length of a sequence;
+    no result depends on them but the time does (without them the launch is laid out for one sequence with all the
+    queries and for lengths that fill the page table).  Rows of q that cu_seqlens gives to no sequence are
+    unspecified in out and lse."""
     if scale is None:
         scale = cache[0].shape[-1] ** -0.5
     return _binding().kv8_attention(q, cu_seqlens, lengths, page_table, *cache, max_q, max_len, scale, window,

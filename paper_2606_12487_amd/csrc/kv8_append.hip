@@ -14,10 +14,12 @@
 // factor of two of a floating-point format's range, which e4m3 does not feel.
 //
 // A page that is new (its first slot is written now) has its other slots
-// cleared.  2 bytes read and 1 written per element; bound by the chain of loads
-// (offsets, table, rows) and the reduction between them: a token for each of 64
-// sequences (8 heads of 128) takes 7.4 us, 4500 tokens of three prompts 10.1 us
-// (2.6 TB/s).
+// cleared.  2 bytes read and 1 written per element; bound by latency: the loads
+// of offsets, table and rows in turn (the rows are loaded once the table's entry
+// is known to be a page, though their addresses do not depend on it) and the
+// reduction behind them.  A token for each of 64 sequences (8 heads of 128) takes
+// 7.4 us, 4500 tokens of three prompts 10.1 us (2.6 TB/s), at three workgroups
+// on a compute unit.
 #include "internal.h"
 #include "kv8_device.h"
 #include "wave_device.h"

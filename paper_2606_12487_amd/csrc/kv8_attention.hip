@@ -9,12 +9,15 @@
 //
 // (kc, vc: the e4m3 codes.)  A row that sees nothing gives 0 and -inf.
 //
-// One pass over the keys with the running maximum m and sum l of the softmax
-// in base 2, fp32 throughout except P, which is rounded to fp16 (half to even,
-// relative error 2^-12 of a weight in (0, 1], absolute 2^-25 below 2^-14) as an
-// operand of the second product.  Codes are exact in fp16, queries are taken
-// as they are, and the scales are applied to fp32 sums: k's to the scores, v's
-// by keeping the output accumulators in units of the current page's v scale.
+// One pass over the keys with the softmax's sum l in base 2, relative to a
+// reference m that follows the running maximum (below).  fp32 throughout except
+// P, which is rounded to fp16 as an operand of the second product: half to even,
+// a relative error of 2^-12 of a weight, absolute 2^-25 below 2^-14, where the
+// row's largest weight is 1 or more.  That adds up to a quarter to the error of
+// the outputs' own rounding to fp16 (2.6e-4 against 2.1e-4 of their size).
+// Codes are exact in fp16, queries are taken as they are, and the scales are
+// applied in fp32: k's to the scores, v's as its ratio to the unit in which the
+// output accumulates.
 //
 // Both products run on the matrix cores transposed: S^T = K Q^T has the page's
 // tokens as rows and the queries as columns, O^T = V^T P^T the channels as
@@ -49,7 +52,8 @@ __device__ __forceinline__ uint4 stream16(const uint8_t* p) {
 //
 // Bound by the bytes of the cache: 64 sequences of up to 8192 tokens (64 heads
 // on 8, head size 128) take 141 us, 4.9 TB/s; two of up to 131072 take 86 us,
-// 5.3 TB/s; 16 with 32 key heads behind a window of 4096 take 90 us, 5.9 TB/s.
+// 5.3 TB/s; 16 with 32 key heads behind a window of 4096 take 90 us, 6.0 TB/s
+// (a plain read stream reaches 7.1).
 template <int D>
 __global__ void __launch_bounds__(256, D == 64 ? 4 : D == 128 ? 2 : 1) kv8_decode_kernel(AttnArgs a) {
   constexpr int kC = D / 64;     // 64-channel parts of a row

@@ -28,8 +28,8 @@ struct AttnArgs {
   int chunk, splits;       // pages of a part; the last part takes what is left
   __half* out;
   float* lse;
-  float* part_o;           // [splits][T * heads][D], relative to their maxima
-  float2* part_ml;         // [splits][T * heads] (maximum, sum), base 2
+  float* part_o;           // [splits][T * heads][D], relative to their references
+  float2* part_ml;         // [splits][T * heads] (reference, sum), base 2
 };
 
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }

@@ -15,7 +15,7 @@
 // list of the best `top`, the few logits that enter it.  Rows are split over
 // workgroups while there are too few of them; a second launch then joins the
 // parts.  Without alternatives 256 threads hold 32 logits each: 2047 x 100003
-// fp32 take 143 us, 5.7 TB/s, bound by bytes.  With them 512 hold 16, so that
+// fp32 take 143 us, 5.7 of a plain read's 7.1 TB/s, bound by bytes.  With them 512 hold 16, so that
 // the work that a row needs once (bound, ranks, join) is spread wider: 64 x
 // 131072 fp16 with 20 alternatives take 22.3 us, bound by the latency of those
 // chains in two launches (27 us with 256 threads, 27.6 with 1024).
@@ -395,8 +395,8 @@ __global__ void __launch_bounds__(TOP ? kTopThreads : 64) join_logprobs_kernel(L
   }
 }
 
-// Parts of a row: enough workgroups for 8 of 256 threads, or the two of 1024
-// that it holds, on each compute unit, of one chunk or more.
+// Parts of a row: enough workgroups for 8 of 256 threads, or with alternatives
+// the two of 512 that it holds, on each compute unit, of one chunk or more.
 int choose_splits(const TokenLogprobs& c) {
   const int64_t chunks = ((int64_t)c.V + kChunk - 1) / kChunk;
   const int64_t want = ((c.top ? 2 : 8) * (int64_t)device_cus() + c.M - 1) / c.M;
