@@ -12,7 +12,7 @@
 // One pass over the keys with the softmax's sum l in base 2, relative to a
 // reference m that follows the running maximum (below).  fp32 throughout except
 // P, which is rounded to fp16 as an operand of the second product: half to even,
-// a relative error of 2^-12 of a weight, absolute 2^-25 below 2^-14, where the
+// a relative error up to 2^-11 of a weight, absolute 2^-25 below 2^-14, where the
 // row's largest weight is 1 or more.  That adds up to a quarter to the error of
 // the outputs' own rounding to fp16 (2.6e-4 against 2.1e-4 of their size).
 // Codes are exact in fp16, queries are taken as they are, and the scales are

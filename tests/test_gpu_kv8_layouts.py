@@ -93,3 +93,32 @@ def test_decode_in_hundreds_of_parts(lengths, width):
     cu, arrays = _cu([1] * B), _host(cache)
     args = (_d(q), _d(cu), _d(np.array(lengths, np.int32)), _d(wide), cache)
     _check(args, dict(max_q=1), arrays, q, cu, lengths, wide, [0], Hkv, 0, 0)
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_prompts_in_a_graph(D):
+    # Replays give what the eager call gives on the same buffers, with eager work between them.
+    rng = np.random.default_rng(D + 7)
+    Hkv, group = 2, 4
+    lengths, new = [300, 90], [100, 37]
+    cache, table = _sequences(rng, lengths, Hkv, D, 2)
+    q = torch.zeros((sum(new), Hkv * group, D), dtype=torch.float16, device="cuda")
+    n, cu, tab = _d(np.array(lengths, np.int32)), _d(_cu(new)), _d(table)
+    out, lse = torch.empty_like(q), torch.empty(q.shape[:2], device="cuda")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        dptq.kv8_attention(q, cu, n, tab, cache, window=150, sinks=3, max_q=100, out=out, lse=lse)
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        dptq.kv8_attention(q, cu, n, tab, cache, window=150, sinks=3, max_q=100, out=out, lse=lse)
+    for i in range(4):
+        q.copy_(_d(rng.standard_normal(tuple(q.shape)).astype(np.float16)))
+        n.copy_(_d(np.array([300 - 60 * i, 90 - 11 * i], np.int32)))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = out.clone(), lse.clone()
+        want = dptq.kv8_attention(q, cu, n, tab, cache, window=150, sinks=3, max_q=100)
+        assert torch.equal(got[0].view(torch.int16), want[0].view(torch.int16))
+        assert torch.equal(got[1].view(torch.int32), want[1].view(torch.int32))
