@@ -444,6 +444,53 @@ int dptq_kv8_append(const void* k, int64_t ld_k, const void* v, int64_t ld_v, in
                     float* v_scales, int64_t max_new, void* stream);
 
 /*
+ * dptq_rotary - rotary positions on queries and keys, in one launch.
+ *
+ * Of each head the first rotary_dim = r channels turn in pairs, the others are
+ * copied.  Pair i < r / 2 is channels (i, i + r / 2), or (2i, 2i + 1) where
+ * interleaved; its angle is a = positions[t] * inv_freq[i], in 64 bits:
+ *
+ *   y1 = fl16(c x1 - s x2),  y2 = fl16(s x1 + c x2),  c = scale cos a, s = scale sin a
+ *
+ * in fp32.  Frequencies stretched for long contexts are other inv_freq, and the
+ * factor that some of them go with is scale.
+ *
+ *   q          device, fp16 [T, heads, head_dim], ld_q elements from a token to
+ *              the next (a multiple of 8, >= heads * head_dim)
+ *   k          the same with kv_heads and ld_k; NULL with kv_heads = 0
+ *   T          tokens, 0 <= T < 2^30; heads >= 1, heads + kv_heads <= 8192
+ *   head_dim   a multiple of 8, 8 <= head_dim <= 512
+ *   positions  device, int32 [T], any value
+ *   inv_freq   device, double [r / 2], 8-byte aligned, finite
+ *   rotary_dim even, 2 <= rotary_dim <= head_dim
+ *   scale      finite
+ *   q_out, k_out  device, fp16 outputs, ld_q_out and ld_k_out as ld_q: q and k
+ *              themselves (with the same ld), or memory that does not overlap them
+ */
+int dptq_rotary(const void* q, int64_t ld_q, int32_t heads, const void* k, int64_t ld_k, int32_t kv_heads,
+                int64_t T, int32_t head_dim, const int32_t* positions, const double* inv_freq,
+                int32_t rotary_dim, int32_t interleaved, float scale, void* q_out, int64_t ld_q_out,
+                void* k_out, int64_t ld_k_out, void* stream);
+
+/*
+ * dptq_rotary_kv8_append - dptq_rotary and dptq_kv8_append in one launch: q is
+ * rotated into q_out, and k, rotated and rounded to fp16, goes into the cache
+ * with v.  The same bits as the two calls.
+ *
+ * Token row cu_seqlens[b] + i is at position lengths[b] - (new tokens of b) + i,
+ * of q as of k; q is rotated whether or not the token's page is there.  Rows
+ * that cu_seqlens gives to no sequence are not written in q_out.  k itself is
+ * only read.  Arguments as for the two calls; head_dim as for the cache.
+ */
+int dptq_rotary_kv8_append(const void* q, int64_t ld_q, int32_t heads, const void* k, int64_t ld_k,
+                           const void* v, int64_t ld_v, int64_t T, const int32_t* cu_seqlens,
+                           const int32_t* lengths, int64_t B, const int32_t* page_table,
+                           int64_t max_pages, int64_t num_pages, int32_t kv_heads, int32_t head_dim,
+                           uint8_t* k_pages, uint8_t* v_pages, float* k_scales, float* v_scales,
+                           const double* inv_freq, int32_t rotary_dim, int32_t interleaved, float scale,
+                           void* q_out, int64_t ld_q_out, int64_t max_new, void* stream);
+
+/*
  * dptq_kv8_attention - attention of the new tokens' queries over the cache,
  * which holds their keys and values already.
  *

@@ -15,6 +15,7 @@ calling a function whose library is missing raises.
 import collections
 import ctypes
 import importlib.util
+import math
 import os
 
 __all__ = ["DptqError", "lib", "library_path", "rotate_quant", "qlinear", "qlinear_acc",
@@ -26,7 +27,7 @@ __all__ = ["DptqError", "lib", "library_path", "rotate_quant", "qlinear", "qline
            "WEIGHTS_FP6", "WEIGHTS_A8_ORDER", "WEIGHTS_DECODE", "qlinear_decode_native",
            "qlinear_decode_native_acc",
            "rms_norm_quant", "KV8Cache", "KV8_PAGE", "kv8_cache", "kv8_append", "kv8_attention",
-           "token_logprobs", "MAX_TOP",
+           "token_logprobs", "MAX_TOP", "rotary", "rotary_inv_freq", "rotary_kv8_append",
            "EXPORTED_FUNCTIONS", "GEMM_AUTO",
            "GEMM_DECODE", "GEMM_TILE_256X128", "GEMM_TILE_192X256"]
 
@@ -49,7 +50,8 @@ EXPORTED_FUNCTIONS = ("dptq_status_string", "dptq_version", "dptq_rotate_quant",
                       "dptq_qlinear_a8", "dptq_prepacked_bytes", "dptq_prepack_weights",
                       "dptq_qlinear_decode_native", "dptq_rms_norm_quant", "dptq_kv8_append",
                       "dptq_kv8_attention_workspace", "dptq_kv8_attention",
-                      "dptq_token_logprobs_workspace", "dptq_token_logprobs")
+                      "dptq_token_logprobs_workspace", "dptq_token_logprobs", "dptq_rotary",
+                      "dptq_rotary_kv8_append")
 
 # Code layouts of dptq_rotate_quant_ex.
 LAYOUT_PACKED, LAYOUT_FP6 = 0, 1
@@ -115,6 +117,12 @@ def lib():
         L.dptq_kv8_attention.argtypes = [vp, i64, i64, vp, vp, i64, vp, i64, i64, i32, i32, i32, vp, vp, vp, vp,
                                          ctypes.c_float, i32, i32, i64, i64, vp, vp, vp, i64, vp]
         L.dptq_kv8_attention.restype = ctypes.c_int
+        L.dptq_rotary.argtypes = [vp, i64, i32, vp, i64, i32, i64, i32, vp, vp, i32, i32, ctypes.c_float, vp, i64, vp,
+                                  i64, vp]
+        L.dptq_rotary.restype = ctypes.c_int
+        L.dptq_rotary_kv8_append.argtypes = [vp, i64, i32, vp, i64, vp, i64, i64, vp, vp, i64, vp, i64, i64, i32, i32,
+                                             vp, vp, vp, vp, vp, i32, i32, ctypes.c_float, vp, i64, i64, vp]
+        L.dptq_rotary_kv8_append.restype = ctypes.c_int
         L.dptq_token_logprobs_workspace.argtypes = [i64, i64, i32, i32]
         L.dptq_token_logprobs_workspace.restype = ctypes.c_int64
         L.dptq_token_logprobs.argtypes = [vp, i32, i64, i64, i64, vp, i32, vp, vp, vp, vp, vp, i64, vp]
@@ -560,6 +568,55 @@ def kv8_append(k, v, cu_seqlens, lengths, page_table, cache, max_new=None):
     most new tokens of a sequence if known (sizes the launch; no result depends on it)."""
     _binding().kv8_append(k, v, cu_seqlens, lengths, page_table, *cache, max_new)
     return cache
+
+
+def rotary_inv_freq(rotary_dim, base=10000.0, factor=1.0, original_length=None, low_turns=1.0, high_turns=4.0,
+                    ramp="turns", device="cuda"):
+    """Frequencies of rotary positions: float64 [rotary_dim / 2], base ** (-2 i / rotary_dim).  For contexts `factor`
+    times as long as those of the training: divided by factor; with original_length, the length trained for, only
+    where a pair turns at most low_turns times over it, not at all where it turns high_turns times or more, and in
+    between in proportion to the turns (ramp "turns") or to i (ramp "index", from the whole i below high_turns to the
+    one above low_turns)."""
+    if rotary_dim < 2 or rotary_dim % 2:
+        raise ValueError("rotary_dim must be even and positive")
+    if not (base > 1 and factor > 0):
+        raise ValueError("base must be above 1 and factor positive")
+    if ramp not in ("turns", "index"):
+        raise ValueError('ramp must be "turns" or "index"')
+    n = rotary_dim // 2
+    f = [float(base) ** (-i / n) for i in range(n)]
+    if original_length is None:
+        f = [x / factor for x in f]
+    else:
+        if not (original_length > 0 and 0 < low_turns < high_turns):
+            raise ValueError("original_length must be positive and 0 < low_turns < high_turns")
+        turns = original_length / (2 * math.pi)    # of a pair of frequency 1
+        if ramp == "index":                        # f = turns^-1 t at index n log(turns / t) / log(base)
+            first, last = (n * math.log(turns / t) / math.log(base) for t in (high_turns, low_turns))
+            first, last = max(math.floor(first), 0), min(math.ceil(last), n - 1)
+            kept = [1 - (i - first) / max(last - first, 1e-3) for i in range(n)]
+        else:
+            kept = [(x * turns - low_turns) / (high_turns - low_turns) for x in f]
+        f = [x * (k + (1 - k) / factor) for x, k in zip(f, (min(max(k, 0.0), 1.0) for k in kept))]
+    torch = _torch()
+    return torch.tensor(f, dtype=torch.float64, device=device)
+
+
+def rotary(q, k, positions, inv_freq, interleaved=False, scale=1.0, q_out=None, k_out=None):
+    """Rotary positions on queries and keys (fp16 [T, heads, head_dim]; rows may be parts of wider ones; k may be
+    None) -> (q_out, k_out).  positions int32 [T]; inv_freq float64 [r / 2] (rotary_inv_freq): of each head the first r
+    channels turn, in pairs (i, i + r / 2), or (2i, 2i + 1) where interleaved, by positions * inv_freq[i].  scale: of
+    the channels that turn.  q_out, k_out may be q and k."""
+    return _binding().rotary(q, k, positions, inv_freq, interleaved, scale, q_out, k_out)
+
+
+def rotary_kv8_append(q, k, v, cu_seqlens, lengths, page_table, cache, inv_freq, interleaved=False, scale=1.0,
+                      max_new=None, q_out=None):
+    """rotary and kv8_append in one launch, with the same bits: rotates the new tokens' queries into q_out, which it
+    returns, and writes their rotated keys and their values into the cache, in place.  Positions are those of the
+    tokens in their sequences; q_out may be q, and its rows that cu_seqlens gives to no sequence are not written."""
+    return _binding().rotary_kv8_append(q, k, v, cu_seqlens, lengths, page_table, *cache, inv_freq, interleaved, scale,
+                                        max_new, q_out)
 
 
 def kv8_attention(q, cu_seqlens, lengths, page_table, cache, scale=None, window=0, sinks=0, max_q=None,

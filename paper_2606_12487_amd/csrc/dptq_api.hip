@@ -1,6 +1,7 @@
 // C ABI: argument checks, then dispatch to the gfx950 kernels.
 #include "dptq.h"
 #include "internal.h"
+#include "rotary_device.h"
 
 namespace {
 
@@ -110,6 +111,15 @@ int attention_shape(int64_t T, int64_t B, int64_t max_pages, int64_t num_pages, 
   c->sinks = sinks;
   c->max_q = max_q > 0 && max_q < T ? max_q : T;
   c->max_len = max_len > 0 && max_len < capacity ? max_len : capacity;
+  return DPTQ_OK;
+}
+
+// What rotary positions add to the check of a call.
+int check_rotary(int32_t heads, int32_t kv_heads, int32_t head_dim, int32_t rotary_dim, float scale) {
+  if (heads < 1 || kv_heads < 0 || head_dim < 1 || head_dim % 8 != 0) return DPTQ_ERR_INVALID_ARG;
+  if (rotary_dim < 2 || rotary_dim % 2 != 0 || rotary_dim > head_dim) return DPTQ_ERR_INVALID_ARG;
+  if (!(scale >= -3.0e38f && scale <= 3.0e38f)) return DPTQ_ERR_INVALID_ARG;   // also rejects NaN
+  if (head_dim > dptq::kMaxRotaryHead || heads > 8192 || kv_heads > 8192 - heads) return DPTQ_ERR_UNSUPPORTED;
   return DPTQ_OK;
 }
 
@@ -493,6 +503,51 @@ int dptq_kv8_append(const void* k, int64_t ld_k, const void* v, int64_t ld_v, in
   if (!kv8_pointers(c) || !rows_ok(k, ld_k, row) || !rows_ok(v, ld_v, row)) return DPTQ_ERR_INVALID_ARG;
   return from_hip(dptq::launch_kv8_append(c, k, ld_k, v, ld_v, max_new > 0 && max_new < T ? max_new : T,
                                           static_cast<hipStream_t>(stream)));
+}
+
+int dptq_rotary(const void* q, int64_t ld_q, int32_t heads, const void* k, int64_t ld_k, int32_t kv_heads,
+                int64_t T, int32_t head_dim, const int32_t* positions, const double* inv_freq,
+                int32_t rotary_dim, int32_t interleaved, float scale, void* q_out, int64_t ld_q_out,
+                void* k_out, int64_t ld_k_out, void* stream) {
+  const int st = check_rotary(heads, kv_heads, head_dim, rotary_dim, scale);
+  if (st != DPTQ_OK) return st;
+  if (T < 0) return DPTQ_ERR_INVALID_ARG;
+  if (T >= kMost30) return DPTQ_ERR_UNSUPPORTED;
+  if (T == 0) return DPTQ_OK;
+  const int64_t row = (int64_t)heads * head_dim, kv_row = (int64_t)kv_heads * head_dim;
+  if (!rows_ok(q, ld_q, row) || !rows_ok(q_out, ld_q_out, row)) return DPTQ_ERR_INVALID_ARG;
+  if (kv_heads > 0 && (!rows_ok(k, ld_k, kv_row) || !rows_ok(k_out, ld_k_out, kv_row))) return DPTQ_ERR_INVALID_ARG;
+  if (!positions || !inv_freq || !aligned4(positions) || !aligned8(inv_freq)) return DPTQ_ERR_INVALID_ARG;
+  if ((q == q_out && ld_q != ld_q_out) || (kv_heads > 0 && k == k_out && ld_k != ld_k_out))
+    return DPTQ_ERR_INVALID_ARG;
+  const dptq::RotaryCall c{q, k, q_out, k_out, ld_q, ld_k, ld_q_out, ld_k_out, T, heads, kv_heads,
+                           head_dim, rotary_dim, positions, inv_freq, interleaved != 0, scale};
+  return from_hip(dptq::launch_rotary(c, static_cast<hipStream_t>(stream)));
+}
+
+int dptq_rotary_kv8_append(const void* q, int64_t ld_q, int32_t heads, const void* k, int64_t ld_k,
+                           const void* v, int64_t ld_v, int64_t T, const int32_t* cu_seqlens,
+                           const int32_t* lengths, int64_t B, const int32_t* page_table,
+                           int64_t max_pages, int64_t num_pages, int32_t kv_heads, int32_t head_dim,
+                           uint8_t* k_pages, uint8_t* v_pages, float* k_scales, float* v_scales,
+                           const double* inv_freq, int32_t rotary_dim, int32_t interleaved, float scale,
+                           void* q_out, int64_t ld_q_out, int64_t max_new, void* stream) {
+  int st = check_kv8_shape(T, B, max_pages, num_pages, kv_heads, head_dim);
+  if (st == DPTQ_OK) st = check_rotary(heads, kv_heads, head_dim, rotary_dim, scale);
+  if (st != DPTQ_OK) return st;
+  if (max_new < 0) return DPTQ_ERR_INVALID_ARG;
+  if (T == 0 || B == 0) return DPTQ_OK;
+  const dptq::Kv8Cache c{k_pages, v_pages, k_scales, v_scales, cu_seqlens, lengths, page_table,
+                         T, B, max_pages, num_pages, kv_heads, head_dim};
+  const int64_t row = (int64_t)heads * head_dim, kv_row = (int64_t)kv_heads * head_dim;
+  if (!kv8_pointers(c) || !rows_ok(k, ld_k, kv_row) || !rows_ok(v, ld_v, kv_row)) return DPTQ_ERR_INVALID_ARG;
+  if (!rows_ok(q, ld_q, row) || !rows_ok(q_out, ld_q_out, row) || (q == q_out && ld_q != ld_q_out))
+    return DPTQ_ERR_INVALID_ARG;
+  if (!inv_freq || !aligned8(inv_freq)) return DPTQ_ERR_INVALID_ARG;
+  const dptq::RotaryCall r{q, k, q_out, nullptr, ld_q, ld_k, ld_q_out, 0, T, heads, kv_heads,
+                           head_dim, rotary_dim, nullptr, inv_freq, interleaved != 0, scale};
+  return from_hip(dptq::launch_rotary_kv8_append(c, r, v, ld_v, max_new > 0 && max_new < T ? max_new : T,
+                                                 static_cast<hipStream_t>(stream)));
 }
 
 int64_t dptq_kv8_attention_workspace(int64_t T, int64_t B, int64_t max_pages, int32_t heads,

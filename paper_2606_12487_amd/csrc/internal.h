@@ -65,6 +65,23 @@ struct Kv8Cache {
 // ld_k, ld_v: elements from a token's row to the next; max_new sizes the grid.
 hipError_t launch_kv8_append(const Kv8Cache& c, const void* k, int64_t ld_k, const void* v, int64_t ld_v,
                              int64_t max_new, hipStream_t stream);
+// Rotary positions (rotary_device.h) on q and k (kv_heads 0: q alone), out of
+// place or in place; ld: elements from a token's row to the next.
+struct RotaryCall {
+  const void *q, *k;
+  void *q_out, *k_out;
+  int64_t ld_q, ld_k, ld_q_out, ld_k_out, T;
+  int heads, kv_heads, head_dim, rotary_dim;
+  const int32_t* positions;   // [T]; not read by launch_rotary_kv8_append
+  const double* inv_freq;     // [rotary_dim / 2]
+  bool interleaved;
+  float scale;
+};
+hipError_t launch_rotary(const RotaryCall& c, hipStream_t stream);
+// launch_kv8_append with the keys of r, rotated, and q rotated into q_out: the
+// positions are those of the new tokens.  r.k_out is not written.
+hipError_t launch_rotary_kv8_append(const Kv8Cache& c, const RotaryCall& r, const void* v, int64_t ld_v,
+                                    int64_t max_new, hipStream_t stream);
 struct Kv8Attention {
   Kv8Cache cache;
   const void* q;

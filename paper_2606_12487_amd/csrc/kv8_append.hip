@@ -20,8 +20,16 @@
 // reduction behind them.  A token for each of 64 sequences (8 heads of 128) takes
 // 7.4 us, 4500 tokens of three prompts 10.1 us (2.6 TB/s), at three workgroups
 // on a compute unit.
+//
+// With rotary positions (kv8_append_kernel<D, true>) the keys are rotated and
+// rounded to fp16 first, in the same registers: a workgroup of K loads the other
+// channel of each pair too (a second load of bytes that its neighbour loads) and
+// computes its own angles.  Further workgroups rotate the queries, 64 tokens of
+// a sequence each, a token and a part of its heads to a wave.  The codes are
+// those of rotary and kv8_append one after the other, bit for bit.
 #include "internal.h"
 #include "kv8_device.h"
+#include "rotary_device.h"
 #include "wave_device.h"
 
 namespace dptq {
@@ -37,6 +45,67 @@ struct AppendArgs {
   const int32_t *cu, *lengths, *table;
   int T, max_pages, num_pages, heads;
 };
+
+// The queries' side of a call with rotary positions.
+struct RotaryQ {
+  Rotary r;
+  const __half* q;
+  __half* out;
+  int64_t ld, ld_out;
+  int heads, parts;   // parts of 256 units
+};
+constexpr int kRotaryUnits = 4;   // of a lane
+
+// Rotates the queries of tokens [64 x, 64 x + 64) of a sequence, and so on by
+// gridDim.x; the workgroup is slice `slice` of `slices` of them.
+template <bool INTER, bool WIDE>
+__device__ __forceinline__ void rotate_q(const RotaryQ& a, const KvSeq& s, int slice, int slices, float2* angles) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  for (int64_t first = 64 * (int64_t)blockIdx.x; first < s.count; first += 64 * (int64_t)gridDim.x) {
+    const int tokens = (int)min((int64_t)64, s.count - first);
+    for (int i = slice * (kThreads / 64) + wave; i < tokens * a.parts; i += slices * (kThreads / 64)) {
+      const int t = i / a.parts, part = i - t * a.parts;
+      const int64_t row = s.first_row + first + t;
+      rotary_angles(a.r, (int)(s.start + first + t), angles, lane);
+      rotary_units<INTER, WIDE, kRotaryUnits>(a.r, angles, RotaryRows{a.q + row * a.ld, a.out + row * a.ld_out, a.heads},
+                                              RotaryRows{nullptr, nullptr, 0}, part * 64 * kRotaryUnits, lane);
+      // The next token's angles wait for these reads.
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+    }
+  }
+}
+
+// Octet v (channels c to c + 7) of the key row at head, at position p, rotated.
+__device__ __forceinline__ uint4 rotate_octet(const Rotary& r, uint4 v, const __half* head, int c, int p) {
+  if (c >= 2 * r.half) return v;
+  float f[8], g[8], y[8];
+  unpack8(v, f);
+  const bool second = c >= r.half;   // of whole octets' pairs
+  if (r.interleaved) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) g[j] = f[j ^ 1];
+  } else if (r.wide) {
+    unpack8(*reinterpret_cast<const uint4*>(head + (second ? c - r.half : c + r.half)), g);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int ch = c + j;
+      if (ch < 2 * r.half) g[j] = __half2float(head[ch < r.half ? ch + r.half : ch - r.half]);
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const int ch = c + j;
+    y[j] = f[j];
+    if (ch >= 2 * r.half) continue;   // an octet that the pairs end in
+    const bool upper = r.interleaved ? ch & 1 : ch >= r.half;
+    const int i = r.interleaved ? ch >> 1 : upper ? ch - r.half : ch;
+    const float2 t = rotary_angle(p, r.inv_freq[i], r.scale);
+    y[j] = upper ? rotary_second(g[j], f[j], t) : rotary_first(f[j], g[j], t);
+  }
+  return pack8(y);
+}
 
 // Two floats to e4m3, in the low or high half of old.
 template <bool HI>
@@ -67,8 +136,8 @@ __device__ __forceinline__ uint32_t slot_mask(int first, int lo, int hi) {
   return m;
 }
 
-template <int D>
-__global__ void __launch_bounds__(kThreads) kv8_append_kernel(AppendArgs a) {
+template <int D, bool ROTARY>
+__global__ void __launch_bounds__(kThreads) kv8_append_kernel(AppendArgs a, RotaryQ rq) {
   constexpr int kOctets = D / 8;                       // of channels
   constexpr int kPer = kPage * kOctets / kThreads;     // tokens x octets of a thread
   constexpr int kRow = kPage + 4;                      // of the staged V codes, a channel a row
@@ -77,6 +146,19 @@ __global__ void __launch_bounds__(kThreads) kv8_append_kernel(AppendArgs a) {
   const int b = blockIdx.z, head = blockIdx.y >> 1;
   const bool is_v = blockIdx.y & 1;
   const KvSeq q = kv_seq(a.cu, a.lengths, b, a.T);
+  if constexpr (ROTARY) {
+    if ((int)blockIdx.y >= 2 * a.heads) {
+      __shared__ float2 angles[kThreads / 64][D / 2];
+      float2* const mine = angles[threadIdx.x >> 6];
+      const int slice = blockIdx.y - 2 * a.heads, slices = gridDim.y - 2 * a.heads;
+      if (rq.r.interleaved)
+        rq.r.wide ? rotate_q<true, true>(rq, q, slice, slices, mine) : rotate_q<true, false>(rq, q, slice, slices, mine);
+      else
+        rq.r.wide ? rotate_q<false, true>(rq, q, slice, slices, mine)
+                  : rotate_q<false, false>(rq, q, slice, slices, mine);
+      return;
+    }
+  }
   if (q.count == 0 || q.length == 0) return;
   const int begin = max(q.start, 0);
   const int last_block = min((q.length - 1) / kPage, a.max_pages - 1);
@@ -107,6 +189,18 @@ __global__ void __launch_bounds__(kThreads) kv8_append_kernel(AppendArgs a) {
       if (slot >= lo && slot < hi) {
         const int64_t t = (int64_t)q.first_row + ((int64_t)blk * kPage + slot - q.start);
         v[i] = *reinterpret_cast<const uint4*>(rows + t * a.ld[is_v]);
+      }
+    }
+    if constexpr (ROTARY) {
+      if (!is_v) {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+          const int slot = first_slot + i * slot_step;
+          if (slot < lo || slot >= hi) continue;
+          const int p = blk * kPage + slot;
+          const int64_t t = (int64_t)q.first_row + ((int64_t)p - q.start);
+          v[i] = rotate_octet(rq.r, v[i], rows - 8 * octet + t * a.ld[0], 8 * octet, p);
+        }
       }
     }
 #pragma unroll
@@ -194,10 +288,7 @@ __global__ void __launch_bounds__(kThreads) kv8_append_kernel(AppendArgs a) {
   }
 }
 
-}  // namespace
-
-hipError_t launch_kv8_append(const Kv8Cache& c, const void* k, int64_t ld_k, const void* v, int64_t ld_v,
-                             int64_t max_new, hipStream_t stream) {
+AppendArgs append_args(const Kv8Cache& c, const void* k, int64_t ld_k, const void* v, int64_t ld_v) {
   AppendArgs a{};
   a.x[0] = static_cast<const __half*>(k);
   a.x[1] = static_cast<const __half*>(v);
@@ -214,17 +305,52 @@ hipError_t launch_kv8_append(const Kv8Cache& c, const void* k, int64_t ld_k, con
   a.max_pages = (int)c.max_pages;
   a.num_pages = (int)c.num_pages;
   a.heads = c.kv_heads;
-  // Pages that max_new tokens can touch; a sequence with more loops.
-  int64_t blocks = (max_new + kPage - 2) / kPage + 1;
-  blocks = blocks < c.max_pages ? blocks : c.max_pages;
-  const dim3 grid((unsigned)(blocks < 65535 ? blocks : 65535), (unsigned)(2 * c.kv_heads), (unsigned)c.B);
-  switch (c.head_dim) {
-    case 64: kv8_append_kernel<64><<<grid, kThreads, 0, stream>>>(a); break;
-    case 128: kv8_append_kernel<128><<<grid, kThreads, 0, stream>>>(a); break;
-    case 256: kv8_append_kernel<256><<<grid, kThreads, 0, stream>>>(a); break;
+  return a;
+}
+
+template <bool ROTARY>
+hipError_t launch(const AppendArgs& a, const RotaryQ& rq, int head_dim, dim3 grid, hipStream_t stream) {
+  switch (head_dim) {
+    case 64: kv8_append_kernel<64, ROTARY><<<grid, kThreads, 0, stream>>>(a, rq); break;
+    case 128: kv8_append_kernel<128, ROTARY><<<grid, kThreads, 0, stream>>>(a, rq); break;
+    case 256: kv8_append_kernel<256, ROTARY><<<grid, kThreads, 0, stream>>>(a, rq); break;
     default: return hipErrorInvalidValue;
   }
   return hipGetLastError();
+}
+
+// Workgroups along a sequence's new tokens, for what `most` tiles of 64 hold.
+unsigned tiles(int64_t most) { return (unsigned)(most < 1 ? 1 : most < 65535 ? most : 65535); }
+
+}  // namespace
+
+hipError_t launch_kv8_append(const Kv8Cache& c, const void* k, int64_t ld_k, const void* v, int64_t ld_v,
+                             int64_t max_new, hipStream_t stream) {
+  // Pages that max_new tokens can touch; a sequence with more loops.
+  const int64_t blocks = (max_new + kPage - 2) / kPage + 1;
+  const dim3 grid(tiles(blocks < c.max_pages ? blocks : c.max_pages), (unsigned)(2 * c.kv_heads), (unsigned)c.B);
+  return launch<false>(append_args(c, k, ld_k, v, ld_v), RotaryQ{}, c.head_dim, grid, stream);
+}
+
+hipError_t launch_rotary_kv8_append(const Kv8Cache& c, const RotaryCall& r, const void* v, int64_t ld_v,
+                                    int64_t max_new, hipStream_t stream) {
+  AppendArgs a = append_args(c, r.k, r.ld_k, v, ld_v);
+  if (c.num_pages == 0) a.max_pages = 0;   // nothing of the table is read
+  RotaryQ rq{};
+  rq.r = make_rotary(r.inv_freq, r.head_dim, r.rotary_dim, r.interleaved, r.scale);
+  rq.q = static_cast<const __half*>(r.q);
+  rq.out = static_cast<__half*>(r.q_out);
+  rq.ld = r.ld_q;
+  rq.ld_out = r.ld_q_out;
+  rq.heads = r.heads;
+  rq.parts = (int)(((int64_t)r.heads * rq.r.units + 64 * kRotaryUnits - 1) / (64 * kRotaryUnits));
+  // Slices of the queries of up to 64 tokens: as many as give a wave four
+  // tokens' parts.
+  const int64_t waves = (max_new < 64 ? max_new : 64) * rq.parts;
+  const int64_t slices = (waves + 15) / 16;
+  const dim3 grid(tiles((max_new + kPage - 2) / kPage + 1), (unsigned)(2 * c.kv_heads + (slices < 1024 ? slices : 1024)),
+                  (unsigned)c.B);
+  return launch<true>(a, rq, c.head_dim, grid, stream);
 }
 
 }  // namespace dptq

@@ -599,6 +599,101 @@ PyObject* kv8_append(PyObject* const* a) {
   Py_RETURN_NONE;
 }
 
+// An output of token rows [T, heads, D]: a new dense one, or the caller's, whose
+// rows may be parts of wider ones.
+struct RowsOut {
+  Out out;
+  int64_t ld;
+  RowsOut(PyObject* given, const char* name, int64_t T, int64_t heads, int64_t D, const at::Tensor& x, const char* of)
+      : out(Py_None, name, at::kHalf, {T, heads, D}, x), ld(heads * D) {
+    if (given == Py_None) return;
+    out.t = token_rows(given, name, T, heads, D, &ld);
+    same_device(out.t, name, x, of);
+    Py_INCREF(given);
+    out.o = given;
+  }
+};
+
+double real(PyObject* o) {
+  PyObject* f = PyNumber_Float(o);
+  if (!f) throw Raised{};
+  const double v = PyFloat_AS_DOUBLE(f);
+  Py_DECREF(f);
+  return v;
+}
+
+bool truth(PyObject* o) {
+  const int v = PyObject_IsTrue(o);
+  if (v < 0) throw Raised{};
+  return v == 1;
+}
+
+// The frequencies of rotary positions, at most head_dim / 2 of them.
+const at::Tensor& frequencies(PyObject* o, int64_t D, const at::Tensor& x, const char* of) {
+  const at::Tensor& f = tensor(o, "inv_freq", at::kDouble);
+  if (f.dim() != 1 || f.size(0) < 1 || 2 * f.size(0) > D)
+    fail(PyExc_ValueError, "inv_freq must be 1-D with 1 to head_dim / 2 frequencies");
+  same_device(f, "inv_freq", x, of);
+  return f;
+}
+
+int64_t head_dim_of(PyObject* o, const char* name) {
+  const at::Tensor& t = gpu_tensor(o, name, at::kHalf);
+  if (t.dim() != 3) fail(PyExc_ValueError, std::string(name) + " must be 3-D [T, heads, head_dim]");
+  return t.size(2);
+}
+
+// rotary(q, k, positions, inv_freq, interleaved, scale, q_out, k_out)
+PyObject* rotary(PyObject* const* a) {
+  const int64_t D = head_dim_of(a[0], "q");
+  int64_t ld_q, ld_k = 0;
+  const at::Tensor& q = token_rows(a[0], "q", -1, -1, D, &ld_q);
+  const int64_t T = q.size(0), H = q.size(1);
+  const bool keys = a[1] != Py_None;
+  if (!keys && a[7] != Py_None) fail(PyExc_ValueError, "k_out is given without k");
+  const at::Tensor& k = keys ? token_rows(a[1], "k", T, -1, D, &ld_k) : q;
+  const int64_t Hkv = keys ? k.size(1) : 0;
+  if (keys) same_device(k, "k", q, "q");
+  if (H < 1 || H > 8192 || Hkv > 8192 || D > 8192) fail(PyExc_ValueError, "q and k must have 1 to 8192 heads");
+  const at::Tensor& positions = tensor_of(a[2], "positions", at::kInt, {T});
+  same_device(positions, "positions", q, "q");
+  const at::Tensor& f = frequencies(a[3], D, q, "q");
+  RowsOut q_out(a[6], "q_out", T, H, D, q, "q"), k_out(keys ? a[7] : a[0], "k_out", T, keys ? Hkv : H, D, q, "q");
+  allocate(q_out.out, k_out.out);
+  call("dptq_rotary", q, dptq_rotary, ptr(q), ld_q, (int32_t)H, keys ? ptr(k) : nullptr, ld_k, (int32_t)Hkv, T,
+       (int32_t)D, ptr<int32_t>(positions), ptr<double>(f), (int32_t)(2 * f.size(0)), (int32_t)truth(a[4]),
+       (float)real(a[5]), q_out.out.ptr(), q_out.ld, keys ? k_out.out.ptr() : nullptr, k_out.ld);
+  if (keys) return tuple(q_out.out, k_out.out);
+  PyObject* r = PyTuple_Pack(2, q_out.out.o, Py_None);
+  if (!r) throw Raised{};
+  return r;
+}
+
+// rotary_kv8_append(q, k, v, cu_seqlens, lengths, page_table, k_pages, v_pages, k_scales, v_scales, inv_freq,
+//                   interleaved, scale, max_new, q_out)
+PyObject* rotary_kv8_append(PyObject* const* a) {
+  const Cache c = cache_args(a + 3);
+  int64_t ld_q, ld_k, ld_v;
+  const at::Tensor& q = token_rows(a[0], "q", -1, -1, c.D, &ld_q);
+  const int64_t T = q.size(0), H = q.size(1);
+  const at::Tensor& k = token_rows(a[1], "k", T, c.heads, c.D, &ld_k);
+  const at::Tensor& v = token_rows(a[2], "v", T, c.heads, c.D, &ld_v);
+  same_device(q, "q", c.k, "k_pages");
+  same_device(k, "k", c.k, "k_pages");
+  same_device(v, "v", c.k, "k_pages");
+  if (H < 1 || H > 8192 || c.heads > 8192) fail(PyExc_ValueError, "q must have 1 to 8192 heads");
+  const at::Tensor& f = frequencies(a[10], c.D, q, "q");
+  const int64_t max_new = size_hint(a[13], "max_new");
+  RowsOut q_out(a[14], "q_out", T, H, c.D, q, "q");
+  allocate(q_out.out);
+  call("dptq_rotary_kv8_append", q, dptq_rotary_kv8_append, ptr(q), ld_q, (int32_t)H, ptr(k), ld_k, ptr(v), ld_v, T,
+       ptr<int32_t>(c.cu), ptr<int32_t>(c.lengths), c.B, ptr<int32_t>(c.table), c.max_pages, c.pages,
+       (int32_t)c.heads, (int32_t)c.D, ptr<uint8_t>(c.k), ptr<uint8_t>(c.v), ptr<float>(c.ks), ptr<float>(c.vs),
+       ptr<double>(f), (int32_t)(2 * f.size(0)), (int32_t)truth(a[11]), (float)real(a[12]), q_out.out.ptr(), q_out.ld,
+       max_new);
+  return q_out.out.release();
+}
+
 // kv8_attention(q, cu_seqlens, lengths, page_table, k_pages, v_pages, k_scales, v_scales, max_q, max_len, scale,
 //               window, sinks, out, lse)
 PyObject* kv8_attention(PyObject* const* a) {
@@ -712,6 +807,8 @@ PyMethodDef kMethods[] = {
     DPTQ_ENTRY(rms_norm_quant, 7),
     DPTQ_ENTRY(kv8_append, 10),
     DPTQ_ENTRY(kv8_attention, 15),
+    DPTQ_ENTRY(rotary, 8),
+    DPTQ_ENTRY(rotary_kv8_append, 15),
     DPTQ_ENTRY(token_logprobs, 7),
     {nullptr, nullptr, 0, nullptr},
 };
