@@ -699,6 +699,7 @@ int dptq_qlinear_fp6(const uint8_t* a_fp6, const float* a_scales, int64_t M, int
 
 /* Device-native weight layouts of dptq_prepack_weights. */
 typedef enum {
+  DPTQ_WEIGHTS_PACKED = 0,  /* the dptq_qlinear layout as it is (dptq_qlinear_gated) */
   DPTQ_WEIGHTS_FP6 = 1,     /* FP6 block layout: the 4-bit layers on dptq_qlinear_fp6 */
   DPTQ_WEIGHTS_A8_ORDER = 2, /* 8-bit activation order: the 8-bit layers on dptq_qlinear_a8 */
   DPTQ_WEIGHTS_DECODE = 3    /* decode layout: any layer's M <= 16 GEMM on
@@ -756,6 +757,49 @@ int dptq_prepack_weights(const uint8_t* w_packed, int64_t N, int64_t K, int32_t 
 int dptq_qlinear_decode_native(const void* codes, const float* a_scales, int64_t M, int64_t K,
                                int32_t bits, const uint8_t* w_dec, const float* w_scales,
                                int64_t N, void* y, int32_t* acc, void* stream);
+
+/* Activations of a gated feed-forward block. */
+typedef enum {
+  DPTQ_GATE_SILU = 0,      /* g / (1 + exp(-g)) */
+  DPTQ_GATE_GELU_TANH = 1  /* g / 2 * (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) */
+} dptq_gate_activation;
+
+/*
+ * dptq_qlinear_gated - both projections of a gated feed-forward block, its
+ * activation and the product, in one launch:
+ *
+ *   g[m,f] = acc(m, gate channel f) * a_scales[m] * w_scales[gate channel f]   (fp32)
+ *   u[m,f] = the same of the up channel f
+ *   y[m,f] = fl16(act(g[m,f]) * u[m,f])
+ *
+ * with the exact accumulators of dptq_qlinear and g and u not rounded to fp16 in
+ * between.  The weights are one matrix of N = 2 F rows: rows 16 i to 16 i + 7 are
+ * the gate channels 8 i to 8 i + 7, rows 16 i + 8 to 16 i + 15 the up channels 8 i
+ * to 8 i + 7 (fp32 rows put in that order before dptq_prepare_weights, or packed
+ * ones: every layout of dptq_prepack_weights takes them as they are).
+ *
+ *   codes, a_scales, M, K, bits   as for dptq_qlinear
+ *   w         device, the weights in the layout that `weights` names
+ *   weights   DPTQ_WEIGHTS_PACKED (the dptq_qlinear layout), DPTQ_WEIGHTS_A8_ORDER
+ *             (bits 8) or DPTQ_WEIGHTS_DECODE (M <= 16, else
+ *             DPTQ_ERR_UNSUPPORTED)
+ *   w_scales  device, float [2 F], in the order of the rows
+ *   F         channels, a multiple of 8, >= 8; N = 2 F within dptq_qlinear's range
+ *   act       a dptq_gate_activation
+ *   y         device, fp16 [M, F], 16-byte aligned
+ */
+int dptq_qlinear_gated(const void* codes, const float* a_scales, int64_t M, int64_t K, int32_t bits,
+                       const uint8_t* w, int32_t weights, const float* w_scales, int64_t F, int32_t act,
+                       void* y, void* stream);
+
+/*
+ * dptq_qlinear_gated_fp6 - the same at bits 4 on FP6 operands (dptq_qlinear_fp6:
+ * prefill shapes), with the same results bit for bit.  a_fp6 and w_fp6 hold M and
+ * 2 F rows in the FP6 block layout; pointers as for dptq_qlinear_fp6.
+ */
+int dptq_qlinear_gated_fp6(const uint8_t* a_fp6, const float* a_scales, int64_t M, int64_t K,
+                           const uint8_t* w_fp6, const float* w_scales, int64_t F, int32_t act, void* y,
+                           void* stream);
 
 #ifdef __cplusplus
 }

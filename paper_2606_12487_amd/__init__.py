@@ -28,6 +28,8 @@ __all__ = ["DptqError", "lib", "library_path", "rotate_quant", "qlinear", "qline
            "qlinear_decode_native_acc",
            "rms_norm_quant", "KV8Cache", "KV8_PAGE", "kv8_cache", "kv8_append", "kv8_attention",
            "token_logprobs", "MAX_TOP", "rotary", "rotary_inv_freq", "rotary_kv8_append",
+           "gate_up_rows", "qlinear_gated", "qlinear_gated_a8", "qlinear_gated_decode_native", "qlinear_gated_fp6",
+           "WEIGHTS_PACKED",
            "EXPORTED_FUNCTIONS", "GEMM_AUTO",
            "GEMM_DECODE", "GEMM_TILE_256X128", "GEMM_TILE_192X256"]
 
@@ -51,12 +53,13 @@ EXPORTED_FUNCTIONS = ("dptq_status_string", "dptq_version", "dptq_rotate_quant",
                       "dptq_qlinear_decode_native", "dptq_rms_norm_quant", "dptq_kv8_append",
                       "dptq_kv8_attention_workspace", "dptq_kv8_attention",
                       "dptq_token_logprobs_workspace", "dptq_token_logprobs", "dptq_rotary",
-                      "dptq_rotary_kv8_append")
+                      "dptq_rotary_kv8_append", "dptq_qlinear_gated", "dptq_qlinear_gated_fp6")
 
 # Code layouts of dptq_rotate_quant_ex.
 LAYOUT_PACKED, LAYOUT_FP6 = 0, 1
 
-# Device-native weight layouts of dptq_prepack_weights.
+# Weight layouts: dptq_qlinear's, and the device-native ones of dptq_prepack_weights.
+WEIGHTS_PACKED = 0
 WEIGHTS_FP6, WEIGHTS_A8_ORDER, WEIGHTS_DECODE = 1, 2, 3
 
 # GEMM kernels (dptq_gemm_kernel); every kernel returns the same bits.
@@ -117,6 +120,10 @@ def lib():
         L.dptq_kv8_attention.argtypes = [vp, i64, i64, vp, vp, i64, vp, i64, i64, i32, i32, i32, vp, vp, vp, vp,
                                          ctypes.c_float, i32, i32, i64, i64, vp, vp, vp, i64, vp]
         L.dptq_kv8_attention.restype = ctypes.c_int
+        L.dptq_qlinear_gated.argtypes = [vp, vp, i64, i64, i32, vp, i32, vp, i64, i32, vp, vp]
+        L.dptq_qlinear_gated.restype = ctypes.c_int
+        L.dptq_qlinear_gated_fp6.argtypes = [vp, vp, i64, i64, vp, vp, i64, i32, vp, vp]
+        L.dptq_qlinear_gated_fp6.restype = ctypes.c_int
         L.dptq_rotary.argtypes = [vp, i64, i32, vp, i64, i32, i64, i32, vp, vp, i32, i32, ctypes.c_float, vp, i64, vp,
                                   i64, vp]
         L.dptq_rotary.restype = ctypes.c_int
@@ -508,6 +515,40 @@ def qlinear_decode_fused(x, had_size, bits, w_packed, w_scales, y=None, codes=No
     """Decode-shape (M <= 16) rotate + quantize + GEMM from fp16 x: one launch
     or two (mode, DECODE_AUTO picks).  Returns (y [M, N] fp16, codes, scales)."""
     return _binding().qlinear_decode_fused(x, had_size, bits, w_packed, w_scales, y, codes, scales, mode)
+
+
+def gate_up_rows(gate, up):
+    """The weights of a gated block as one matrix: rows [F, K] of the gate and of the up projection -> [2 F, K], eight
+    of each in turn (F a multiple of 8).  For fp32 rows before prepare_weights, packed rows, or scales [F]."""
+    torch = _torch()
+    if gate.shape != up.shape or gate.dtype != up.dtype or gate.device != up.device:
+        raise ValueError("gate and up must be alike in shape, dtype and device")
+    if gate.dim() < 1 or gate.shape[0] < 8 or gate.shape[0] % 8:
+        raise ValueError("the channels must be a positive multiple of 8")
+    return torch.stack((gate.unflatten(0, (-1, 8)), up.unflatten(0, (-1, 8))), 1).flatten(0, 2)
+
+
+def qlinear_gated(codes, a_scales, bits, w_packed, w_scales, y=None, activation="silu"):
+    """A gated feed-forward block up to its last projection, in one launch: y [M, F] fp16 = act(g) * u with g and u the
+    dequantized products of the gate's and the up projection's channels, in fp32.  w_packed [2 F, K/2] and w_scales
+    [2 F]: prepare_weights of gate_up_rows(gate, up).  activation: "silu" or "gelu_tanh"."""
+    return _binding().qlinear_gated(codes, a_scales, bits, w_packed, w_scales, y, activation)
+
+
+def qlinear_gated_a8(codes, a_scales, w_a8, w_scales, y=None, activation="silu"):
+    """qlinear_gated at 8 bits against weights from pack_w4_a8: the same y bit for bit."""
+    return _binding().qlinear_gated_a8(codes, a_scales, w_a8, w_scales, y, activation)
+
+
+def qlinear_gated_decode_native(codes, a_scales, bits, w_dec, w_scales, y=None, activation="silu"):
+    """qlinear_gated for M <= 16 tokens on weights from prepack_weights(w, WEIGHTS_DECODE): the same y bit for bit."""
+    return _binding().qlinear_gated_decode_native(codes, a_scales, bits, w_dec, w_scales, y, activation)
+
+
+def qlinear_gated_fp6(a6, a_scales, w6, w_scales, M, K, F, y=None, activation="silu"):
+    """qlinear_gated at 4 bits on operands in the FP6 block layout (M rows of activations, 2 F of weights): the same y
+    bit for bit."""
+    return _binding().qlinear_gated_fp6(a6, a_scales, w6, w_scales, M, K, F, y, activation)
 
 
 def rotate_quant_range(x, had_size, bits, codes=None, scales=None, zeros=None):

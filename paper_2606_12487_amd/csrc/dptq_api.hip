@@ -114,6 +114,23 @@ int attention_shape(int64_t T, int64_t B, int64_t max_pages, int64_t num_pages, 
   return DPTQ_OK;
 }
 
+// The gated epilogue of an activation: sigmoid's argument is g (c1 + c2 g^2), in
+// powers of two.
+bool gate_of(int32_t act, dptq::Gate* gate) {
+  constexpr double kLog2e = 1.4426950408889634, kC1 = 1.5957691216057308;   // 2 sqrt(2 / pi)
+  if (act == DPTQ_GATE_SILU) *gate = dptq::Gate{(float)-kLog2e, 0.0f};
+  else if (act == DPTQ_GATE_GELU_TANH) *gate = dptq::Gate{(float)(-kLog2e * kC1), (float)(-kLog2e * kC1 * 0.044715)};
+  else return false;
+  return true;
+}
+
+// Sizes of a gated block: those of dptq_qlinear with 2 F rows of weights.
+int check_gated_shape(int64_t M, int64_t K, int32_t bits, int64_t F) {
+  if (F < 1 || F % 8 != 0) return DPTQ_ERR_INVALID_ARG;
+  if (F > 0x3FFFFFF8) return DPTQ_ERR_UNSUPPORTED;
+  return check_gemm_shape(M, K, bits, 2 * F);
+}
+
 // What rotary positions add to the check of a call.
 int check_rotary(int32_t heads, int32_t kv_heads, int32_t head_dim, int32_t rotary_dim, float scale) {
   if (heads < 1 || kv_heads < 0 || head_dim < 1 || head_dim % 8 != 0) return DPTQ_ERR_INVALID_ARG;
@@ -411,6 +428,44 @@ int dptq_qlinear_fp6(const uint8_t* a_fp6, const float* a_scales, int64_t M, int
   return from_hip(dptq::launch_qlinear_fp6(a_fp6, y ? a_scales : nullptr, M, (int)K, w_fp6,
                                            y ? w_scales : nullptr, N, y, y ? nullptr : acc,
                                            static_cast<hipStream_t>(stream)));
+}
+
+int dptq_qlinear_gated(const void* codes, const float* a_scales, int64_t M, int64_t K, int32_t bits,
+                       const uint8_t* w, int32_t weights, const float* w_scales, int64_t F, int32_t act,
+                       void* y, void* stream) {
+  const int st = check_gated_shape(M, K, bits, F);
+  if (st != DPTQ_OK) return st;
+  dptq::Gate gate{};
+  if (!gate_of(act, &gate)) return DPTQ_ERR_INVALID_ARG;
+  if (weights != DPTQ_WEIGHTS_PACKED && weights != DPTQ_WEIGHTS_A8_ORDER && weights != DPTQ_WEIGHTS_DECODE)
+    return DPTQ_ERR_INVALID_ARG;
+  if (weights == DPTQ_WEIGHTS_A8_ORDER && bits != 8) return DPTQ_ERR_INVALID_ARG;
+  if (weights == DPTQ_WEIGHTS_DECODE && M > 16) return DPTQ_ERR_UNSUPPORTED;
+  if (M == 0) return DPTQ_OK;
+  if (!codes || !a_scales || !w || !w_scales || !y) return DPTQ_ERR_INVALID_ARG;
+  if (!aligned16(codes) || !aligned16(a_scales) || !aligned16(w) || !aligned16(w_scales) || !aligned16(y))
+    return DPTQ_ERR_INVALID_ARG;
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  if (weights == DPTQ_WEIGHTS_DECODE)
+    return from_hip(dptq::launch_qlinear_decode_native(codes, a_scales, M, (int)K, bits, w, w_scales, 2 * F, y, nullptr,
+                                                       s, &gate));
+  return from_hip(dptq::launch_qlinear_gated(codes, a_scales, M, (int)K, bits, w, w_scales, 2 * F, y, weights, gate, s));
+}
+
+int dptq_qlinear_gated_fp6(const uint8_t* a_fp6, const float* a_scales, int64_t M, int64_t K,
+                           const uint8_t* w_fp6, const float* w_scales, int64_t F, int32_t act, void* y,
+                           void* stream) {
+  const int st = check_gated_shape(M, K, 4, F);
+  if (st != DPTQ_OK) return st;
+  dptq::Gate gate{};
+  if (!gate_of(act, &gate)) return DPTQ_ERR_INVALID_ARG;
+  if (((M + 255) / 256) * ((2 * F + 191) / 192) > 0x7FFFFFFF) return DPTQ_ERR_UNSUPPORTED;
+  if (M == 0) return DPTQ_OK;
+  if (!a_fp6 || !a_scales || !w_fp6 || !w_scales || !y) return DPTQ_ERR_INVALID_ARG;
+  if (!aligned16(a_fp6) || !aligned16(w_fp6) || !aligned4(a_scales) || !aligned4(w_scales) || !aligned16(y))
+    return DPTQ_ERR_INVALID_ARG;
+  return from_hip(dptq::launch_qlinear_fp6(a_fp6, a_scales, M, (int)K, w_fp6, w_scales, 2 * F, y, nullptr,
+                                           static_cast<hipStream_t>(stream), &gate));
 }
 
 int dptq_qlinear_decode_fused(const void* x, int64_t M, int64_t K, int32_t had_size,

@@ -5,6 +5,7 @@
 #include <hip/hip_fp16.h>
 #include <stdint.h>
 
+#include "gate_device.h"
 #include "gemm_rules.h"
 
 namespace dptq {
@@ -126,6 +127,7 @@ struct KsplitCall {
   const int32_t* a_zeros;
   const int32_t* w_sums;
   int cus;   // compute units
+  const Gate* gate;   // gated epilogue: y is [M, N / 2]; nullptr: none
 };
 // Weight layouts: canonical nibbles (any output), the 8-bit activation order
 // (bits 8, y), the decode layout (M <= 16, y or acc).
@@ -143,6 +145,11 @@ hipError_t launch_qlinear(const void* codes, const float* a_scales, int64_t M,
                           int K, int bits, const uint8_t* w_packed,
                           const float* w_scales, int64_t N, void* y,
                           int32_t* out_acc, int kernel, hipStream_t stream);
+// The gated epilogue (gate_device.h) on the kernel that launch_qlinear chooses:
+// y [M, N / 2].  weights: kWeightsCanonical or kWeightsA8Order (bits 8).
+hipError_t launch_qlinear_gated(const void* codes, const float* a_scales, int64_t M, int K, int bits,
+                                const uint8_t* w, const float* w_scales, int64_t N, void* y, int weights,
+                                const Gate& gate, hipStream_t stream);
 
 // 4-bit weights [N, K/2] in the canonical nibble order -> the 8-bit
 // activation order (per dword: k0..k3 in the low nibbles, k4..k7 in the high
@@ -159,7 +166,8 @@ hipError_t launch_pack_decode(const uint8_t* w_packed, int64_t N, int K, uint8_t
 // out_acc != nullptr, against weights in the decode layout.
 hipError_t launch_qlinear_decode_native(const void* codes, const float* a_scales, int64_t M, int K,
                                         int bits, const uint8_t* w_dec, const float* w_scales,
-                                        int64_t N, void* y, int32_t* out_acc, hipStream_t stream);
+                                        int64_t N, void* y, int32_t* out_acc, hipStream_t stream,
+                                        const Gate* gate = nullptr);
 // W4A8 GEMM + epilogue against weights in the 8-bit activation order; the
 // kernel choice as for launch_qlinear.
 hipError_t launch_qlinear_a8(const void* codes, const float* a_scales, int64_t M, int K,
@@ -211,10 +219,12 @@ hipError_t launch_pack_fp6(const uint8_t* codes, int64_t R, int K, uint8_t* out,
 // out_acc != nullptr selects the raw int32 accumulator output.
 hipError_t launch_qlinear_fp6(const uint8_t* a6, const float* a_scales, int64_t M, int K,
                               const uint8_t* w6, const float* w_scales, int64_t N, void* y,
-                              int32_t* out_acc, hipStream_t stream);
+                              int32_t* out_acc, hipStream_t stream,
+                              const Gate* gate = nullptr);
 // Its kernel for medium batches (qgemm_fp6_ksplit.hip), on a tile of gemm_rules.h.
 hipError_t launch_fp6_ksplit(int tile, const uint8_t* a6, const float* a_scales, int64_t M, int K,
                              const uint8_t* w6, const float* w_scales, int64_t N, void* y, int32_t* acc,
-                             hipStream_t stream);
+                             hipStream_t stream,
+                             const Gate* gate = nullptr);
 
 }  // namespace dptq

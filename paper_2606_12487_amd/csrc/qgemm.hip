@@ -111,13 +111,13 @@ template <int BITS> using PrefillCfg = Cfg<BITS, 256, 128, 4, 2>;
 // ZP (the prefill kernels and the decode kernel alike): the range quantizer's
 // zero-point correction acc + (2^(BITS-1) - a_zeros[m]) * w_sums[n], exact in
 // int32, before the dequantization.
-template <class C, bool ACC_OUT, bool WA8 = false, bool ZP = false>
+template <class C, bool ACC_OUT, bool WA8 = false, bool ZP = false, bool GATED = false>
 __global__ void __launch_bounds__(C::kThreads)
 qgemm_prefill(const uint8_t* __restrict__ a_codes, const float* __restrict__ a_scales,
               const uint8_t* __restrict__ w_packed, const float* __restrict__ w_scales,
               int M, int N, int K, __half* __restrict__ y, int32_t* __restrict__ acc_out,
               const int32_t* __restrict__ a_zeros = nullptr,
-              const int32_t* __restrict__ w_sums = nullptr) {
+              const int32_t* __restrict__ w_sums = nullptr, Gate gate = Gate{}) {
   constexpr int BITS = C::kBits, kBN = C::kBN, kBM = C::kBM, kWN = C::kWN;
   constexpr int kTI = C::kTI, kTJ = C::kTJ, kWaves = C::kWaves, kThreads = C::kThreads;
   __shared__ __attribute__((aligned(1024))) uint8_t smem[C::kLds];
@@ -398,6 +398,20 @@ qgemm_prefill(const uint8_t* __restrict__ a_codes, const float* __restrict__ a_s
     const int off = ZP ? (1 << (BITS - 1)) - a_zeros[min(m0 + ml, M - 1)] : 0;
 #pragma unroll
     for (int i = 0; i < kTI; ++i) {
+      if constexpr (GATED) {
+        // The tile's rows hold half as many channels.
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+          const int nl = wn * kTI * 32 + i * 32 + 16 * p + 4 * fg;
+          const auto& c = acc[i][j];
+          *reinterpret_cast<uint2*>(smem + ml * C::kOutStride + nl + 4 * fg) =
+              gated4i<BITS>(v4i{c[8 * p], c[8 * p + 1], c[8 * p + 2], c[8 * p + 3]},
+                            v4i{c[8 * p + 4], c[8 * p + 5], c[8 * p + 6], c[8 * p + 7]}, as,
+                            *reinterpret_cast<const float4*>(w_scales + min(n0 + nl, N - 4)),
+                            *reinterpret_cast<const float4*>(w_scales + min(n0 + nl + 8, N - 4)), gate);
+        }
+        continue;
+      }
 #pragma unroll
       for (int b = 0; b < 4; ++b) {
         const int nl = wn * kTI * 32 + i * 32 + 8 * b + 4 * fg;
@@ -410,14 +424,15 @@ qgemm_prefill(const uint8_t* __restrict__ a_codes, const float* __restrict__ a_s
     }
   }
   lds_barrier();
-  // Rows of BN halves = BN / 8 16-byte chunks.
-  constexpr int kRowChunks = kBN / 8;
+  // Rows of BN halves = BN / 8 16-byte chunks (gated: half of that).
+  constexpr int kRowChunks = kBN / (GATED ? 16 : 8);
+  const int cols = GATED ? N / 2 : N, first = GATED ? n0 / 2 : n0;
   for (int idx = t; idx < kBM * kRowChunks; idx += kThreads) {
     const int ml = idx / kRowChunks, cc = idx - ml * kRowChunks;
-    const int m = m0 + ml, n = n0 + cc * 8;
-    if (m >= M || n >= N) continue;
+    const int m = m0 + ml, n = first + cc * 8;
+    if (m >= M || n >= cols) continue;
     const uint4 v = *reinterpret_cast<const uint4*>(smem + ml * C::kOutStride + cc * 16);
-    *reinterpret_cast<uint4*>(y + (size_t)m * N + n) = v;
+    *reinterpret_cast<uint4*>(y + (size_t)m * cols + n) = v;
   }
 }
 
@@ -492,13 +507,13 @@ __device__ __forceinline__ void sched_step() {
   }
 }
 
-template <int BITS, bool ACC_OUT, bool WA8 = false, bool ZP = false>
+template <int BITS, bool ACC_OUT, bool WA8 = false, bool ZP = false, bool GATED = false>
 __global__ void __launch_bounds__(256)
 qgemm_prefill_wide(const uint8_t* __restrict__ a_codes, const float* __restrict__ a_scales,
                    const uint8_t* __restrict__ w_packed, const float* __restrict__ w_scales,
                    int M, int N, int K, __half* __restrict__ y, int32_t* __restrict__ acc_out,
                    const int32_t* __restrict__ a_zeros = nullptr,
-                   const int32_t* __restrict__ w_sums = nullptr) {
+                   const int32_t* __restrict__ w_sums = nullptr, Gate gate = Gate{}) {
   using C = Wide<BITS>;
   constexpr int kTI = C::kTI, kTJ = C::kTJ, kB = C::kBufs;
   __shared__ __attribute__((aligned(1024))) uint8_t smem[C::kLds];
@@ -715,6 +730,26 @@ qgemm_prefill_wide(const uint8_t* __restrict__ a_codes, const float* __restrict_
       const int off = ZP ? (1 << (BITS - 1)) - a_zeros[m] : 0;
 #pragma unroll
       for (int i = 0; i < kTI; ++i) {
+        if constexpr (GATED) {
+          // Registers 8p .. 8p + 3 are the gate's rows, the next four up's: lane l
+          // holds channels 8p + 4 g + 0..3, and the swap joins eight of them.
+          uint2 x[2];
+#pragma unroll
+          for (int p = 0; p < 2; ++p) {
+            const int nl = nbase + i * 32 + 16 * p + 4 * fg;
+            const auto& c = acc[i][j];
+            x[p] = gated4i<BITS>(v4i{c[8 * p], c[8 * p + 1], c[8 * p + 2], c[8 * p + 3]},
+                                 v4i{c[8 * p + 4], c[8 * p + 5], c[8 * p + 6], c[8 * p + 7]}, as,
+                                 *reinterpret_cast<const float4*>(sc + 256 + nl),
+                                 *reinterpret_cast<const float4*>(sc + 256 + nl + 8), gate);
+          }
+          const auto s0 = __builtin_amdgcn_permlane32_swap(x[0].x, x[1].x, false, false);
+          const auto s1 = __builtin_amdgcn_permlane32_swap(x[0].y, x[1].y, false, false);
+          *reinterpret_cast<uint4*>(y + (size_t)m * (N / 2) + (n0 + nbase + i * 32) / 2 + 8 * fg) =
+              make_uint4(s0[0], s1[0], s0[1], s1[1]);
+          __builtin_amdgcn_sched_barrier(0);
+          continue;
+        }
 #pragma unroll
         for (int p = 0; p < 2; ++p) {
           const int nl = nbase + i * 32 + 16 * p + 4 * fg;
@@ -896,24 +931,24 @@ pack_w4_a8_kernel(const uint32_t* __restrict__ w, int64_t ndw, uint32_t* __restr
   out[i] = o;
 }
 
-template <class C, bool ACC_OUT, bool WA8, bool ZP>
+template <class C, bool ACC_OUT, bool WA8, bool ZP, bool GATED>
 void launch_prefill(const uint8_t* a, const float* as, int64_t M, int K, const uint8_t* w,
                     const float* ws, int64_t N, __half* y, int32_t* acc, const int32_t* az,
-                    const int32_t* wsum, hipStream_t stream) {
+                    const int32_t* wsum, const Gate& gate, hipStream_t stream) {
   const int64_t tiles = ((M + C::kBM - 1) / C::kBM) * ((N + C::kBN - 1) / C::kBN);
-  hipLaunchKernelGGL((qgemm_prefill<C, ACC_OUT, WA8, ZP>), dim3((unsigned)tiles), dim3(C::kThreads), 0,
-                     stream, a, as, w, ws, (int)M, (int)N, K, y, acc, az, wsum);
+  hipLaunchKernelGGL((qgemm_prefill<C, ACC_OUT, WA8, ZP, GATED>), dim3((unsigned)tiles), dim3(C::kThreads), 0,
+                     stream, a, as, w, ws, (int)M, (int)N, K, y, acc, az, wsum, gate);
 }
 
-template <int BITS, bool ACC_OUT, bool WA8, bool ZP>
+template <int BITS, bool ACC_OUT, bool WA8, bool ZP, bool GATED>
 void launch_wide(const uint8_t* a, const float* as, int64_t M, int K, const uint8_t* w,
                  const float* ws, int64_t N, __half* y, int32_t* acc, const int32_t* az,
-                 const int32_t* wsum, int cus, hipStream_t stream) {
+                 const int32_t* wsum, int cus, const Gate& gate, hipStream_t stream) {
   using C = Wide<BITS>;
   const int64_t tiles = ((M + C::kBM - 1) / C::kBM) * ((N + C::kBN - 1) / C::kBN);
   const int64_t grid = tiles < cus ? tiles : cus;
-  hipLaunchKernelGGL((qgemm_prefill_wide<BITS, ACC_OUT, WA8, ZP>), dim3((unsigned)grid), dim3(C::kThreads),
-                     0, stream, a, as, w, ws, (int)M, (int)N, K, y, acc, az, wsum);
+  hipLaunchKernelGGL((qgemm_prefill_wide<BITS, ACC_OUT, WA8, ZP, GATED>), dim3((unsigned)grid),
+                     dim3(C::kThreads), 0, stream, a, as, w, ws, (int)M, (int)N, K, y, acc, az, wsum, gate);
 }
 
 static_assert(Wide<4>::kMinK == rules::wide_min_k(4) && Wide<8>::kMinK == rules::wide_min_k(8) &&
@@ -922,11 +957,11 @@ static_assert(Wide<4>::kMinK == rules::wide_min_k(4) && Wide<8>::kMinK == rules:
                   PrefillCfg<8>::kBM == rules::kTileM && PrefillCfg<8>::kBN == rules::kTileN,
               "the dispatch rules are for these tiles");
 
-template <int BITS, bool ACC_OUT, bool WA8 = false, bool ZP = false>
+template <int BITS, bool ACC_OUT, bool WA8 = false, bool ZP = false, bool GATED = false>
 hipError_t launch_t(const uint8_t* a, const float* as, int64_t M, int K,
                     const uint8_t* w, const float* ws, int64_t N, __half* y,
                     int32_t* acc, int kernel, hipStream_t stream,
-                    const int32_t* az = nullptr, const int32_t* wsum = nullptr) {
+                    const int32_t* az = nullptr, const int32_t* wsum = nullptr, const Gate& gate = Gate{}) {
   if (M == 0) return hipSuccess;
   const int cus = device_cus();
   const rules::GemmRoute c = kernel == kGemmAuto ? rules::gemm_route(M, N, K, BITS, cus) : rules::GemmRoute{kernel, -1};
@@ -934,13 +969,13 @@ hipError_t launch_t(const uint8_t* a, const float* as, int64_t M, int K,
     case kGemmDecode:
     case kGemmKsplit:
       return launch_ksplit(KsplitCall{a, as, M, K, w, ws, N, ACC_OUT ? nullptr : y, ACC_OUT ? acc : nullptr,
-                                      az, wsum, cus},
+                                      az, wsum, cus, GATED ? &gate : nullptr},
                            BITS, WA8 ? kWeightsA8Order : kWeightsCanonical, c.tile, stream);
     case kGemmWide:
-      launch_wide<BITS, ACC_OUT, WA8, ZP>(a, as, M, K, w, ws, N, y, acc, az, wsum, cus, stream);
+      launch_wide<BITS, ACC_OUT, WA8, ZP, GATED>(a, as, M, K, w, ws, N, y, acc, az, wsum, cus, gate, stream);
       break;
     default:
-      launch_prefill<PrefillCfg<BITS>, ACC_OUT, WA8, ZP>(a, as, M, K, w, ws, N, y, acc, az, wsum, stream);
+      launch_prefill<PrefillCfg<BITS>, ACC_OUT, WA8, ZP, GATED>(a, as, M, K, w, ws, N, y, acc, az, wsum, gate, stream);
       break;
   }
   return hipGetLastError();
@@ -1004,6 +1039,21 @@ hipError_t launch_qlinear(const void* codes, const float* a_scales, int64_t M, i
   return launch_t<8, false>(a, a_scales, M, K, w_packed, w_scales, N, yh, nullptr, kernel, stream);
 }
 
+hipError_t launch_qlinear_gated(const void* codes, const float* a_scales, int64_t M, int K, int bits,
+                                const uint8_t* w, const float* w_scales, int64_t N, void* y, int weights,
+                                const Gate& gate, hipStream_t stream) {
+  const uint8_t* a = static_cast<const uint8_t*>(codes);
+  __half* yh = static_cast<__half*>(y);
+  if (weights == kWeightsA8Order)
+    return launch_t<8, false, true, false, true>(a, a_scales, M, K, w, w_scales, N, yh, nullptr, kGemmAuto, stream,
+                                                 nullptr, nullptr, gate);
+  if (bits == 4)
+    return launch_t<4, false, false, false, true>(a, a_scales, M, K, w, w_scales, N, yh, nullptr, kGemmAuto, stream,
+                                                  nullptr, nullptr, gate);
+  return launch_t<8, false, false, false, true>(a, a_scales, M, K, w, w_scales, N, yh, nullptr, kGemmAuto, stream,
+                                                nullptr, nullptr, gate);
+}
+
 hipError_t launch_pack_w4_a8(const uint8_t* w_packed, int64_t N, int K, uint8_t* out,
                              hipStream_t stream) {
   const int64_t ndw = N * (K / 8);
@@ -1025,9 +1075,10 @@ hipError_t launch_pack_decode(const uint8_t* w_packed, int64_t N, int K, uint8_t
 
 hipError_t launch_qlinear_decode_native(const void* codes, const float* a_scales, int64_t M, int K,
                                         int bits, const uint8_t* w_dec, const float* w_scales,
-                                        int64_t N, void* y, int32_t* out_acc, hipStream_t stream) {
+                                        int64_t N, void* y, int32_t* out_acc, hipStream_t stream,
+                                        const Gate* gate) {
   return launch_ksplit(KsplitCall{static_cast<const uint8_t*>(codes), a_scales, M, K, w_dec, w_scales, N,
-                                  static_cast<__half*>(y), out_acc, nullptr, nullptr, device_cus()},
+                                  static_cast<__half*>(y), out_acc, nullptr, nullptr, device_cus(), gate},
                        bits, kWeightsDecode, -1, stream);
 }
 

@@ -30,15 +30,15 @@ constexpr int kDecBatch = 4;
 // acc + (2^(BITS-1) - a_zeros[m]) * w_sums[n] (exact int32), before the
 // dequantization.  WDEC: weights in the decode layout, where the 16 rows x 64
 // bytes of a block's 128-k chunk are one contiguous KiB in lane order.
-// BATCH: chunks per wavefront in flight.
+// BATCH: chunks per wavefront in flight.  GATED: gate_device.h.
 template <int BITS, bool ACC_OUT, bool ZP = false, bool WA8 = false, int NB = 1, bool WDEC = false,
-          int BATCH = kDecBatch>
+          int BATCH = kDecBatch, bool GATED = false>
 __global__ void __launch_bounds__(kDecWaves * 64)
 qgemm_decode(const uint8_t* __restrict__ a_codes, const float* __restrict__ a_scales,
              const uint8_t* __restrict__ w_packed, const float* __restrict__ w_scales,
              int M, int N, int K, __half* __restrict__ y, int32_t* __restrict__ acc_out,
              const int32_t* __restrict__ a_zeros = nullptr,
-             const int32_t* __restrict__ w_sums = nullptr) {
+             const int32_t* __restrict__ w_sums = nullptr, Gate gate = Gate{}) {
   static_assert(NB == 1 || NB == 2, "blocks per workgroup");
   __shared__ v4i part[NB][kDecWaves][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -102,6 +102,22 @@ qgemm_decode(const uint8_t* __restrict__ a_codes, const float* __restrict__ a_sc
   __syncthreads();
   // Wavefront nb < NB sums and writes block nb.
   if (wave >= NB) return;
+  if constexpr (GATED) {
+    // Lanes 0 to 31 hold the gate's rows, the others the same rows of up.
+    if (lane >= 32 || !mvalid) return;
+    v4i g = part[wave][0][lane], u = part[wave][0][lane + 32];
+#pragma unroll
+    for (int w = 1; w < kDecWaves; ++w) {
+      const v4i p = part[wave][w][lane], q = part[wave][w][lane + 32];
+      g.x += p.x; g.y += p.y; g.z += p.z; g.w += p.w;
+      u.x += q.x; u.y += q.y; u.z += q.z; u.w += q.w;
+    }
+    const int nb = n0 + wave * 16;
+    *reinterpret_cast<uint2*>(y + (size_t)fr * (N / 2) + nb / 2 + fg * 4) =
+        gated4i<BITS>(g, u, a_scales[fr], *reinterpret_cast<const float4*>(w_scales + nb + fg * 4),
+                      *reinterpret_cast<const float4*>(w_scales + nb + 8 + fg * 4), gate);
+    return;
+  }
   v4i tot = part[wave][0][lane];
 #pragma unroll
   for (int w = 1; w < kDecWaves; ++w) {
@@ -134,33 +150,38 @@ qgemm_decode(const uint8_t* __restrict__ a_codes, const float* __restrict__ a_sc
   }
 }
 
-template <int BITS, bool ACC_OUT, bool ZP, bool WA8, bool WDEC, int NB, int BATCH>
+template <int BITS, bool ACC_OUT, bool ZP, bool WA8, bool WDEC, bool GATED, int NB, int BATCH>
 void launch_t(const KsplitCall& c, hipStream_t stream) {
-  hipLaunchKernelGGL((qgemm_decode<BITS, ACC_OUT, ZP, WA8, NB, WDEC, BATCH>), dim3((unsigned)(c.N / (16 * NB))),
+  hipLaunchKernelGGL((qgemm_decode<BITS, ACC_OUT, ZP, WA8, NB, WDEC, BATCH, GATED>), dim3((unsigned)(c.N / (16 * NB))),
                      dim3(kDecWaves * 64), 0, stream, c.a, c.a_scales, c.w, c.w_scales, (int)c.M, (int)c.N, c.K,
-                     c.y, c.acc, c.a_zeros, c.w_sums);
+                     c.y, c.acc, c.a_zeros, c.w_sums, c.gate ? *c.gate : Gate{});
 }
 
-template <int BITS, bool ACC_OUT, bool ZP, bool WA8, bool WDEC>
+template <int BITS, bool ACC_OUT, bool ZP, bool WA8, bool WDEC, bool GATED = false>
 void launch(const KsplitCall& c, hipStream_t stream) {
   const int blocks = rules::decode_blocks(c.M, c.N, BITS, c.cus);
   if (blocks == 2)
-    launch_t<BITS, ACC_OUT, ZP, WA8, WDEC, 2, kDecBatch>(c, stream);
+    launch_t<BITS, ACC_OUT, ZP, WA8, WDEC, GATED, 2, kDecBatch>(c, stream);
   else if (WDEC && rules::decode_batch(c.M, c.N, c.K, blocks, c.cus) == 8)
-    launch_t<BITS, ACC_OUT, ZP, WA8, WDEC, 1, WDEC ? 8 : kDecBatch>(c, stream);
+    launch_t<BITS, ACC_OUT, ZP, WA8, WDEC, GATED, 1, WDEC ? 8 : kDecBatch>(c, stream);
   else
-    launch_t<BITS, ACC_OUT, ZP, WA8, WDEC, 1, kDecBatch>(c, stream);
+    launch_t<BITS, ACC_OUT, ZP, WA8, WDEC, GATED, 1, kDecBatch>(c, stream);
 }
 
 }  // namespace
 
 hipError_t launch_decode_regs(const KsplitCall& c, int bits, int weights, hipStream_t stream) {
-  const bool acc = c.acc != nullptr, zp = c.a_zeros != nullptr;
+  const bool acc = c.acc != nullptr, zp = c.a_zeros != nullptr, gated = c.gate != nullptr;
   if (weights == kWeightsDecode) {
-    if (bits == 4) acc ? launch<4, true, false, false, true>(c, stream) : launch<4, false, false, false, true>(c, stream);
+    if (gated) bits == 4 ? launch<4, false, false, false, true, true>(c, stream)
+                         : launch<8, false, false, false, true, true>(c, stream);
+    else if (bits == 4) acc ? launch<4, true, false, false, true>(c, stream) : launch<4, false, false, false, true>(c, stream);
     else acc ? launch<8, true, false, false, true>(c, stream) : launch<8, false, false, false, true>(c, stream);
   } else if (weights == kWeightsA8Order) {
-    launch<8, false, false, true, false>(c, stream);
+    gated ? launch<8, false, false, true, false, true>(c, stream) : launch<8, false, false, true, false>(c, stream);
+  } else if (gated) {
+    bits == 4 ? launch<4, false, false, false, false, true>(c, stream)
+              : launch<8, false, false, false, false, true>(c, stream);
   } else if (bits == 4) {
     if (acc) launch<4, true, false, false, false>(c, stream);
     else if (zp) launch<4, false, true, false, false>(c, stream);

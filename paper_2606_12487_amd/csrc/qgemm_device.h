@@ -6,6 +6,8 @@
 #include <hip/hip_fp16.h>
 #include <stdint.h>
 
+#include "gate_device.h"
+
 namespace dptq {
 namespace qg {
 
@@ -101,6 +103,16 @@ __device__ __forceinline__ uint2 dequant4z(int a0, int a1, int a2, int a3, float
   pk.x = (uint32_t)__half_as_ushort(h0) | ((uint32_t)__half_as_ushort(h1) << 16);
   pk.y = (uint32_t)__half_as_ushort(h2) | ((uint32_t)__half_as_ushort(h3) << 16);
   return pk;
+}
+
+// The gated epilogue of four gate accumulators and the up channels' four.
+template <int BITS>
+__device__ __forceinline__ uint2 gated4i(v4i g, v4i u, float as, float4 wg, float4 wu, Gate k) {
+  return gated4(make_float4((float)unscale<BITS>(g.x), (float)unscale<BITS>(g.y), (float)unscale<BITS>(g.z),
+                            (float)unscale<BITS>(g.w)),
+                make_float4((float)unscale<BITS>(u.x), (float)unscale<BITS>(u.y), (float)unscale<BITS>(u.z),
+                            (float)unscale<BITS>(u.w)),
+                as, wg, wu, k);
 }
 
 // Logical tile of workgroup bid: the workgroups of one XCD (bid mod 8) take

@@ -166,13 +166,13 @@ constexpr int f6_part_after(int f, int frags, int parts) {
 // one full tile of padded rows each way and three stages per tile) shift edge
 // tiles inward so every load is a base plus a constant; the CLAMP variant
 // (small shapes) clamps each block row instead.
-template <int WV, bool ACC_OUT, bool CLAMP>
+template <int WV, bool ACC_OUT, bool CLAMP, bool GATED>
 __device__ __forceinline__ void qgemm_fp6_body(const uint8_t* __restrict__ a6,
                                                const float* __restrict__ a_scales,
                                                const uint8_t* __restrict__ w6,
                                                const float* __restrict__ w_scales, int M, int N,
                                                int K, __half* __restrict__ y,
-                                               int32_t* __restrict__ acc_out, uint8_t* smem) {
+                                               int32_t* __restrict__ acc_out, Gate gate, uint8_t* smem) {
   using C = F6;
   constexpr int kTI = C::kTI, kTJ = C::kTJ;
   constexpr int WN = WV & 1, WM = WV >> 1;
@@ -382,6 +382,27 @@ __device__ __forceinline__ void qgemm_fp6_body(const uint8_t* __restrict__ a6,
         const int m = m0 + mbase + j * 32;
 #pragma unroll
         for (int i = 0; i < kTI; ++i) {
+          if constexpr (GATED) {
+            // Registers 8p .. 8p + 3 are the gate's rows, the next four up's: lane l
+            // holds channels 8p + 4 g + 0..3, and the swap joins eight of them.
+            uint2 x[2];
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
+              const int nl = nbase + i * 32 + 16 * p + 4 * fg;
+              const auto& c = acc[i][j];
+              x[p] = gated4(make_float4(c[8 * p], c[8 * p + 1], c[8 * p + 2], c[8 * p + 3]),
+                            make_float4(c[8 * p + 4], c[8 * p + 5], c[8 * p + 6], c[8 * p + 7]), as,
+                            *reinterpret_cast<const float4*>(sc + 256 + nl),
+                            *reinterpret_cast<const float4*>(sc + 256 + nl + 8), gate);
+            }
+            const auto s0 = __builtin_amdgcn_permlane32_swap(x[0].x, x[1].x, false, false);
+            const auto s1 = __builtin_amdgcn_permlane32_swap(x[0].y, x[1].y, false, false);
+            const int f = (n0 + nbase + i * 32) / 2 + 8 * fg;
+            if (inside || (m < M && f < N / 2))
+              *reinterpret_cast<uint4*>(y + (size_t)m * (N / 2) + f) = make_uint4(s0[0], s1[0], s0[1], s1[1]);
+            __builtin_amdgcn_sched_barrier(0);
+            continue;
+          }
 #pragma unroll
           for (int p = 0; p < 2; ++p) {
             const int nl = nbase + i * 32 + 16 * p + 4 * fg;
@@ -495,17 +516,17 @@ __device__ __forceinline__ void qgemm_fp6_body(const uint8_t* __restrict__ a6,
   f6_wait_vmcnt<0>();   // the re-issued tail loads land before the LDS is released
 }
 
-template <bool ACC_OUT, bool CLAMP>
+template <bool ACC_OUT, bool CLAMP, bool GATED = false>
 __global__ void __launch_bounds__(256)
 qgemm_fp6(const uint8_t* __restrict__ a6, const float* __restrict__ a_scales,
           const uint8_t* __restrict__ w6, const float* __restrict__ w_scales, int M, int N,
-          int K, __half* __restrict__ y, int32_t* __restrict__ acc_out) {
+          int K, __half* __restrict__ y, int32_t* __restrict__ acc_out, Gate gate) {
   __shared__ __attribute__((aligned(1024))) uint8_t smem[F6::kLds];
   switch (__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) {
-    case 0: qgemm_fp6_body<0, ACC_OUT, CLAMP>(a6, a_scales, w6, w_scales, M, N, K, y, acc_out, smem); break;
-    case 1: qgemm_fp6_body<1, ACC_OUT, CLAMP>(a6, a_scales, w6, w_scales, M, N, K, y, acc_out, smem); break;
-    case 2: qgemm_fp6_body<2, ACC_OUT, CLAMP>(a6, a_scales, w6, w_scales, M, N, K, y, acc_out, smem); break;
-    default: qgemm_fp6_body<3, ACC_OUT, CLAMP>(a6, a_scales, w6, w_scales, M, N, K, y, acc_out, smem); break;
+    case 0: qgemm_fp6_body<0, ACC_OUT, CLAMP, GATED>(a6, a_scales, w6, w_scales, M, N, K, y, acc_out, gate, smem); break;
+    case 1: qgemm_fp6_body<1, ACC_OUT, CLAMP, GATED>(a6, a_scales, w6, w_scales, M, N, K, y, acc_out, gate, smem); break;
+    case 2: qgemm_fp6_body<2, ACC_OUT, CLAMP, GATED>(a6, a_scales, w6, w_scales, M, N, K, y, acc_out, gate, smem); break;
+    default: qgemm_fp6_body<3, ACC_OUT, CLAMP, GATED>(a6, a_scales, w6, w_scales, M, N, K, y, acc_out, gate, smem); break;
   }
 }
 
@@ -524,30 +545,37 @@ hipError_t launch_pack_fp6(const uint8_t* codes, int64_t R, int K, uint8_t* out,
 
 hipError_t launch_qlinear_fp6(const uint8_t* a6, const float* a_scales, int64_t M, int K,
                               const uint8_t* w6, const float* w_scales, int64_t N, void* y,
-                              int32_t* out_acc, hipStream_t stream) {
+                              int32_t* out_acc, hipStream_t stream, const Gate* gate) {
   if (M == 0) return hipSuccess;
   const int cus = device_cus(), tile = rules::fp6_ksplit_or_none(M, N, K, cus);
-  if (tile >= 0) return launch_fp6_ksplit(tile, a6, a_scales, M, K, w6, w_scales, N, y, out_acc, stream);
+  if (tile >= 0) return launch_fp6_ksplit(tile, a6, a_scales, M, K, w6, w_scales, N, y, out_acc, stream, gate);
   const int64_t tiles = ((M + F6::kBM - 1) / F6::kBM) * ((N + F6::kBN - 1) / F6::kBN);
   const int64_t grid = tiles < cus ? tiles : cus;
   // Fast shapes: at least one full tile of padded rows each way and three
   // stages per tile.
   const bool clamp = (M + 31) / 32 < F6::kABlk || (N + 31) / 32 < F6::kWBlk || K < 3 * 128;
   __half* yh = static_cast<__half*>(y);
-  if (out_acc) {
+  if (gate) {
+    if (clamp)
+      hipLaunchKernelGGL((qgemm_fp6<false, true, true>), dim3((unsigned)grid), dim3(256), 0, stream, a6,
+                         a_scales, w6, w_scales, (int)M, (int)N, K, yh, nullptr, *gate);
+    else
+      hipLaunchKernelGGL((qgemm_fp6<false, false, true>), dim3((unsigned)grid), dim3(256), 0, stream, a6,
+                         a_scales, w6, w_scales, (int)M, (int)N, K, yh, nullptr, *gate);
+  } else if (out_acc) {
     if (clamp)
       hipLaunchKernelGGL((qgemm_fp6<true, true>), dim3((unsigned)grid), dim3(256), 0, stream, a6,
-                         a_scales, w6, w_scales, (int)M, (int)N, K, yh, out_acc);
+                         a_scales, w6, w_scales, (int)M, (int)N, K, yh, out_acc, Gate{});
     else
       hipLaunchKernelGGL((qgemm_fp6<true, false>), dim3((unsigned)grid), dim3(256), 0, stream, a6,
-                         a_scales, w6, w_scales, (int)M, (int)N, K, yh, out_acc);
+                         a_scales, w6, w_scales, (int)M, (int)N, K, yh, out_acc, Gate{});
   } else {
     if (clamp)
       hipLaunchKernelGGL((qgemm_fp6<false, true>), dim3((unsigned)grid), dim3(256), 0, stream, a6,
-                         a_scales, w6, w_scales, (int)M, (int)N, K, yh, out_acc);
+                         a_scales, w6, w_scales, (int)M, (int)N, K, yh, out_acc, Gate{});
     else
       hipLaunchKernelGGL((qgemm_fp6<false, false>), dim3((unsigned)grid), dim3(256), 0, stream, a6,
-                         a_scales, w6, w_scales, (int)M, (int)N, K, yh, out_acc);
+                         a_scales, w6, w_scales, (int)M, (int)N, K, yh, out_acc, Gate{});
   }
   return hipGetLastError();
 }

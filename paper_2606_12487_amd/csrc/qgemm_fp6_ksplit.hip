@@ -39,11 +39,11 @@ __device__ __forceinline__ void wait_lgkm0_fence() { asm volatile("s_waitcnt lgk
 
 // A stage is 128 k of the tile: TI weight and TJ activation blocks; each
 // wavefront has BUFS stages of its own.
-template <int TI, int TJ, int WAVES, int BUFS, bool ACC_OUT>
+template <int TI, int TJ, int WAVES, int BUFS, bool ACC_OUT, bool GATED>
 __global__ void __launch_bounds__(WAVES * 64)
 qgemm_fp6_ksplit(const uint8_t* __restrict__ a6, const float* __restrict__ a_scales,
                  const uint8_t* __restrict__ w6, const float* __restrict__ w_scales, int M, int N,
-                 int K, __half* __restrict__ y, int32_t* __restrict__ acc_out) {
+                 int K, __half* __restrict__ y, int32_t* __restrict__ acc_out, Gate gate) {
   constexpr int kLoads = 3 * (TI + TJ);                 // 1 KiB each, per stage
   constexpr int kStage = kLoads * 1024;
   constexpr int kRing = WAVES * BUFS * kStage;
@@ -175,6 +175,11 @@ qgemm_fp6_ksplit(const uint8_t* __restrict__ a6, const float* __restrict__ a_sca
         const v4f_dw v0 = *reinterpret_cast<const v4f_dw*>(w_scales + nb + 4 * fg);
         const v4f_dw v1 = *reinterpret_cast<const v4f_dw*>(w_scales + nb + 8 + 4 * fg);
         const float4 ws0 = make_float4(v0.x, v0.y, v0.z, v0.w), ws1 = make_float4(v1.x, v1.y, v1.z, v1.w);
+        if constexpr (GATED) {   // t0 the gate's rows, t1 up's
+          if (m < M)
+            *reinterpret_cast<uint2*>(y + (size_t)m * (N / 2) + nb / 2 + 4 * fg) = gated4(t0, t1, as, ws0, ws1, gate);
+          continue;
+        }
         const uint2 x0 = f6_dequant4(t0.x, t0.y, t0.z, t0.w, as, ws0);
         const uint2 x1 = f6_dequant4(t1.x, t1.y, t1.z, t1.w, as, ws1);
         const auto s0 = __builtin_amdgcn_permlane32_swap(x0.x, x1.x, false, false);
@@ -187,19 +192,19 @@ qgemm_fp6_ksplit(const uint8_t* __restrict__ a6, const float* __restrict__ a_sca
   }
 }
 
-template <bool ACC_OUT, int I = 0>
+template <bool ACC_OUT, bool GATED, int I = 0>
 void launch_tile(int tile, const uint8_t* a6, const float* a_scales, int64_t M, int K, const uint8_t* w6,
-                 const float* w_scales, int64_t N, __half* y, int32_t* acc, hipStream_t stream) {
+                 const float* w_scales, int64_t N, __half* y, int32_t* acc, const Gate& gate, hipStream_t stream) {
   if constexpr (I < rules::kNumFp6KsplitTiles) {
     if (tile != I) {
-      launch_tile<ACC_OUT, I + 1>(tile, a6, a_scales, M, K, w6, w_scales, N, y, acc, stream);
+      launch_tile<ACC_OUT, GATED, I + 1>(tile, a6, a_scales, M, K, w6, w_scales, N, y, acc, gate, stream);
       return;
     }
     constexpr rules::Fp6KsplitTile t = rules::kFp6KsplitTiles[I];
     const int64_t mblk = (M + 31) / 32, nblk = (N + 31) / 32;
     const int64_t grid = ((mblk + t.tj - 1) / t.tj) * ((nblk + t.ti - 1) / t.ti);
-    hipLaunchKernelGGL((qgemm_fp6_ksplit<t.ti, t.tj, t.waves, t.bufs, ACC_OUT>), dim3((unsigned)grid),
-                       dim3(t.waves * 64), 0, stream, a6, a_scales, w6, w_scales, (int)M, (int)N, K, y, acc);
+    hipLaunchKernelGGL((qgemm_fp6_ksplit<t.ti, t.tj, t.waves, t.bufs, ACC_OUT, GATED>), dim3((unsigned)grid),
+                       dim3(t.waves * 64), 0, stream, a6, a_scales, w6, w_scales, (int)M, (int)N, K, y, acc, gate);
   }
 }
 
@@ -207,10 +212,11 @@ void launch_tile(int tile, const uint8_t* a6, const float* a_scales, int64_t M, 
 
 hipError_t launch_fp6_ksplit(int tile, const uint8_t* a6, const float* a_scales, int64_t M, int K,
                              const uint8_t* w6, const float* w_scales, int64_t N, void* y, int32_t* acc,
-                             hipStream_t stream) {
+                             hipStream_t stream, const Gate* gate) {
   __half* yh = static_cast<__half*>(y);
-  if (acc) launch_tile<true>(tile, a6, a_scales, M, K, w6, w_scales, N, yh, acc, stream);
-  else launch_tile<false>(tile, a6, a_scales, M, K, w6, w_scales, N, yh, nullptr, stream);
+  if (gate) launch_tile<false, true>(tile, a6, a_scales, M, K, w6, w_scales, N, yh, nullptr, *gate, stream);
+  else if (acc) launch_tile<true, false>(tile, a6, a_scales, M, K, w6, w_scales, N, yh, acc, Gate{}, stream);
+  else launch_tile<false, false>(tile, a6, a_scales, M, K, w6, w_scales, N, yh, nullptr, Gate{}, stream);
   return hipGetLastError();
 }
 

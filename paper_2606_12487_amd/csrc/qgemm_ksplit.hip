@@ -59,12 +59,12 @@ __device__ __forceinline__ int swz_byte(int r) { return 2 * ((-(r >> 2)) & 3) + 
 // bits, so a compute unit keeps 64 to 160 KiB on the way, as much as its LDS
 // holds; two or more smaller stages each were no faster (M = 20, K = 14336,
 // N = 4096 at 4 bits: 7.0 us with one, 7.8 us with two).
-template <int BITS, int TI, int TJ, int WAVES, bool ACC_OUT, bool WA8, bool ZP, bool WDEC>
+template <int BITS, int TI, int TJ, int WAVES, bool ACC_OUT, bool WA8, bool ZP, bool WDEC, bool GATED>
 __global__ void __launch_bounds__(WAVES * 64)
 qgemm_ksplit(const uint8_t* __restrict__ a_codes, const float* __restrict__ a_scales,
              const uint8_t* __restrict__ w_packed, const float* __restrict__ w_scales, int M, int N,
              int K, __half* __restrict__ y, int32_t* __restrict__ acc_out,
-             const int32_t* __restrict__ a_zeros, const int32_t* __restrict__ w_sums) {
+             const int32_t* __restrict__ a_zeros, const int32_t* __restrict__ w_sums, Gate gate) {
   constexpr int kAB = BITS == 4 ? 2 : 4;         // KiB of an activation block per stage
   constexpr int kLoads = 2 * TI + kAB * TJ;      // 1 KiB each, per stage
   constexpr int kStage = kLoads * 1024;
@@ -351,6 +351,18 @@ qgemm_ksplit(const uint8_t* __restrict__ a_codes, const float* __restrict__ a_sc
     for (int u = wave; u < (kPairs ? (blocks + 1) / 2 : blocks); u += WAVES) {
       const int g = kPairs ? 2 * u + (lane >> 5) : u;
       const int f = f0 + g, i = f / TJ, j = f - i * TJ;
+      if constexpr (GATED) {
+        // A lane adds four rows of the gate (groups 0 and 1 of four rows) and the
+        // same four of up (groups 2 and 3).
+        const int q = kPairs ? fg & 1 : fg;
+        const int m = m0 + 16 * j + fr, n = n0 + 16 * i;
+        if (q > 1 || g >= blocks || m >= M || n >= N) continue;
+        *reinterpret_cast<uint2*>(y + (size_t)m * (N / 2) + n / 2 + 4 * q) =
+            gated4i<BITS>(total(g, 16 * q + fr), total(g, 16 * q + 32 + fr), a_scales[m],
+                          *reinterpret_cast<const float4*>(w_scales + n + 4 * q),
+                          *reinterpret_cast<const float4*>(w_scales + n + 8 + 4 * q), gate);
+        continue;
+      }
       const int q = kPairs ? (fg & 1) * 2 : fg;           // group of four n
       const int m = m0 + 16 * j + fr, n = n0 + 16 * i + 4 * q;
       if (g >= blocks || m >= M || n >= N) continue;      // whole blocks of n: N is a multiple of 16
@@ -374,37 +386,37 @@ qgemm_ksplit(const uint8_t* __restrict__ a_codes, const float* __restrict__ a_sc
   }
 }
 
-template <int BITS, int TI, int TJ, int WAVES, bool ACC_OUT, bool WA8, bool ZP, bool WDEC>
+template <int BITS, int TI, int TJ, int WAVES, bool ACC_OUT, bool WA8, bool ZP, bool WDEC, bool GATED>
 void launch_cfg(const KsplitCall& c, hipStream_t stream) {
   const int64_t tiles = ((c.M + 16 * TJ - 1) / (16 * TJ)) * ((c.N + 16 * TI - 1) / (16 * TI));
-  hipLaunchKernelGGL((qgemm_ksplit<BITS, TI, TJ, WAVES, ACC_OUT, WA8, ZP, WDEC>), dim3((unsigned)tiles),
+  hipLaunchKernelGGL((qgemm_ksplit<BITS, TI, TJ, WAVES, ACC_OUT, WA8, ZP, WDEC, GATED>), dim3((unsigned)tiles),
                      dim3(WAVES * 64), 0, stream, c.a, c.a_scales, c.w, c.w_scales, (int)c.M, (int)c.N, c.K,
-                     c.y, c.acc, c.a_zeros, c.w_sums);
+                     c.y, c.acc, c.a_zeros, c.w_sums, c.gate ? *c.gate : Gate{});
 }
 
-template <int BITS, bool ACC_OUT, bool WA8, bool ZP, int I = 0>
+template <int BITS, bool ACC_OUT, bool WA8, bool ZP, bool GATED, int I = 0>
 void launch_tile(int tile, const KsplitCall& c, hipStream_t stream) {
   if constexpr (I < rules::ksplit_tiles(BITS)) {
     constexpr rules::KsplitTile t = rules::ksplit_tile(BITS, I);
     if (tile == I)
-      launch_cfg<BITS, t.ti, t.tj, t.waves, ACC_OUT, WA8, ZP, false>(c, stream);
+      launch_cfg<BITS, t.ti, t.tj, t.waves, ACC_OUT, WA8, ZP, false, GATED>(c, stream);
     else
-      launch_tile<BITS, ACC_OUT, WA8, ZP, I + 1>(tile, c, stream);
+      launch_tile<BITS, ACC_OUT, WA8, ZP, GATED, I + 1>(tile, c, stream);
   }
 }
 
-template <int BITS, bool ACC_OUT, bool WA8, bool ZP, bool WDEC>
+template <int BITS, bool ACC_OUT, bool WA8, bool ZP, bool WDEC, bool GATED = false>
 void launch_decode(const KsplitCall& c, hipStream_t stream) {
   const rules::DecodeTile t = rules::decode_tile(c.N, c.cus);
-  if (t.ti == 1) launch_cfg<BITS, 1, 1, 8, ACC_OUT, WA8, ZP, WDEC>(c, stream);
-  else if (t.waves == 4) launch_cfg<BITS, 2, 1, 4, ACC_OUT, WA8, ZP, WDEC>(c, stream);
-  else launch_cfg<BITS, 2, 1, 8, ACC_OUT, WA8, ZP, WDEC>(c, stream);
+  if (t.ti == 1) launch_cfg<BITS, 1, 1, 8, ACC_OUT, WA8, ZP, WDEC, GATED>(c, stream);
+  else if (t.waves == 4) launch_cfg<BITS, 2, 1, 4, ACC_OUT, WA8, ZP, WDEC, GATED>(c, stream);
+  else launch_cfg<BITS, 2, 1, 8, ACC_OUT, WA8, ZP, WDEC, GATED>(c, stream);
 }
 
-template <int BITS, bool ACC_OUT, bool WA8, bool ZP>
+template <int BITS, bool ACC_OUT, bool WA8, bool ZP, bool GATED = false>
 void launch_canonical(const KsplitCall& c, int tile, hipStream_t stream) {
-  if (c.M <= 16) launch_decode<BITS, ACC_OUT, WA8, ZP, false>(c, stream);
-  else launch_tile<BITS, ACC_OUT, WA8, ZP>(tile, c, stream);
+  if (c.M <= 16) launch_decode<BITS, ACC_OUT, WA8, ZP, false, GATED>(c, stream);
+  else launch_tile<BITS, ACC_OUT, WA8, ZP, GATED>(tile, c, stream);
 }
 
 }  // namespace
@@ -414,14 +426,20 @@ hipError_t launch_ksplit(const KsplitCall& c, int bits, int weights, int tile, h
   if (c.M > 16 && tile < 0) return hipErrorInvalidValue;
   if (c.M <= 16 && rules::decode_in_regs(c.M, c.N, c.K, bits, weights == kWeightsDecode, c.cus))
     return launch_decode_regs(c, bits, weights, stream);
-  const bool acc = c.acc != nullptr, zp = c.a_zeros != nullptr;
+  const bool acc = c.acc != nullptr, zp = c.a_zeros != nullptr, gated = c.gate != nullptr;
   if (weights == kWeightsDecode) {
-    if (bits == 4) acc ? launch_decode<4, true, false, false, true>(c, stream)
+    if (gated) bits == 4 ? launch_decode<4, false, false, false, true, true>(c, stream)
+                         : launch_decode<8, false, false, false, true, true>(c, stream);
+    else if (bits == 4) acc ? launch_decode<4, true, false, false, true>(c, stream)
                        : launch_decode<4, false, false, false, true>(c, stream);
     else acc ? launch_decode<8, true, false, false, true>(c, stream)
              : launch_decode<8, false, false, false, true>(c, stream);
   } else if (weights == kWeightsA8Order) {
-    launch_canonical<8, false, true, false>(c, tile, stream);
+    gated ? launch_canonical<8, false, true, false, true>(c, tile, stream)
+          : launch_canonical<8, false, true, false>(c, tile, stream);
+  } else if (gated) {
+    bits == 4 ? launch_canonical<4, false, false, false, true>(c, tile, stream)
+              : launch_canonical<8, false, false, false, true>(c, tile, stream);
   } else if (bits == 4) {
     if (acc) launch_canonical<4, true, false, false>(c, tile, stream);
     else if (zp) launch_canonical<4, false, false, true>(c, tile, stream);

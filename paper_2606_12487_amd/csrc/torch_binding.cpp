@@ -247,6 +247,11 @@ PyObject* tuple(O&... outs) {
   return r;
 }
 
+void same_device(const at::Tensor& t, const char* name, const at::Tensor& x, const char* of) {
+  if (t.device() != x.device())
+    fail(PyExc_ValueError, std::string(name) + " must be on the same device as " + of);
+}
+
 const at::Tensor* signs_of(PyObject* o, int64_t K, const at::Tensor& x) {
   if (o == Py_None) return nullptr;
   const at::Tensor& s = tensor_of(o, "signs", at::kByte, {(K + 7) / 8});
@@ -396,6 +401,81 @@ PyObject* qlinear_fp6(PyObject* const* a) {
   return y.release();
 }
 
+// The activation of a gated block, by its name.
+int32_t gate_activation(PyObject* o) {
+  if (PyUnicode_Check(o)) {
+    if (PyUnicode_CompareWithASCIIString(o, "silu") == 0) return DPTQ_GATE_SILU;
+    if (PyUnicode_CompareWithASCIIString(o, "gelu_tanh") == 0) return DPTQ_GATE_GELU_TANH;
+  }
+  fail(PyExc_ValueError, "activation must be 'silu' or 'gelu_tanh'");
+}
+
+// The channels of a gated block with N rows of weights.
+int64_t gated_channels(int64_t N) {
+  if (N < 16 || N % 16) fail(PyExc_ValueError, "a gated block has 2 F rows of weights, F a multiple of 8");
+  return N / 2;
+}
+
+// On weights in the layout `weights`, [N, K/2] or in the decode layout.
+PyObject* gated(PyObject* o_codes, PyObject* o_as, int32_t bits, PyObject* o_w, int32_t weights, PyObject* o_ws,
+                PyObject* o_y, PyObject* o_act) {
+  const at::Tensor& codes = tensor(o_codes, "codes", code_dtype(bits));
+  const int64_t M = dim(codes, 0), K = dim(codes, 1) * (bits == 4 ? 2 : 1);
+  const at::Tensor& ws = tensor(o_ws, "w_scales", at::kFloat);
+  if (ws.dim() != 1) fail(PyExc_ValueError, "w_scales must be 1-D [2 F]");
+  const int64_t N = ws.size(0), F = gated_channels(N);
+  const int64_t n = weights == DPTQ_WEIGHTS_DECODE ? dptq_prepacked_bytes(N, K, DPTQ_WEIGHTS_DECODE) : 0;
+  if (n < 0) fail(PyExc_ValueError, "K must be a multiple of 128 in the decode layout");
+  const at::Tensor& w = weights == DPTQ_WEIGHTS_DECODE ? tensor_of(o_w, "w_dec", at::kByte, {n})
+                                                       : tensor_of(o_w, "w_packed", at::kByte, {N, K / 2});
+  const at::Tensor& as = tensor_of(o_as, "a_scales", at::kFloat, {M});
+  same_device(as, "a_scales", codes, "codes");
+  same_device(w, "w", codes, "codes");
+  same_device(ws, "w_scales", codes, "codes");
+  const int32_t act = gate_activation(o_act);
+  Out y(o_y, "y", at::kHalf, {M, F}, codes);
+  allocate(y);
+  same_device(y.t, "y", codes, "codes");
+  call("dptq_qlinear_gated", codes, dptq_qlinear_gated, ptr(codes), ptr<float>(as), M, K, bits, ptr<uint8_t>(w),
+       weights, ptr<float>(ws), F, act, y.ptr());
+  return y.release();
+}
+
+// qlinear_gated(codes, a_scales, bits, w_packed, w_scales, y, activation)
+PyObject* qlinear_gated(PyObject* const* a) {
+  return gated(a[0], a[1], bits_4_or_8(a[2]), a[3], DPTQ_WEIGHTS_PACKED, a[4], a[5], a[6]);
+}
+
+// qlinear_gated_a8(codes, a_scales, w_a8, w_scales, y, activation)
+PyObject* qlinear_gated_a8(PyObject* const* a) {
+  return gated(a[0], a[1], 8, a[2], DPTQ_WEIGHTS_A8_ORDER, a[3], a[4], a[5]);
+}
+
+// qlinear_gated_decode_native(codes, a_scales, bits, w_dec, w_scales, y, activation)
+PyObject* qlinear_gated_decode_native(PyObject* const* a) {
+  return gated(a[0], a[1], bits_4_or_8(a[2]), a[3], DPTQ_WEIGHTS_DECODE, a[4], a[5], a[6]);
+}
+
+// qlinear_gated_fp6(a6, a_scales, w6, w_scales, M, K, F, y, activation)
+PyObject* qlinear_gated_fp6(PyObject* const* a) {
+  const int64_t M = integer(a[4], "M"), K = integer(a[5], "K"), F = integer(a[6], "F");
+  if (F < 8 || F % 8 || F > 0x3FFFFFF8) fail(PyExc_ValueError, "F must be a positive multiple of 8");
+  const at::Tensor& a6 = tensor_of(a[0], "a_fp6", at::kByte, {fp6_bytes(M, K)});
+  const at::Tensor& w6 = tensor_of(a[2], "w_fp6", at::kByte, {fp6_bytes(2 * F, K)});
+  const at::Tensor& as = tensor_of(a[1], "a_scales", at::kFloat, {M});
+  const at::Tensor& ws = tensor_of(a[3], "w_scales", at::kFloat, {2 * F});
+  same_device(as, "a_scales", a6, "a_fp6");
+  same_device(w6, "w_fp6", a6, "a_fp6");
+  same_device(ws, "w_scales", a6, "a_fp6");
+  const int32_t act = gate_activation(a[8]);
+  Out y(a[7], "y", at::kHalf, {M, F}, a6);
+  allocate(y);
+  same_device(y.t, "y", a6, "a_fp6");
+  call("dptq_qlinear_gated_fp6", a6, dptq_qlinear_gated_fp6, ptr<uint8_t>(a6), ptr<float>(as), M, K,
+       ptr<uint8_t>(w6), ptr<float>(ws), F, act, y.ptr());
+  return y.release();
+}
+
 // qlinear_decode_fused(x, had_size, bits, w_packed, w_scales, y, codes, scales, mode)
 PyObject* qlinear_decode_fused(PyObject* const* a) {
   const at::Tensor& x = tensor(a[0], "x", at::kHalf);
@@ -491,11 +571,6 @@ PyObject* kv_dequant(PyObject* const* a) {
   call("dptq_kv_dequant", codes, dptq_kv_dequant, ptr<uint8_t>(codes), ptr<float>(scales), ptr<float>(mins),
        T, D, g, out.ptr());
   return out.release();
-}
-
-void same_device(const at::Tensor& t, const char* name, const at::Tensor& x, const char* of) {
-  if (t.device() != x.device())
-    fail(PyExc_ValueError, std::string(name) + " must be on the same device as " + of);
 }
 
 // rms_norm_quant(x, weight, eps, residual, sum, codes, scales)
@@ -800,6 +875,10 @@ PyMethodDef kMethods[] = {
     DPTQ_ENTRY(qlinear_decode_native, 6),
     DPTQ_ENTRY(qlinear_fp6, 8),
     DPTQ_ENTRY(qlinear_decode_fused, 9),
+    DPTQ_ENTRY(qlinear_gated, 7),
+    DPTQ_ENTRY(qlinear_gated_a8, 6),
+    DPTQ_ENTRY(qlinear_gated_decode_native, 7),
+    DPTQ_ENTRY(qlinear_gated_fp6, 9),
     DPTQ_ENTRY(qlinear_range, 8),
     DPTQ_ENTRY(residual_dynamics, 8),
     DPTQ_ENTRY(kv_quant, 5),

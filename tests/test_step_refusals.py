@@ -67,6 +67,48 @@ def test_rotary_kv8_append(L, status, changes):
     assert _call(L.dptq_rotary_kv8_append, APPEND, APPEND_GOOD, **changes) == status
 
 
+GATED = ["codes", "a_scales", "M", "K", "bits", "w", "weights", "w_scales", "F", "act", "y", "stream"]
+GATED_GOOD = dict(codes=P, a_scales=P, M=4, K=256, bits=8, w=P, weights=0, w_scales=P, F=32, act=0, y=P, stream=None)
+
+
+@pytest.mark.parametrize("status,changes", [
+    (INVALID, dict(M=-1)), (INVALID, dict(F=0)), (INVALID, dict(F=12)), (INVALID, dict(F=-8)), (INVALID, dict(bits=5)),
+    (UNSUPPORTED, dict(K=200)), (UNSUPPORTED, dict(K=1 << 17)), (UNSUPPORTED, dict(F=1 << 30)), (INVALID, dict(act=2)),
+    (INVALID, dict(act=-1)), (INVALID, dict(weights=1)), (INVALID, dict(weights=4)), (INVALID, dict(weights=2, bits=4)),
+    (UNSUPPORTED, dict(weights=3, M=17)), (INVALID, dict(codes=None)), (INVALID, dict(a_scales=None)),
+    (INVALID, dict(w=None)), (INVALID, dict(w_scales=None)), (INVALID, dict(y=None)), (INVALID, dict(codes=P + 8)),
+    (INVALID, dict(a_scales=P + 4)), (INVALID, dict(w_scales=P + 4)), (INVALID, dict(y=P + 2)), (INVALID, dict(w=P + 1)),
+    (OK, dict(M=0, codes=None, y=None)),
+])
+def test_gated(L, status, changes):
+    assert _call(L.dptq_qlinear_gated, GATED, GATED_GOOD, **changes) == status
+
+
+FP6 = ["a6", "a_scales", "M", "K", "w6", "w_scales", "F", "act", "y", "stream"]
+FP6_GOOD = dict(a6=P, a_scales=P, M=40, K=256, w6=P, w_scales=P, F=32, act=1, y=P, stream=None)
+
+
+@pytest.mark.parametrize("status,changes", [
+    (INVALID, dict(M=-1)), (INVALID, dict(F=4)), (UNSUPPORTED, dict(K=64)), (INVALID, dict(act=7)),
+    (INVALID, dict(a6=None)), (INVALID, dict(a_scales=P + 2)), (INVALID, dict(w6=P + 4)), (INVALID, dict(w_scales=None)),
+    (INVALID, dict(y=P + 8)), (OK, dict(M=0, a6=None)),
+])
+def test_gated_fp6(L, status, changes):
+    assert _call(L.dptq_qlinear_gated_fp6, FP6, FP6_GOOD, **changes) == status
+
+
+def test_gate_up_rows():
+    gate, up = torch.arange(48).view(24, 2), torch.arange(100, 148).view(24, 2)
+    w = dptq.gate_up_rows(gate, up)
+    assert w.shape == (48, 2) and w.is_contiguous()
+    for f in range(24):
+        row = f // 8 * 16 + f % 8
+        assert torch.equal(w[row], gate[f]) and torch.equal(w[row + 8], up[f])
+    for a, b in ((gate[:20], up[:20]), (gate, up[:16]), (gate, up.float()), (gate[:0], up[:0])):
+        with pytest.raises(ValueError):
+            dptq.gate_up_rows(a, b)
+
+
 def test_frequencies():
     f = dptq.rotary_inv_freq(64, device="cpu")
     assert f.dtype == torch.float64 and f.tolist() == [10000.0 ** (-i / 32) for i in range(32)]
