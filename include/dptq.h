@@ -566,6 +566,43 @@ int dptq_token_logprobs(const void* logits, int32_t dtype, int64_t ld, int64_t M
                         void* stream);
 
 /*
+ * dptq_sample_tokens - one token of each row of logits, drawn under temperature,
+ * top-k, top-p and min-p from a given uniform number.
+ *
+ * The tokens of a row are taken in order: larger logits first, equal ones by
+ * index.  With w_v = exp((x_v - max x) / temperature), sums of w in that order:
+ *
+ *   K1 = the first top_k tokens          (all where top_k <= 0)
+ *   K2 = those of K1 before which the sum of w is below top_p times that of K1;
+ *        the first always                (K1 where top_p >= 1)
+ *   K3 = those of K2 with w >= min_p, the first always   (K2 where min_p <= 0)
+ *   token = the first one up to which the sum of w is above uniform times that
+ *        of K3;  prob = w_token / that of K3
+ *
+ * A temperature of 0 or below takes the first token, with prob 1, whatever the
+ * others say.  Weights and sums in 64 bits, of integers where their order could
+ * matter: the same call gives the same bits.  A logit of -inf is masked: it is
+ * never taken.  A row of nothing else gives token -1 and prob 0.  Rows that hold
+ * NaN or +inf, and NaN parameters, give unspecified tokens in [-1, V).
+ *
+ *   logits      device, fp16 (dtype DPTQ_F16) or float (DPTQ_F32) [M, V], ld
+ *               elements from a row to the next (>= V), aligned to its elements
+ *   M           rows, 0 <= M < 2^31; V: 1 <= V < 2^30
+ *   uniform     device, float [M], in [0, 1)
+ *   temperature, top_k, top_p, min_p   device, float or int32 [M]; NULL: the
+ *               value beside it for every row
+ *   tokens      device, int64 [M] output; probs device, float [M] output
+ *   workspace   device, 16-byte aligned, dptq_sample_tokens_workspace bytes
+ *               (NULL where that is 0)
+ */
+int64_t dptq_sample_tokens_workspace(int64_t M, int64_t V, int32_t dtype); /* -1: invalid */
+int dptq_sample_tokens(const void* logits, int32_t dtype, int64_t ld, int64_t M, int64_t V,
+                       const float* uniform, const float* temperature, float temperature_all,
+                       const int32_t* top_k, int32_t top_k_all, const float* top_p, float top_p_all,
+                       const float* min_p, float min_p_all, int64_t* tokens, float* probs,
+                       void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
  * dptq_layer_policy - phase-aware activation precision (host only).
  * Algorithm 1 step 2 with the sensitive set of Eq. 21.
  *

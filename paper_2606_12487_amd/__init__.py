@@ -29,7 +29,7 @@ __all__ = ["DptqError", "lib", "library_path", "rotate_quant", "qlinear", "qline
            "rms_norm_quant", "KV8Cache", "KV8_PAGE", "kv8_cache", "kv8_append", "kv8_attention",
            "token_logprobs", "MAX_TOP", "rotary", "rotary_inv_freq", "rotary_kv8_append",
            "gate_up_rows", "qlinear_gated", "qlinear_gated_a8", "qlinear_gated_decode_native", "qlinear_gated_fp6",
-           "WEIGHTS_PACKED",
+           "WEIGHTS_PACKED", "sample_tokens",
            "EXPORTED_FUNCTIONS", "GEMM_AUTO",
            "GEMM_DECODE", "GEMM_TILE_256X128", "GEMM_TILE_192X256"]
 
@@ -53,7 +53,8 @@ EXPORTED_FUNCTIONS = ("dptq_status_string", "dptq_version", "dptq_rotate_quant",
                       "dptq_qlinear_decode_native", "dptq_rms_norm_quant", "dptq_kv8_append",
                       "dptq_kv8_attention_workspace", "dptq_kv8_attention",
                       "dptq_token_logprobs_workspace", "dptq_token_logprobs", "dptq_rotary",
-                      "dptq_rotary_kv8_append", "dptq_qlinear_gated", "dptq_qlinear_gated_fp6")
+                      "dptq_rotary_kv8_append", "dptq_qlinear_gated", "dptq_qlinear_gated_fp6",
+                      "dptq_sample_tokens_workspace", "dptq_sample_tokens")
 
 # Code layouts of dptq_rotate_quant_ex.
 LAYOUT_PACKED, LAYOUT_FP6 = 0, 1
@@ -120,6 +121,12 @@ def lib():
         L.dptq_kv8_attention.argtypes = [vp, i64, i64, vp, vp, i64, vp, i64, i64, i32, i32, i32, vp, vp, vp, vp,
                                          ctypes.c_float, i32, i32, i64, i64, vp, vp, vp, i64, vp]
         L.dptq_kv8_attention.restype = ctypes.c_int
+        f32 = ctypes.c_float
+        L.dptq_sample_tokens_workspace.argtypes = [i64, i64, i32]
+        L.dptq_sample_tokens_workspace.restype = ctypes.c_int64
+        L.dptq_sample_tokens.argtypes = [vp, i32, i64, i64, i64, vp, vp, f32, vp, i32, vp, f32, vp, f32, vp, vp, vp, i64,
+                                         vp]
+        L.dptq_sample_tokens.restype = ctypes.c_int
         L.dptq_qlinear_gated.argtypes = [vp, vp, i64, i64, i32, vp, i32, vp, i64, i32, vp, vp]
         L.dptq_qlinear_gated.restype = ctypes.c_int
         L.dptq_qlinear_gated_fp6.argtypes = [vp, vp, i64, i64, vp, vp, i64, i32, vp, vp]
@@ -685,3 +692,13 @@ def token_logprobs(logits, tokens, top=0, logprobs=None, entropy=None, top_logpr
     and equal ones by index: (logprobs fp32 [M], entropy fp32 [M], top_logprobs fp32 [M, top], top_ids int64
     [M, top]).  Logits of -inf are masked."""
     return _binding().token_logprobs(logits, tokens, top, logprobs, entropy, top_logprobs, top_ids)
+
+
+def sample_tokens(logits, uniform, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, tokens=None, probs=None):
+    """One token of each row of logits (fp16 or fp32 [M, V]; rows may be parts of wider ones), drawn from the given
+    uniform numbers (float32 [M], in [0, 1)): (tokens int64 [M], probs fp32 [M], the token's probability among those
+    that are left).  Each parameter is a number or a tensor [M] (float32; top_k int32).  In this order: the top_k
+    largest logits stay (0: all), of these the likeliest up to a probability of top_p, of these the ones at least min_p
+    times as likely as the first; then the likeliest tokens up to a probability of `uniform`, the last of which is
+    taken.  Temperature 0: the largest logit.  Logits of -inf are masked; a row of nothing else gives -1."""
+    return _binding().sample_tokens(logits, uniform, temperature, top_k, top_p, min_p, tokens, probs)

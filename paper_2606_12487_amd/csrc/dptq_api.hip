@@ -152,6 +152,16 @@ int logprobs_shape(int64_t ld, int64_t M, int64_t V, int32_t top, int32_t dtype,
   return DPTQ_OK;
 }
 
+int sample_shape(int64_t ld, int64_t M, int64_t V, int32_t dtype, dptq::SampleTokens* c) {
+  dptq::TokenLogprobs l{};   // the same rows
+  const int st = logprobs_shape(ld, M, V, 0, dtype, &l);
+  c->fp32 = l.fp32;
+  c->ld = l.ld;
+  c->M = l.M;
+  c->V = l.V;
+  return st;
+}
+
 }  // namespace
 
 extern "C" {
@@ -677,6 +687,44 @@ int dptq_token_logprobs(const void* logits, int32_t dtype, int64_t ld, int64_t M
   c.top_ids = top_ids;
   c.workspace = workspace;
   return from_hip(dptq::launch_token_logprobs(c, static_cast<hipStream_t>(stream)));
+}
+
+int64_t dptq_sample_tokens_workspace(int64_t M, int64_t V, int32_t dtype) {
+  dptq::SampleTokens c{};
+  if (sample_shape(V, M, V, dtype, &c) != DPTQ_OK) return -1;
+  return M == 0 ? 0 : dptq::sample_tokens_workspace(c);
+}
+
+int dptq_sample_tokens(const void* logits, int32_t dtype, int64_t ld, int64_t M, int64_t V,
+                       const float* uniform, const float* temperature, float temperature_all,
+                       const int32_t* top_k, int32_t top_k_all, const float* top_p, float top_p_all,
+                       const float* min_p, float min_p_all, int64_t* tokens, float* probs,
+                       void* workspace, int64_t workspace_bytes, void* stream) {
+  dptq::SampleTokens c{};
+  const int st = sample_shape(ld, M, V, dtype, &c);
+  if (st != DPTQ_OK) return st;
+  if (M == 0) return DPTQ_OK;
+  if (!logits || !uniform || !tokens || !probs) return DPTQ_ERR_INVALID_ARG;
+  const uintptr_t element = c.fp32 ? 4 : 2;
+  if (reinterpret_cast<uintptr_t>(logits) % element != 0 || !aligned4(uniform) || !aligned4(temperature) ||
+      !aligned4(top_k) || !aligned4(top_p) || !aligned4(min_p) || !aligned8(tokens) || !aligned4(probs))
+    return DPTQ_ERR_INVALID_ARG;
+  const int64_t need = dptq::sample_tokens_workspace(c);
+  if (need > 0 && (!workspace || !aligned16(workspace) || workspace_bytes < need)) return DPTQ_ERR_INVALID_ARG;
+  c.logits = logits;
+  c.uniform = uniform;
+  c.temperature = temperature;
+  c.top_k = top_k;
+  c.top_p = top_p;
+  c.min_p = min_p;
+  c.temperature_all = temperature_all;
+  c.top_k_all = top_k_all;
+  c.top_p_all = top_p_all;
+  c.min_p_all = min_p_all;
+  c.tokens = tokens;
+  c.probs = probs;
+  c.workspace = workspace;
+  return from_hip(dptq::launch_sample_tokens(c, static_cast<hipStream_t>(stream)));
 }
 
 int dptq_layer_policy(int32_t num_layers, const uint8_t* mask, int32_t* bits_out) {

@@ -111,6 +111,22 @@ struct TokenLogprobs {
 int64_t token_logprobs_workspace(const TokenLogprobs& c);   // bytes
 hipError_t launch_token_logprobs(const TokenLogprobs& c, hipStream_t stream);
 
+struct SampleTokens {
+  const void* logits;   // fp16 or fp32 rows, ld elements apart
+  bool fp32;
+  int64_t ld, M;
+  int V;
+  const float *uniform, *temperature, *top_p, *min_p;   // [M]; all but uniform may be nullptr: the value for all
+  const int32_t* top_k;
+  float temperature_all, top_p_all, min_p_all;
+  int32_t top_k_all;
+  int64_t* tokens;
+  float* probs;
+  void* workspace;
+};
+int64_t sample_tokens_workspace(const SampleTokens& c);   // bytes; M > 0
+hipError_t launch_sample_tokens(const SampleTokens& c, hipStream_t stream);
+
 // One call of the K-split GEMM (qgemm_ksplit.hip): y from the dequant epilogue,
 // with the zero-point correction when a_zeros is given, or the raw
 // accumulators when acc is.

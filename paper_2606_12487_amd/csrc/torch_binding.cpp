@@ -838,6 +838,61 @@ PyObject* token_logprobs(PyObject* const* a) {
   return tuple(lp, entropy, top_lp, ids);
 }
 
+// Logits [M, V], fp16 or fp32, rows *ld apart.
+const at::Tensor& logit_rows(PyObject* o, int32_t* dtype, int64_t* ld) {
+  if (!THPVariable_Check(o)) fail(PyExc_TypeError, "logits must be a torch.Tensor");
+  const at::ScalarType type = THPVariable_Unpack(o).scalar_type();
+  const bool half = type == at::kHalf;
+  if (!half && type != at::kFloat) fail(PyExc_TypeError, "logits must have dtype torch.float16 or torch.float32");
+  const at::Tensor& x = gpu_tensor(o, "logits", type);
+  two_d(x, "logits must be 2-D [M, V]");
+  *ld = x.size(0) > 1 ? x.stride(0) : x.size(1);
+  if ((x.size(1) > 1 && x.stride(1) != 1) || *ld < x.size(1)) fail(PyExc_ValueError, "logits must have dense rows");
+  *dtype = half ? DPTQ_F16 : DPTQ_F32;
+  return x;
+}
+
+// A parameter of each row, a tensor [M] (nullptr: a number for all).
+const at::Tensor* of_rows(PyObject* o, const char* name, at::ScalarType type, int64_t M, const at::Tensor& x) {
+  if (!THPVariable_Check(o)) return nullptr;
+  const at::Tensor& t = tensor_of(o, name, type, {M});
+  same_device(t, name, x, "logits");
+  return &t;
+}
+
+// sample_tokens(logits, uniform, temperature, top_k, top_p, min_p, tokens, probs)
+PyObject* sample_tokens(PyObject* const* a) {
+  int32_t dtype;
+  int64_t ld;
+  const at::Tensor& x = logit_rows(a[0], &dtype, &ld);
+  const int64_t M = x.size(0), V = x.size(1);
+  const at::Tensor& u = tensor_of(a[1], "uniform", at::kFloat, {M});
+  same_device(u, "uniform", x, "logits");
+  const at::Tensor* t = of_rows(a[2], "temperature", at::kFloat, M, x);
+  const at::Tensor* k = of_rows(a[3], "top_k", at::kInt, M, x);
+  const at::Tensor* p = of_rows(a[4], "top_p", at::kFloat, M, x);
+  const at::Tensor* m = of_rows(a[5], "min_p", at::kFloat, M, x);
+  const double t_all = t ? 0 : real(a[2]), p_all = p ? 0 : real(a[4]), m_all = m ? 0 : real(a[5]);
+  const int64_t k_all = k ? 0 : integer(a[3], "top_k");
+  if (!t && !(t_all >= 0)) fail(PyExc_ValueError, "temperature must not be negative");
+  if (k_all < 0 || k_all > 0x7FFFFFFF) fail(PyExc_ValueError, "top_k must be in [0, 2^31)");
+  if (!p && !(p_all >= 0)) fail(PyExc_ValueError, "top_p must not be negative");
+  if (!m && !(m_all >= 0)) fail(PyExc_ValueError, "min_p must not be negative");
+  Out tokens(a[6], "tokens", at::kLong, {M}, x);
+  Out probs(a[7], "probs", at::kFloat, {M}, x);
+  const int64_t bytes = dptq_sample_tokens_workspace(M, V, dtype);
+  Out work(Py_None, "workspace", at::kByte, {bytes > 0 ? bytes : 0}, x);
+  if (bytes > 0) allocate(tokens, probs, work);
+  else allocate(tokens, probs);
+  same_device(tokens.t, "tokens", x, "logits");
+  same_device(probs.t, "probs", x, "logits");
+  call("dptq_sample_tokens", x, dptq_sample_tokens, ptr(x), dtype, ld, M, V, ptr<float>(u),
+       t ? ptr<float>(*t) : nullptr, (float)t_all, k ? ptr<int32_t>(*k) : nullptr, (int32_t)k_all,
+       p ? ptr<float>(*p) : nullptr, (float)p_all, m ? ptr<float>(*m) : nullptr, (float)m_all, tokens.ptr<int64_t>(),
+       probs.ptr<float>(), bytes > 0 ? work.ptr() : nullptr, bytes > 0 ? bytes : 0);
+  return tuple(tokens, probs);
+}
+
 // init(raise_error, raw_stream)
 PyObject* init(PyObject* const* a) {
   Py_INCREF(a[0]);
@@ -889,6 +944,7 @@ PyMethodDef kMethods[] = {
     DPTQ_ENTRY(rotary, 8),
     DPTQ_ENTRY(rotary_kv8_append, 15),
     DPTQ_ENTRY(token_logprobs, 7),
+    DPTQ_ENTRY(sample_tokens, 8),
     {nullptr, nullptr, 0, nullptr},
 };
 

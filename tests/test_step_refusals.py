@@ -97,6 +97,32 @@ def test_gated_fp6(L, status, changes):
     assert _call(L.dptq_qlinear_gated_fp6, FP6, FP6_GOOD, **changes) == status
 
 
+SAMPLE = ["logits", "dtype", "ld", "M", "V", "uniform", "temperature", "t", "top_k", "k", "top_p", "p", "min_p", "m",
+          "tokens", "probs", "workspace", "bytes", "stream"]
+SAMPLE_GOOD = dict(logits=P, dtype=0, ld=1000, M=600, V=1000, uniform=P, temperature=P, t=1.0, top_k=P, k=0, top_p=P,
+                   p=1.0, min_p=P, m=0.0, tokens=P, probs=P, workspace=None, bytes=0, stream=None)
+
+
+@pytest.mark.parametrize("status,changes", [
+    (INVALID, dict(M=-1)), (INVALID, dict(V=0)), (INVALID, dict(ld=999)), (INVALID, dict(dtype=2)),
+    (UNSUPPORTED, dict(M=1 << 31)), (UNSUPPORTED, dict(V=1 << 30, ld=1 << 30)), (INVALID, dict(logits=None)),
+    (INVALID, dict(uniform=None)), (INVALID, dict(tokens=None)), (INVALID, dict(probs=None)), (INVALID, dict(logits=P + 1)),
+    (INVALID, dict(dtype=1, logits=P + 2)), (INVALID, dict(uniform=P + 2)), (INVALID, dict(temperature=P + 1)),
+    (INVALID, dict(top_k=P + 2)), (INVALID, dict(top_p=P + 2)), (INVALID, dict(min_p=P + 2)),
+    (INVALID, dict(tokens=P + 4)), (INVALID, dict(probs=P + 2)),
+    (INVALID, dict(M=1, V=100000, ld=100000)), (INVALID, dict(M=1, V=100000, ld=100000, workspace=P, bytes=1000)),
+    (INVALID, dict(M=1, V=100000, ld=100000, workspace=P + 8, bytes=1 << 30)), (OK, dict(M=0, logits=None)),
+])
+def test_sample_tokens(L, status, changes):
+    assert _call(L.dptq_sample_tokens, SAMPLE, SAMPLE_GOOD, **changes) == status
+
+
+def test_sample_tokens_workspace(L):
+    assert L.dptq_sample_tokens_workspace(0, 100, 0) == 0 and L.dptq_sample_tokens_workspace(1, 0, 0) == -1
+    assert L.dptq_sample_tokens_workspace(1, 100, 5) == -1 and L.dptq_sample_tokens_workspace(-1, 100, 0) == -1
+    assert L.dptq_sample_tokens_workspace(1, 100, 0) == 0 and L.dptq_sample_tokens_workspace(1, 1 << 17, 1) > 0
+
+
 def test_gate_up_rows():
     gate, up = torch.arange(48).view(24, 2), torch.arange(100, 148).view(24, 2)
     w = dptq.gate_up_rows(gate, up)
