@@ -22,20 +22,21 @@
 //
 // w in 64 bits: with 131072 tokens of like weight a relative error of 2^-24 in
 // the sums would change one token in a hundred.  2^t = 2^n (1 + f q(f)) with n
-// the nearest integer and q the interpolant of degree 8 at Chebyshev's nodes on
-// [-1/2, 1/2], to 4e-14.
+// the nearest integer and q the interpolant of degree 6 at Chebyshev's nodes on
+// [-1/2, 1/2], to 1.2e-10, and alternating, so that sums are closer.
 #include "internal.h"
+#include "wave_device.h"
 
 namespace dptq {
 namespace {
 
 constexpr int kThreads = 1024, kWaves = kThreads / 64;
-constexpr int kBins = 1024;       // one a thread
+constexpr int kBinBits = 10, kBins = 1 << kBinBits;   // one a thread
 constexpr int kCap = 2048;        // tokens that are sorted at once
-constexpr int kMinPart = 8192;    // logits of a part of a row, at least
+constexpr int kMinPart = 16384;    // logits of a part of a row, at least
 
 // Values as integers in their order; -0 is 0.
-constexpr uint32_t kLowestKey = 0x00800000u, kHighestKey = 0xFF800000u;   // -FLT_MAX to +inf: what counts
+constexpr uint32_t kLowestKey = 0x00800000u;   // of -FLT_MAX; what is not masked is this or above
 __device__ __forceinline__ uint32_t key_of(float x) {
   const uint32_t u = __float_as_uint(x + 0.0f);
   return u ^ (u >> 31 ? 0xFFFFFFFFu : 0x80000000u);
@@ -43,17 +44,18 @@ __device__ __forceinline__ uint32_t key_of(float x) {
 __device__ __forceinline__ float value_of(uint32_t k) {
   return __uint_as_float(k ^ (k >> 31 ? 0x80000000u : 0xFFFFFFFFu));
 }
-__device__ __forceinline__ bool counts(uint32_t k) { return k - kLowestKey <= kHighestKey - kLowestKey; }
 
 // Bins: five bits of the mantissa and 16 octaves, 2^-6 to 2^10, for each sign;
 // smaller magnitudes in the bins at zero, larger ones in the outermost.
 constexpr int kBinShift = 18, kBinBase = (127 - 6) << 5;
-__device__ __forceinline__ int bin_of(uint32_t k) {
-  const bool positive = k >> 31;
-  const int q = (int)(((positive ? k : ~k) & 0x7FFFFFFFu) >> kBinShift) - kBinBase;
+// Of a value that counts, and of its key.
+__device__ __forceinline__ int bin_of(float x) {
+  const uint32_t u = __float_as_uint(x + 0.0f);   // -0 is 0
+  const int q = (int)(u << 1 >> (kBinShift + 1)) - kBinBase;
   const int c = min(max(q, 0), kBins / 2 - 1);
-  return positive ? kBins / 2 + c : kBins / 2 - 1 - c;
+  return c ^ ((int)u >> 31 & (kBins - 1)) ^ kBins / 2;   // negative: kBins / 2 - 1 - c
 }
+__device__ __forceinline__ int bin_of(uint32_t k) { return bin_of(value_of(k)); }
 struct Range {
   uint32_t lo, hi;   // keys, both in it
 };
@@ -66,18 +68,24 @@ __device__ __forceinline__ Range range_of(int bin) {
   return Range{b == 0x7F800000u ? kLowestKey : 0x7FFFFFFFu - b, 0x7FFFFFFFu - a};   // magnitudes a to b, negative
 }
 
+// a b + c with c in scalar registers: as an FMA of three operands; the compiler
+// keeps the constants in vector registers and copies each before its FMA.
+__device__ __forceinline__ double fma_scalar(double a, double b, double c) {
+  double d;
+  asm("v_fma_f64 %0, %1, %2, %3" : "=v"(d) : "v"(a), "v"(b), "s"(c));
+  return d;
+}
+
 // 2^((x - m) c) in 64 bits, for x <= m.
 __device__ __forceinline__ double weight(float x, float m, double c) {
   const double t = fmax(((double)x - (double)m) * c, -2000.0);
   const double n = __builtin_rint(t), f = t - n;
-  double q = __builtin_fma(f, 0x1.b639ab2e49ae8p-24, 0x1.63d1341b008a0p-20);
-  q = __builtin_fma(f, q, 0x1.ffcb942c7e385p-17);
-  q = __builtin_fma(f, q, 0x1.4308ac87f8c3cp-13);
-  q = __builtin_fma(f, q, 0x1.5d87fe872c528p-10);
-  q = __builtin_fma(f, q, 0x1.3b2ab71819e07p-7);
-  q = __builtin_fma(f, q, 0x1.c6b08d7047e27p-5);
-  q = __builtin_fma(f, q, 0x1.ebfbdff823cfep-3);
-  q = __builtin_fma(f, q, 0x1.62e42fefa39edp-1);
+  double q = fma_scalar(f, 0x1.00a5814f2a63cp-16, 0x1.443fffcaa2337p-13);
+  q = fma_scalar(f, q, 0x1.5d879ead1c114p-10);
+  q = fma_scalar(f, q, 0x1.3b2a1b7150c21p-7);
+  q = fma_scalar(f, q, 0x1.c6b08d883db58p-5);
+  q = fma_scalar(f, q, 0x1.ebfbe045f4d5cp-3);
+  q = fma_scalar(f, q, 0x1.62e42fefa39f0p-1);
   q = __builtin_fma(f, q, 1.0);
   return __builtin_ldexp(q, (int)n);
 }
@@ -89,34 +97,84 @@ __device__ __forceinline__ u64 fixed(double w, double unit) {
   return (u64)__double_as_longlong(__builtin_fma(w, unit, 0x1p52)) & 0xFFFFFFFFFFFFFull;
 }
 
-// Calls f(x[i], i) for lo <= i < hi over a workgroup; 16-byte loads where they
-// are whole, U in flight.
-template <int U, typename T, typename F>
-__device__ __forceinline__ void for_logits(const T* x, int lo, int hi, const F& f) {
-  constexpr int E = 16 / sizeof(T);
-  const int start = lo - (int)((reinterpret_cast<uintptr_t>(x + lo) & 15) / sizeof(T));
-  for (int64_t at = start; at < hi; at += (int64_t)U * kThreads * E) {
-    uint4 v[U];
-    int64_t i[U];
-    bool whole[U];
+// Logits [lo, hi) of a row as a workgroup reads them: what lies before the first
+// and after the last whole 16 bytes, a logit to a thread, and between them
+// vectors, four to a thread at a time.  The loops over the four are not unrolled:
+// the code has to come into the instruction cache first, and a row is not long.
+template <typename T>
+struct Reader {
+  static constexpr int kEach = 16 / sizeof(T), kLoads = 4, kSpan = kLoads * kThreads;
+  const T* x;
+  int lo, hi, first, vectors;   // first: index of the first vector's first logit
+  struct Chunk {
+    uint4 v[kLoads];
+  };
+
+  __device__ __forceinline__ Reader(const T* row, int from, int to) : x(row), lo(from), hi(to) {
+    const int past = (int)((reinterpret_cast<uintptr_t>(x + lo) & 15) / sizeof(T));
+    first = min(past ? lo + kEach - past : lo, hi);
+    vectors = (hi - first) / kEach;
+  }
+  __device__ __forceinline__ uint4 none() const {
+    const uint32_t w = sizeof(T) == 2 ? 0xFC00FC00u : 0xFF800000u;   // -inf
+    return make_uint4(w, w, w, w);
+  }
+  // Vectors [at, at + kSpan); -inf for those that there are not.
+  __device__ __forceinline__ void load(int at, Chunk& c) const {
+    const uint4* const p = reinterpret_cast<const uint4*>(x + first);
 #pragma unroll
-    for (int n = 0; n < U; ++n) {
-      i[n] = at + ((int64_t)n * kThreads + threadIdx.x) * E;
-      whole[n] = i[n] >= lo && i[n] + E <= hi;
-      if (whole[n]) v[n] = *reinterpret_cast<const uint4*>(x + i[n]);
-    }
-#pragma unroll
-    for (int n = 0; n < U; ++n) {
-      if (whole[n]) {
-        const T* const e = reinterpret_cast<const T*>(&v[n]);
-#pragma unroll
-        for (int j = 0; j < E; ++j) f((float)e[j], (int)i[n] + j);
-      } else {
-        for (int j = 0; j < E; ++j)
-          if (i[n] + j >= lo && i[n] + j < hi) f((float)x[i[n] + j], (int)(i[n] + j));
-      }
+    for (int n = 0; n < kLoads; ++n) {
+      const int i = at + n * kThreads + (int)threadIdx.x;
+      c.v[n] = none();
+      if (i < vectors) c.v[n] = p[i];
     }
   }
+  // f(logit, number in its vector, index of the vector's first logit), vector by vector.
+  template <typename F>
+  __device__ __forceinline__ void each(Chunk c, int at, const F& f) const {
+    int i = first + (at + (int)threadIdx.x) * kEach;
+#pragma unroll 1
+    for (int n = 0; n < kLoads; ++n) {
+      f(c.v[0], i);
+#pragma unroll
+      for (int k = 0; k + 1 < kLoads; ++k) c.v[k] = c.v[k + 1];
+      i += kThreads * kEach;
+    }
+  }
+  // The thread's logit of the ends, as a vector of it and -inf, and its index.
+  __device__ __forceinline__ uint4 ends(int& i) const {
+    const int t = threadIdx.x, last = first + vectors * kEach;
+    i = t < first - lo ? lo + t : t >= 64 && t - 64 < hi - last ? last + t - 64 : -1;
+    uint4 v = none();
+    if (i >= 0) {
+      if constexpr (sizeof(T) == 2) v.x = 0xFC000000u | __half_as_ushort(x[i]);
+      else v.x = __float_as_uint(x[i]);
+    }
+    return v;
+  }
+};
+template <typename T, typename F>
+__device__ __forceinline__ void values(uint4 v, const F& f) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    if constexpr (sizeof(T) == 2) {
+      const __half2 h = *reinterpret_cast<const __half2*>(&w[k]);
+      f(__low2float(h), 2 * k);
+      f(__high2float(h), 2 * k + 1);
+    } else {
+      f(__uint_as_float(w[k]), k);
+    }
+  }
+}
+
+// Value j of a vector.
+template <typename T>
+__device__ __forceinline__ float value_at(uint4 v, int j) {
+  const int k = sizeof(T) == 2 ? j >> 1 : j;
+  const uint32_t w = k < 2 ? (k ? v.y : v.x) : k == 2 ? v.z : v.w;
+  if constexpr (sizeof(T) == 2) return __half2float(__ushort_as_half((unsigned short)(j & 1 ? w >> 16 : w)));
+  else return __uint_as_float(w);
 }
 
 struct SampleArgs {
@@ -131,16 +189,31 @@ struct SampleArgs {
   int top_k_all;
   int64_t* tokens;
   float* probs;
+  // Of rows in parts, from the first launch: their histograms.
   u64* mass;                // [M][splits][kBins]
   uint32_t* count;
   float* most;              // [M][splits]
 };
 
-// log2(e) / T; a greedy row (T = 0) is that of T = 1.
-__device__ __forceinline__ double factor(const SampleArgs& a, int64_t row, bool* greedy) {
+// What a row asks for.
+struct Asked {
+  double c;        // log2(e) / T; a greedy row (T = 0) is that of T = 1
+  float u, top_p, min_p;
+  uint32_t top_k;  // 0: all
+  bool greedy;
+};
+__device__ __forceinline__ Asked asked_of(const SampleArgs& a, int64_t row) {
   const float t = a.temperature ? a.temperature[row] : a.temperature_all;
-  *greedy = !(t > 0.0f);
-  return 1.4426950408889634 / (*greedy ? 1.0 : (double)t);
+  const int32_t k = a.top_k ? a.top_k[row] : a.top_k_all;
+  Asked q;
+  q.u = a.u[row];
+  q.top_p = a.top_p ? a.top_p[row] : a.top_p_all;
+  q.min_p = a.min_p ? a.min_p[row] : a.min_p_all;
+  q.greedy = !(t > 0.0f);
+  q.c = 1.4426950408889634 / (q.greedy ? 1.0 : (double)t);
+  // A top_p of 0 or a min_p above 1 leaves the first one, as a greedy row does.
+  q.top_k = q.greedy || q.top_p <= 0.0f || q.min_p > 1.0f ? 1u : k > 0 ? (uint32_t)k : 0u;
+  return q;
 }
 
 struct Histogram {
@@ -150,82 +223,181 @@ struct Histogram {
 
 struct Shared {
   Histogram h;                 // of the row, then of a bin that is cut again
-  double mass[kBins + 1];      // before bin kBins - 1 - j
+  u64 mass[kBins + 1];         // before bin kBins - 1 - j
   uint32_t count[kBins + 1];
   u64 list[kCap];              // key and ~index, in the order
-  double sum[kCap];            // up to each
-  double wave_d[kWaves];
-  uint32_t wave_u[kWaves];
-  float wave_f[kWaves];
+  u64 sum[kCap];               // up to each
+  u64 wave_m[2][kWaves];
+  uint32_t wave_n[2][kWaves];
+  float wave_f[2][kWaves];
   int n, found;
 };
 
-__device__ __forceinline__ void clear(Histogram& h) {
-  h.mass[threadIdx.x] = 0;
-  h.count[threadIdx.x] = 0;
+// The sum of the waves before this one, of each wave's value (lane 63's), in
+// part; a barrier comes before the reads, and the callers alternate between two
+// parts.
+template <typename V>
+__device__ __forceinline__ void put_wave(V x, V* part) {
+  if ((threadIdx.x & 63) == 63) part[threadIdx.x >> 6] = x;
+}
+template <typename V>
+__device__ __forceinline__ V waves_before(const V* part) {
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const V x = wave_scan((threadIdx.x & 63) < kWaves ? part[threadIdx.x & 63] : (V)0);
+  V before = 0;
+  if constexpr (sizeof(V) == 8) {
+    const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)x, wave ? wave - 1 : 0);
+    const uint32_t hi = __builtin_amdgcn_readlane((uint32_t)(x >> 32), wave ? wave - 1 : 0);
+    before = (u64)hi << 32 | lo;
+  } else {
+    before = __builtin_amdgcn_readlane(x, wave ? wave - 1 : 0);
+  }
+  return wave ? before : (V)0;
 }
 
-__device__ __forceinline__ float block_max(float x, float* part) {
-  for (int s = 32; s > 0; s >>= 1) x = fmaxf(x, __shfl_xor(x, s));
-  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = x;
-  __syncthreads();
-  x = part[threadIdx.x & (kWaves - 1)];
-  for (int s = kWaves / 2; s > 0; s >>= 1) x = fmaxf(x, __shfl_xor(x, s));
-  return x;
-}
-
-// The largest logit of [lo, hi), and their histogram relative to it.
+// The histogram of logits [lo, hi) of a row, relative to the largest of them,
+// which it returns: chunk by chunk, and where a larger one comes up the sums so
+// far are scaled down to it.  Barriers: none at the end.
 template <typename T>
 __device__ __forceinline__ float histogram(const T* x, int lo, int hi, double c, double unit, Histogram& h,
-                                           float* part) {
+                                           float (*part)[kWaves]) {
+  using R = Reader<T>;
+  const int tid = threadIdx.x;
+  h.mass[tid] = 0;
+  h.count[tid] = 0;
+  const R r(x, lo, hi);
+  typename R::Chunk now, next;
+  r.load(0, now);
+  int unused;
+  const uint4 ends = r.ends(unused);
   float m = -INFINITY;
-  for_logits<4>(x, lo, hi, [&](float v, int) { m = fmaxf(m, v); });
-  clear(h);
-  m = block_max(m, part);   // its barrier is the histogram's too
-  for_logits<1>(x, lo, hi, [&](float v, int) {
-    const uint32_t k = key_of(v);
-    if (!counts(k)) return;
-    const int b = bin_of(k);
-    atomicAdd(&h.count[b], 1u);
-    atomicAdd(&h.mass[b], fixed(weight(v, m, c), unit));
-  });
-  __syncthreads();
+  int parity = 0;
+  for (int at = 0; at < r.vectors || at == 0; at += R::kSpan) {
+    if (at + R::kSpan < r.vectors) r.load(at + R::kSpan, next);
+    float most = -INFINITY;
+    const auto larger = [&](float v, int) { most = fmaxf(most, v); };
+#pragma unroll
+    for (int n = 0; n < R::kLoads; ++n) values<T>(now.v[n], larger);
+    if (at == 0) values<T>(ends, larger);
+    most = wave_max(most);
+    put_wave(most, part[parity]);
+    __syncthreads();   // and the last chunk's sums are there
+    most = wave_max(part[parity][tid & (kWaves - 1)]);
+    parity ^= 1;
+    if (most > m) {
+      if (m > -INFINITY) h.mass[tid] = __double2ull_rn((double)h.mass[tid] * weight(m, most, c));
+      m = most;
+      __syncthreads();
+    }
+    if (most > -INFINITY) {
+      const auto add = [&](float v, int) {
+        const int b = bin_of(v);
+        const u64 w = fixed(weight(v, m, c), unit);
+        if (!(v > -INFINITY)) return;   // masked, or NaN
+        atomicAdd(&h.count[b], 1u);
+        atomicAdd(&h.mass[b], w);
+      };
+      r.each(now, at, [&](uint4 v, int) { values<T>(v, add); });
+      if (at == 0 && (lo < r.first || hi > r.first + r.vectors * R::kEach)) {
+        // The ends' single logits.
+        if constexpr (sizeof(T) == 2) add(__half2float(__ushort_as_half((unsigned short)ends.x)), 0);
+        else add(__uint_as_float(ends.x), 0);
+      }
+    }
+    now = next;
+  }
   return m;
 }
 
-// Inclusive sums over the workgroup, in the order of the threads.
-template <typename V>
-__device__ __forceinline__ V block_scan(V x, V* part) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  for (int s = 1; s < 64; s <<= 1) {
-    const V y = __shfl_up(x, s);
-    if (lane >= s) x += y;
-  }
-  if (lane == 63) part[wave] = x;
-  __syncthreads();
-  V before = 0;
-  for (int w = 0; w < kWaves; ++w)
-    if (w < wave) before += part[w];
-  __syncthreads();
-  return before + x;
-}
-
 // What a border is given by.
-enum class By { kCount, kSumBelow, kKey, kSumAbove };
+enum class By { kCount, kSum, kKey };
 struct Border {
   By by;
-  uint32_t n;      // kCount: the n-th token is the last before the border (n >= 1)
-  double sum;      // kSumBelow: tokens before which the sum is below it;
-                   // kSumAbove: the token up to which the sum is above it is the last
-  uint32_t key;    // kKey: tokens of this key and above
+  uint32_t n;      // kCount: the n-th token is the last before it (n >= 1)
+  u64 sum;         // kSum: the first token up to which the sum is this or more is
+                   // the last before it (sum > 0)
+  uint32_t key;    // kKey: it stands behind the tokens of this key and above
 };
 // Where it is: tokens before it, their sum, and the last of them.
 struct Place {
   uint32_t n;
-  double sum;
+  u64 sum;
   uint32_t key;
   int index;
 };
+
+// The first of `size` that holds, of a condition that holds for all behind it
+// too; size (a power of two, at most 64 * 64) if none does.  By every wave for
+// itself.
+template <typename F>
+__device__ __forceinline__ int first_of(int size, const F& holds) {
+  const int lane = threadIdx.x & 63;
+  int at = 0;
+  if (size > 64) {
+    const int step = size / 64;
+    const u64 yes = __ballot(holds(step * lane + step - 1));
+    if (!yes) return size;
+    at = step * (__ffsll((long long)yes) - 1);
+    size = step;
+  }
+  const u64 yes = __ballot(lane < size && holds(at + (lane < size ? lane : 0)));
+  return yes ? at + __ffsll((long long)yes) - 1 : at + size;
+}
+
+// One stage of a bitonic sort of size keys in the order (largest first), e of a
+// thread: key p = 1024 e + thread meets key p ^ j.
+__device__ __forceinline__ u64 better(u64 mine, u64 other, bool first) {
+  return (mine > other) == first ? mine : other;
+}
+template <int J>
+__device__ __forceinline__ u64 lane_xor64(u64 x) {
+  return (u64)lane_xor<J>((uint32_t)(x >> 32)) << 32 | lane_xor<J>((uint32_t)x);
+}
+template <int J>
+__device__ __forceinline__ void sort_in_wave(u64& v, uint32_t p, uint32_t k) {
+  v = better(v, lane_xor64<J>(v), ((p & J) == 0) == ((p & k) == 0));
+}
+__device__ __forceinline__ void sort_list(u64* list, int size) {
+  const uint32_t tid = threadIdx.x;
+  constexpr int E = kCap / kThreads;
+  u64 v[E];
+  bool mine[E];   // of whole waves
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    mine[e] = (int)(e * kThreads + tid) < size;
+    v[e] = mine[e] ? list[e * kThreads + tid] : 0;
+  }
+  __syncthreads();
+  for (uint32_t k = 2; k <= (uint32_t)size; k *= 2) {
+    for (uint32_t j = k / 2; j >= 64; j /= 2) {
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        if (mine[e]) list[e * kThreads + tid] = v[e];
+      __syncthreads();
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const uint32_t p = e * kThreads + tid;
+        if (mine[e]) v[e] = better(v[e], list[p ^ j], ((p & j) == 0) == ((p & k) == 0));
+      }
+      __syncthreads();
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const uint32_t p = e * kThreads + tid;
+      if (!mine[e]) continue;
+      if (k >= 64) sort_in_wave<32>(v[e], p, k);
+      if (k >= 32) sort_in_wave<16>(v[e], p, k);
+      if (k >= 16) sort_in_wave<8>(v[e], p, k);
+      if (k >= 8) sort_in_wave<4>(v[e], p, k);
+      if (k >= 4) sort_in_wave<2>(v[e], p, k);
+      sort_in_wave<1>(v[e], p, k);
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < E; ++e)
+    if (mine[e]) list[e * kThreads + tid] = v[e];
+  __syncthreads();
+}
 
 template <typename T>
 struct Selector {
@@ -237,75 +409,140 @@ struct Selector {
   // What the list holds: all tokens of a range, those before it.
   Range range;
   uint32_t before_n, held;
-  double before_sum;
+  u64 before_sum;
 
   __device__ __forceinline__ double weight_of(uint32_t key) const { return weight(value_of(key), m, c); }
 
-  // The cumulative counts and sums of s.h, descending, after `n` tokens of sum `sum`.
-  __device__ __forceinline__ void cumulate(uint32_t count, double mass, uint32_t n, double sum) {
-    const uint32_t cn = block_scan(count, s.wave_u);
-    const double cm = block_scan(mass, s.wave_d);
-    s.count[threadIdx.x + 1] = n + cn;
-    s.mass[threadIdx.x + 1] = sum + cm;
+  // The cumulative counts and sums of the bins, descending (this thread's is the
+  // one after those of lower threads), after n tokens of sum `sum`.
+  __device__ __forceinline__ void cumulate(uint32_t count, u64 mass, uint32_t n, u64 sum) {
+    const uint32_t cn = wave_scan(count);
+    const u64 cm = wave_scan(mass);
+    put_wave(cn, s.wave_n[0]);
+    put_wave(cm, s.wave_m[0]);
+    __syncthreads();
+    s.count[threadIdx.x + 1] = n + waves_before(s.wave_n[0]) + cn;
+    s.mass[threadIdx.x + 1] = sum + waves_before(s.wave_m[0]) + cm;
     if (threadIdx.x == 0) s.count[0] = n, s.mass[0] = sum;
     __syncthreads();
   }
 
   // Which of the cumulated bins (0: the first in the order) a border is in; the
   // last that is not empty where rounding leaves none.  kKey does not come here.
-  __device__ __forceinline__ int bin_with(const Border& b) {
-    const int j = threadIdx.x;
-    if (j == 0) s.found = -1;
-    __syncthreads();
-    const uint32_t n0 = s.count[j], n1 = s.count[j + 1];
-    const double m0 = s.mass[j], m1 = s.mass[j + 1];
-    const bool here = b.by == By::kCount ? n0 < b.n && b.n <= n1
-                    : b.by == By::kSumBelow ? m0 < b.sum && b.sum <= m1
-                                            : m0 <= b.sum && b.sum < m1;
-    if (here && n1 > n0) s.found = j;
-    __syncthreads();
-    int found = s.found;
-    if (found < 0) {
-      __syncthreads();
-      if (n1 > n0) atomicMax(&s.found, j);
-      __syncthreads();
-      found = max(s.found, 0);
+  __device__ __forceinline__ int bin_with(const Border& b) const {
+    int j = kBins;
+    if (b.by == By::kSum) j = first_of(kBins, [&](int i) { return s.mass[i + 1] >= b.sum; });
+    if (j == kBins) {
+      const uint32_t n = b.by == By::kCount ? b.n : s.count[kBins];
+      j = first_of(kBins, [&](int i) { return s.count[i + 1] >= n; });
     }
-    __syncthreads();
-    return found;
+    return min(j, kBins - 1);
   }
 
-  // Gathers the tokens of a range, at most kCap, in their order, with their sums.
-  __device__ __forceinline__ void load(Range r, uint32_t n, double sum) {
+  // Gathers the tokens of a range into the list, in any order; their number, at
+  // most kCap.
+  __device__ __forceinline__ int gather(Range r) {
+    __syncthreads();   // the list's readers are done
     if (threadIdx.x == 0) s.n = 0;
     __syncthreads();
-    for_logits<4>(x, 0, V, [&](float v, int i) {
-      const uint32_t k = key_of(v);
-      if (k - r.lo > r.hi - r.lo) return;
-      const int at = atomicAdd(&s.n, 1);
-      if (at < kCap) s.list[at] = (u64)k << 32 | (uint32_t)~i;
-    });
-    __syncthreads();
-    const int count = min(s.n, kCap);
-    int size = 64;
-    while (size < count) size *= 2;
-    for (int i = count + threadIdx.x; i < size; i += kThreads) s.list[i] = 0;   // behind all
-    __syncthreads();
-    for (int k = 2; k <= size; k *= 2)
-      for (int j = k / 2; j > 0; j /= 2) {
-        const int i = threadIdx.x, a = 2 * i - (i & (j - 1)), b = a + j;
-        if (i < size / 2) {
-          const u64 p = s.list[a], q = s.list[b];
-          if ((p < q) == ((a & k) == 0)) s.list[a] = q, s.list[b] = p;
-        }
-        __syncthreads();
+    const float least = value_of(r.lo), most = value_of(r.hi);
+    // A thread marks what it has of a vector that begins at index i.
+    const auto take = [&](uint4 v, int i) {
+      uint32_t mine = 0;
+      values<T>(v, [&](float e, int j) { mine |= e >= least && e <= most ? 1u << j : 0u; });
+      if (!mine) return;
+      // One addition for each lane as it is: the compiler would sum up a uniform
+      // address's over the wave, which takes longer for the few lanes here.
+      int offset;
+      asm("v_mov_b32 %0, 0" : "=v"(offset));
+      int to = atomicAdd(&s.n + offset, __popc(mine));
+      for (; mine; mine &= mine - 1, ++to) {
+        const int j = __ffs((int)mine) - 1;
+        if (to < kCap) s.list[to] = (u64)key_of(value_at<T>(v, j)) << 32 | (uint32_t)~(i + j);
       }
+    };
+    using R = Reader<T>;
+    const R reader(x, 0, V);
+    typename R::Chunk now, next;
+    int i;
+    const uint4 ends = reader.ends(i);
+    reader.load(0, now);
+    take(ends, i);
+    for (int at = 0; at < reader.vectors; at += R::kSpan) {
+      if (at + R::kSpan < reader.vectors) reader.load(at + R::kSpan, next);
+      reader.each(now, at, take);
+      now = next;
+    }
+    __syncthreads();
+    return min(s.n, kCap);
+  }
+
+  // Sorts the list's tokens: counted into kBins stretches of the range, scattered
+  // to their stretch, and each put behind those of it that come first.  A stretch
+  // holds a few; false, and nothing done, where one holds more than kCrowd.
+  __device__ __forceinline__ bool sort_by_buckets(int count, Range r) {
+    constexpr int E = kCap / kThreads, kCrowd = 64;
+    uint32_t* const offset = reinterpret_cast<uint32_t*>(s.h.mass);   // [kBins + 1]
+    const int tid = threadIdx.x;
+    const int shift = max(32 - kBinBits - __clz((int)(r.hi - r.lo)), 0);
+    s.h.count[tid] = 0;
+    if (tid == 0) s.found = 0;
+    __syncthreads();
+    u64 v[E];
+    uint32_t bucket[E], place[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int i = e * kThreads + tid;
+      if (i >= count) continue;
+      v[e] = s.list[i];
+      bucket[e] = (r.hi - (uint32_t)(v[e] >> 32)) >> shift;
+      place[e] = atomicAdd(&s.h.count[bucket[e]], 1u);
+      if (place[e] >= (uint32_t)kCrowd) s.found = 1;
+    }
+    __syncthreads();
+    if (s.found) return false;
+    const uint32_t mine = s.h.count[tid], up_to = wave_scan(mine);
+    put_wave(up_to, s.wave_n[1]);
+    __syncthreads();
+    const uint32_t end = waves_before(s.wave_n[1]) + up_to;
+    offset[tid + 1] = end;
+    if (tid == 0) offset[0] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      if (e * kThreads + tid < count) s.sum[offset[bucket[e]] + place[e]] = v[e];
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      if (e * kThreads + tid >= count) continue;
+      const uint32_t from = offset[bucket[e]], to = offset[bucket[e] + 1];
+      uint32_t at = from;
+      for (uint32_t i = from; i < to; ++i) at += s.sum[i] > v[e];
+      s.list[at] = v[e];
+    }
+    __syncthreads();
+    return true;
+  }
+
+  // Puts `count` gathered tokens in their order, with their sums: all of a range,
+  // after n of sum `sum`.
+  __device__ __forceinline__ void arrange(int count, Range r, uint32_t n, u64 sum) {
+    if (!sort_by_buckets(count, r)) {
+      int size = 64;
+      while (size < count) size *= 2;
+      for (int i = count + threadIdx.x; i < size; i += kThreads) s.list[i] = 0;   // behind all
+      __syncthreads();
+      sort_list(s.list, size);
+    }
     const int a = 2 * threadIdx.x;
-    const double w0 = a < count ? weight_of((uint32_t)(s.list[a] >> 32)) : 0.0;
-    const double w1 = a + 1 < count ? weight_of((uint32_t)(s.list[a + 1] >> 32)) : 0.0;
-    const double up_to = block_scan(w0 + w1, s.wave_d);
-    s.sum[a] = sum + (up_to - w1);
-    s.sum[a + 1] = sum + up_to;
+    const u64 w0 = a < count ? fixed(weight_of((uint32_t)(s.list[a] >> 32)), unit) : 0;
+    const u64 w1 = a + 1 < count ? fixed(weight_of((uint32_t)(s.list[a + 1] >> 32)), unit) : 0;
+    const u64 up_to = wave_scan(w0 + w1);
+    put_wave(up_to, s.wave_m[1]);
+    __syncthreads();
+    const u64 all = sum + waves_before(s.wave_m[1]) + up_to;
+    s.sum[a] = all - w1;
+    s.sum[a + 1] = all;
     __syncthreads();
     range = r;
     before_n = n;
@@ -314,30 +551,15 @@ struct Selector {
   }
 
   // A border among the list's tokens.
-  __device__ __forceinline__ Place in_list(const Border& b) {
-    const int i = 2 * threadIdx.x;
-    uint32_t n = 0;   // tokens of the list before the border
-    if (b.by == By::kCount) {
-      n = b.n - before_n;
-    } else {
-      int yes = 0;
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int at = i + e;
-        if (at >= (int)held) continue;
-        if (b.by == By::kKey) yes += (uint32_t)(s.list[at] >> 32) >= b.key;
-        else if (b.by == By::kSumAbove) yes += s.sum[at] <= b.sum;
-        else yes += (at ? s.sum[at - 1] : before_sum) < b.sum;
-      }
-      const uint32_t all = block_scan((uint32_t)yes, s.wave_u);
-      if (threadIdx.x == kThreads - 1) s.n = (int)all;
-      __syncthreads();
-      n = (uint32_t)s.n + (b.by == By::kSumAbove);
-      __syncthreads();
-    }
+  __device__ __forceinline__ Place in_list(const Border& b) const {
+    uint32_t n;   // tokens of the list before the border
+    if (b.by == By::kCount) n = b.n - before_n;
+    else if (b.by == By::kKey) n = first_of(kCap, [&](int i) { return i >= (int)held || (uint32_t)(s.list[i] >> 32) < b.key; });
+    else n = 1 + first_of(kCap, [&](int i) { return i >= (int)held || s.sum[i] >= b.sum; });
     n = min(n, held);
-    Place p{before_n + n, n ? s.sum[n - 1] : before_sum, 0, -1};
+    Place p{before_n + n, before_sum, 0, -1};
     if (n) {
+      p.sum = s.sum[n - 1];
       p.key = (uint32_t)(s.list[n - 1] >> 32);
       p.index = (int)~(uint32_t)s.list[n - 1];
     }
@@ -345,24 +567,24 @@ struct Selector {
   }
 
   // A border among `count` equal values.
-  __device__ __forceinline__ Place in_ties(const Border& b, uint32_t key, uint32_t n0, double sum0, uint32_t count) {
-    const double w = weight_of(key);
-    double n = count;
-    if (b.by == By::kCount) n = (double)(b.n - n0);
-    else if (b.by == By::kKey) n = key >= b.key ? n : 0.0;
-    else if (b.by == By::kSumBelow) n = ceil((b.sum - sum0) / w);
-    else n = floor((b.sum - sum0) / w) + 1.0;
-    const uint32_t k = (uint32_t)fmax(fmin(n, (double)count), b.by == By::kSumAbove ? 1.0 : 0.0);
+  __device__ __forceinline__ Place in_ties(const Border& b, uint32_t key, uint32_t n0, u64 sum0, uint32_t count) {
+    const u64 w = fixed(weight_of(key), unit);
+    uint32_t k = count;
+    if (b.by == By::kCount) k = min(b.n - n0, count);
+    else if (b.by == By::kKey) k = key >= b.key ? count : 0;
+    else if (w) k = (uint32_t)min((b.sum - min(b.sum, sum0) + w - 1) / w, (u64)count);
     Place p{n0 + k, sum0 + k * w, key, -1};
     if (k == 0) return p;
     // The k-th of them by index: each thread counts those of a stretch.
     const int stretch = (V + kThreads - 1) / kThreads;
-    const int lo = min((int64_t)threadIdx.x * stretch, (int64_t)V), hi = min(lo + stretch, V);
+    const int lo = (int)min((int64_t)threadIdx.x * stretch, (int64_t)V), hi = min(lo + stretch, V);
     uint32_t mine = 0;
     for (int i = lo; i < hi; ++i) mine += key_of((float)x[i]) == key;
-    const uint32_t up_to = block_scan(mine, s.wave_u);
+    uint32_t up_to = wave_scan(mine);
+    put_wave(up_to, s.wave_n[1]);
     if (threadIdx.x == 0) s.found = -1;
     __syncthreads();
+    up_to += waves_before(s.wave_n[1]);
     if (up_to >= k && up_to - mine < k) {
       uint32_t at = up_to - mine;
       for (int i = lo; i < hi; ++i) {
@@ -376,43 +598,55 @@ struct Selector {
     return p;
   }
 
-  // A border in the tokens of a range: `count` of them after n0 of sum sum0.
-  __device__ __forceinline__ Place in_range(const Border& b, Range r, uint32_t n0, double sum0, uint32_t count) {
-    while (count > (uint32_t)kCap && r.lo < r.hi) {
+  // Tokens of a range of keys: `count` of them after n0 of sum sum0.
+  struct Part {
+    Range r;
+    uint32_t n0, count;
+    u64 sum0;
+  };
+  // The part of a range with more than kCap tokens that a border is in: at most
+  // kCap, or all equal.  Uses the bins.
+  __device__ __forceinline__ Part narrow(const Border& b, Part p) {
+    while (p.count > (uint32_t)kCap && p.r.lo < p.r.hi) {
       // 2^shift keys a bin, at most kBins of them.
       int shift = 0;
-      while ((r.hi - r.lo) >> shift >= (uint32_t)kBins) ++shift;
-      clear(s.h);
+      while ((p.r.hi - p.r.lo) >> shift >= (uint32_t)kBins) ++shift;
+      s.h.mass[threadIdx.x] = 0;
+      s.h.count[threadIdx.x] = 0;
       __syncthreads();
-      for_logits<1>(x, 0, V, [&](float v, int) {
+      for (int i = threadIdx.x; i < V; i += kThreads) {
+        const float v = (float)x[i];
         const uint32_t k = key_of(v);
-        if (k - r.lo > r.hi - r.lo) return;
-        const uint32_t j = (k - r.lo) >> shift;
+        if (k - p.r.lo > p.r.hi - p.r.lo) continue;
+        const uint32_t j = (k - p.r.lo) >> shift;
         atomicAdd(&s.h.count[j], 1u);
         atomicAdd(&s.h.mass[j], fixed(weight(v, m, c), unit));
-      });
+      }
       __syncthreads();
       const int mine = kBins - 1 - (int)threadIdx.x;
-      cumulate(s.h.count[mine], (double)s.h.mass[mine] / unit, n0, sum0);
-      const int j = b.by == By::kKey ? kBins - 1 - (int)((b.key - r.lo) >> shift) : bin_with(b);
-      n0 = s.count[j];
-      sum0 = s.mass[j];
-      count = s.count[j + 1] - n0;
-      const uint32_t lo = r.lo + ((uint32_t)(kBins - 1 - j) << shift);
-      r = Range{lo, min(r.hi, lo + ((1u << shift) - 1))};
+      cumulate(s.h.count[mine], s.h.mass[mine], p.n0, p.sum0);
+      const int j = b.by == By::kKey ? kBins - 1 - (int)((b.key - p.r.lo) >> shift) : bin_with(b);
+      p.n0 = s.count[j];
+      p.sum0 = s.mass[j];
+      p.count = s.count[j + 1] - p.n0;
+      const uint32_t lo = p.r.lo + ((uint32_t)(kBins - 1 - j) << shift);
+      p.r = Range{lo, min(p.r.hi, lo + ((1u << shift) - 1))};
       __syncthreads();
     }
-    if (count > (uint32_t)kCap) return in_ties(b, r.lo, n0, sum0, count);
-    load(r, n0, sum0);
-    return in_list(b);
+    return p;
   }
 };
+
+// The least sum that is not below p of `sum`, and the least that is above u of it.
+__device__ __forceinline__ u64 below(float p, u64 sum) { return max(__double2ull_ru((double)p * (double)sum), 1ull); }
+__device__ __forceinline__ u64 above(float u, u64 sum) {
+  return __double2ull_rd(fmax((double)u * (double)sum, 0.0)) + 1;
+}
 
 // The row's token, from its histogram: this thread's bin (kBins - 1 - thread) has
 // count tokens of sum mass.
 template <typename T>
-__device__ __forceinline__ void select(const SampleArgs& a, int64_t row, float m, double c, bool greedy,
-                                       uint32_t count, double mass, Shared& s) {
+__device__ __forceinline__ void select(const SampleArgs& a, int64_t row, float m, const Asked& asked, uint32_t count, u64 mass, Shared& s) {
   const T* const x = static_cast<const T*>(a.x) + row * a.ld;
   if (m == -INFINITY) {   // nothing to choose from
     if (threadIdx.x == 0) {
@@ -421,20 +655,17 @@ __device__ __forceinline__ void select(const SampleArgs& a, int64_t row, float m
     }
     return;
   }
-  Selector<T> sel{x, a.V, m, c, a.unit, s, Range{1, 0}, 0, 0, 0.0};
-  sel.cumulate(count, mass, 0, 0.0);
+  Selector<T> sel{x, a.V, m, asked.c, a.unit, s, Range{1, 0}, 0, 0, 0};
+  sel.cumulate(count, mass, 0, 0);
   const uint32_t all = s.count[kBins];
-  const int32_t asked = a.top_k ? a.top_k[row] : a.top_k_all;
-  const float top_p = a.top_p ? a.top_p[row] : a.top_p_all, min_p = a.min_p ? a.min_p[row] : a.min_p_all;
-  // A top_p of 0 leaves the first one, as a greedy row does.
-  const uint32_t k = greedy || top_p <= 0.0f ? 1u : asked > 0 ? min((uint32_t)asked, all) : all;
-  const bool by_k = k < all, by_p = !greedy && top_p < 1.0f, by_min = !greedy && min_p > 0.0f;
+  const float top_p = asked.top_p, min_p = asked.min_p;
+  const uint32_t k = asked.top_k ? min(asked.top_k, all) : all;
+  const bool by_k = k < all, by_p = !asked.greedy && top_p < 1.0f && k > 1, by_min = !asked.greedy && min_p > 0.0f && k > 1;
 
-  // The smallest key of weight min_p: 64 keys of what is left at a time.  Of none
-  // above 1.
+  // The smallest key of weight min_p: 64 keys of what is left at a time.
   uint32_t least = kLowestKey;
   if (by_min) {
-    uint32_t lo = kLowestKey - 1, hi = key_of(m) + (min_p > 1.0f);   // hi has the weight, lo has it not
+    uint32_t lo = kLowestKey - 1, hi = key_of(m);   // hi has the weight, lo has it not
     while (hi - lo > 1) {
       const uint32_t lane = threadIdx.x & 63, span = hi - lo;
       const auto key = [&](uint32_t l) { return lo + (uint32_t)(((u64)span * l + 63) / 64); };
@@ -451,55 +682,70 @@ __device__ __forceinline__ void select(const SampleArgs& a, int64_t row, float m
   // Which borders there are.  Without both of top-k and top-p, one that is bins
   // below that of min-p does not count.
   int bin_first = kBins - 1;
-  if (by_k) bin_first = sel.bin_with(Border{By::kCount, k, 0.0, 0});
-  else if (by_p) bin_first = sel.bin_with(Border{By::kSumBelow, 0, top_p * s.mass[kBins], 0});
+  if (by_k) bin_first = sel.bin_with(Border{By::kCount, k, 0, 0});
+  else if (by_p) bin_first = sel.bin_with(Border{By::kSum, 0, below(top_p, s.mass[kBins]), 0});
   const bool min_first = by_min && !(by_k && by_p) && bin_min < bin_first;
-  // All that the borders can need, if it is little.
   const int last = min_first ? bin_min : bin_first;
-  if (s.count[last + 1] <= (uint32_t)kCap) sel.load(Range{range_of(kBins - 1 - last).lo, kHighestKey}, 0, 0.0);
 
   uint32_t n = all;
-  double sum = s.mass[kBins];
+  u64 sum = s.mass[kBins];
   Place p{};
-  for (int step = 0; step < 5; ++step) {
+  bool whole = false;   // the list has all
+  for (int step = -1; step < 5; ++step) {
     Border b{};
-    if (step == 0) {
-      if (!by_k || min_first) continue;
-      b = Border{By::kCount, k, 0.0, 0};
-    } else if (step == 1) {
-      if (!by_p || min_first || n == 1) continue;
-      b = Border{By::kSumBelow, 0, (double)top_p * sum, 0};
-    } else if (step == 2) {
-      if (!by_min || s.count[bin_min] >= n) continue;   // all that is left is above the bin
-      b = Border{By::kKey, 0, 0.0, least};
-    } else if (step == 3) {
-      if (n == 1) continue;
-      b = Border{By::kSumAbove, 0, (double)a.u[row] * sum, 0};
+    typename Selector<T>::Part part{};
+    bool held = false, ties = false;
+    if (step < 0) {
+      // All that the borders can need, if it is little.
+      part = {Range{range_of(kBins - 1 - last).lo, key_of(m)}, 0, s.count[last + 1], 0};
+      if (part.count > (uint32_t)kCap) continue;
+      whole = true;
     } else {
-      if (n > 1 && p.n <= n) continue;
-      b = Border{By::kCount, n, 0.0, 0};
+      if (step == 0) {
+        if (!by_k || min_first) continue;
+        b = Border{By::kCount, k, 0, 0};
+      } else if (step == 1) {
+        if (!by_p || min_first || n == 1) continue;
+        b = Border{By::kSum, 0, below(top_p, sum), 0};
+      } else if (step == 2) {
+        if (!by_min || s.count[bin_min] >= n) continue;   // all that is left is above the bin
+        b = Border{By::kKey, 0, 0, least};
+      } else if (step == 3) {
+        if (n == 1) continue;
+        b = Border{By::kSum, 0, above(asked.u, sum), 0};
+      } else {
+        if (n > 1 && p.n <= n) continue;
+        b = Border{By::kCount, n, 0, 0};
+      }
+      held = whole;
+      if (!held) {
+        const int j = b.by == By::kKey ? bin_min : sel.bin_with(b);
+        part = {range_of(kBins - 1 - j), s.count[j], s.count[j + 1] - s.count[j], s.mass[j]};
+        // Whatever a border needs is in the list if that holds the border's bin.
+        held = sel.held > 0 && part.r.lo >= sel.range.lo && part.r.hi <= sel.range.hi;
+      }
+      if (!held && part.count > (uint32_t)kCap) {
+        part = sel.narrow(b, part);
+        ties = part.count > (uint32_t)kCap;
+        if (ties) p = sel.in_ties(b, part.r.lo, part.n0, part.sum0, part.count);
+        sel.cumulate(count, mass, 0, 0);   // the row's bins again
+      }
     }
-    const int j = b.by == By::kKey ? bin_min : sel.bin_with(b);
-    const Range r = range_of(kBins - 1 - j);
-    // Whatever a border needs is in the list if that holds the border's bin.
-    if (sel.held > 0 && r.lo >= sel.range.lo && r.hi <= sel.range.hi) {
-      p = sel.in_list(b);
-    } else {
-      p = sel.in_range(b, r, s.count[j], s.mass[j], s.count[j + 1] - s.count[j]);
-      sel.cumulate(count, mass, 0, 0.0);   // the row's bins, where in_range cut one
-    }
+    if (!held && !ties) sel.arrange(sel.gather(part.r), part.r, part.n0, part.sum0);
+    if (step < 0) continue;
+    if (!ties) p = sel.in_list(b);
     if (step < 3 && (p.n < n || step == 0)) {
       n = p.n;
       sum = p.sum;
       if (n < 1) {   // the first one is always kept
         n = 1;
-        sum = 1.0;
+        sum = (u64)a.unit;
       }
     }
   }
   if (threadIdx.x == 0) {
     a.tokens[row] = p.index;
-    a.probs[row] = (float)(sel.weight_of(p.key) / sum);
+    a.probs[row] = (float)(sel.weight_of(p.key) * a.unit / (double)sum);
   }
 }
 
@@ -508,11 +754,11 @@ template <typename T>
 __global__ void __launch_bounds__(kThreads) sample_kernel(SampleArgs a) {
   __shared__ Shared s;
   for (int64_t row = blockIdx.x; row < a.M; row += gridDim.x) {
-    bool greedy;
-    const double c = factor(a, row, &greedy);
-    const float m = histogram(static_cast<const T*>(a.x) + row * a.ld, 0, a.V, c, a.unit, s.h, s.wave_f);
+    const Asked asked = asked_of(a, row);
+    const float m = histogram(static_cast<const T*>(a.x) + row * a.ld, 0, a.V, asked.c, a.unit, s.h, s.wave_f);
+    __syncthreads();
     const int mine = kBins - 1 - (int)threadIdx.x;
-    select<T>(a, row, m, c, greedy, s.h.count[mine], (double)s.h.mass[mine] / a.unit, s);
+    select<T>(a, row, m, asked, s.h.count[mine], s.h.mass[mine], s);
     __syncthreads();
   }
 }
@@ -521,12 +767,12 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(SampleArgs a) {
 template <typename T>
 __global__ void __launch_bounds__(kThreads) sample_histogram_kernel(SampleArgs a) {
   __shared__ Histogram h;
-  __shared__ float part[kWaves];
+  __shared__ float part[2][kWaves];
   const int64_t row = blockIdx.y;
   const int lo = (int)blockIdx.x * a.part, hi = min(lo + a.part, a.V);
-  bool greedy;
-  const double c = factor(a, row, &greedy);
-  const float m = histogram(static_cast<const T*>(a.x) + row * a.ld, lo, hi, c, a.unit, h, part);
+  const Asked asked = asked_of(a, row);
+  const float m = histogram(static_cast<const T*>(a.x) + row * a.ld, lo, hi, asked.c, a.unit, h, part);
+  __syncthreads();
   const int64_t at = row * a.splits + blockIdx.x;
   if (threadIdx.x == 0) a.most[at] = m;
   a.mass[at * kBins + threadIdx.x] = h.mass[threadIdx.x];
@@ -537,22 +783,20 @@ template <typename T>
 __global__ void __launch_bounds__(kThreads) sample_select_kernel(SampleArgs a) {
   __shared__ Shared s;
   const int64_t row = blockIdx.x;
-  bool greedy;
-  const double c = factor(a, row, &greedy);
+  const Asked asked = asked_of(a, row);
+  const float* const most = a.most + row * a.splits;
   float m = -INFINITY;
-  for (int i = 0; i < a.splits; ++i) m = fmaxf(m, a.most[row * a.splits + i]);
+  for (int i = 0; i < a.splits; ++i) m = fmaxf(m, most[i]);
   uint32_t count = 0;
-  double mass = 0.0;
-  const int mine = kBins - 1 - (int)threadIdx.x;
+  u64 mass = 0;
+  const int64_t mine = row * a.splits * kBins + kBins - 1 - (int)threadIdx.x;
   for (int i = 0; i < a.splits; ++i) {
-    const int64_t at = row * a.splits + i;
-    const float here = a.most[at];
-    const uint32_t n = a.count[at * kBins + mine];
-    count += n;
+    count += a.count[mine + (int64_t)i * kBins];
+    const u64 w = a.mass[mine + (int64_t)i * kBins];
     // Each part's sums are relative to its own largest logit.
-    if (n) mass += weight(here, m, c) * ((double)a.mass[at * kBins + mine] / a.unit);
+    mass += most[i] == m || w == 0 ? w : __double2ull_rn((double)w * weight(most[i], m, asked.c));
   }
-  select<T>(a, row, m, c, greedy, count, mass, s);
+  select<T>(a, row, m, asked, count, mass, s);
 }
 
 // Parts of a row: a workgroup for each compute unit, of kMinPart logits or more.
@@ -578,7 +822,7 @@ hipError_t launch(const SampleArgs& a, hipStream_t stream) {
 
 int64_t sample_tokens_workspace(const SampleTokens& c) {
   const int64_t splits = choose_splits(c);
-  return splits == 1 ? 0 : c.M * splits * (kBins * 12 + 16);
+  return splits == 1 ? 0 : c.M * splits * (kBins * 12 + 4);
 }
 
 hipError_t launch_sample_tokens(const SampleTokens& c, hipStream_t stream) {

@@ -33,4 +33,46 @@ __device__ __forceinline__ float wave_sum(float x) {
   return wave_reduce(x, [](float a, float b) { return a + b; });
 }
 
+// Sums over the lanes up to each, in the vector ALU; exact for integers.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t dpp_or_0(uint32_t x) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xF, false);
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ unsigned long long dpp_or_0(unsigned long long x) {
+  return (unsigned long long)dpp_or_0<CTRL, ROWS>((uint32_t)(x >> 32)) << 32 | dpp_or_0<CTRL, ROWS>((uint32_t)x);
+}
+template <typename V>
+__device__ __forceinline__ V wave_scan(V x) {
+  x += dpp_or_0<0x111, 0xF>(x);   // row_shr 1, 2, 4, 8: within rows of 16
+  x += dpp_or_0<0x112, 0xF>(x);
+  x += dpp_or_0<0x114, 0xF>(x);
+  x += dpp_or_0<0x118, 0xF>(x);
+  x += dpp_or_0<0x142, 0xA>(x);   // lane 15 of a row to the next, into rows 1 and 3
+  x += dpp_or_0<0x143, 0xC>(x);   // lane 31 to the upper half
+  return x;
+}
+
+// The value of lane ^ J.
+template <int J>
+__device__ __forceinline__ uint32_t lane_xor(uint32_t x) {
+  static_assert(J == 1 || J == 2 || J == 4 || J == 8 || J == 16 || J == 32);
+  const int v = (int)x;
+  if constexpr (J == 1) return (uint32_t)__builtin_amdgcn_update_dpp(v, v, 0xB1, 0xF, 0xF, true);
+  if constexpr (J == 2) return (uint32_t)__builtin_amdgcn_update_dpp(v, v, 0x4E, 0xF, 0xF, true);
+  if constexpr (J == 4) {   // the mirror of eight, of which each quad is mirrored back
+    const int m = __builtin_amdgcn_update_dpp(v, v, 0x141, 0xF, 0xF, true);
+    return (uint32_t)__builtin_amdgcn_update_dpp(m, m, 0x1B, 0xF, 0xF, true);
+  }
+  if constexpr (J == 8) return (uint32_t)__builtin_amdgcn_update_dpp(v, v, 0x128, 0xF, 0xF, true);   // row_ror 8
+  if constexpr (J == 16) {
+    const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    return threadIdx.x & 16 ? r[0] : r[1];
+  }
+  if constexpr (J == 32) {
+    const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    return threadIdx.x & 32 ? r[0] : r[1];
+  }
+}
+
 }  // namespace dptq
