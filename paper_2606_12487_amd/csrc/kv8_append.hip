@@ -22,11 +22,15 @@
 // on a compute unit.
 //
 // With rotary positions (kv8_append_kernel<D, true>) the keys are rotated and
-// rounded to fp16 first, in the same registers: a workgroup of K loads the other
-// channel of each pair too (a second load of bytes that its neighbour loads) and
-// computes its own angles.  Further workgroups rotate the queries, 64 tokens of
-// a sequence each, a token and a part of its heads to a wave.  The codes are
-// those of rotary and kv8_append one after the other, bit for bit.
+// rounded to fp16 first, and wait in LDS for the page's scale: a workgroup of K
+// loads the other channel of each pair too (a second load of bytes that its
+// neighbour loads) and computes its own angles.  Further workgroups rotate the
+// queries, a token and a part of its heads to a wave.  The codes are those of
+// rotary and kv8_append one after the other, bit for bit.  The queries' way is
+// bound by bytes, and so by the loads in flight, which the kernel's registers
+// limit: three workgroups on a compute unit (two at 256 channels).  4500 tokens
+// of three prompts with 64 heads of queries take 40 us (4.2 TB/s; 60 us with the
+// keys' loops unrolled, at two workgroups), a token for each of 64 sequences 10.2.
 #include "internal.h"
 #include "kv8_device.h"
 #include "rotary_device.h"
@@ -76,17 +80,18 @@ __device__ __forceinline__ void rotate_q(const RotaryQ& a, const KvSeq& s, int s
   }
 }
 
-// Octet v (channels c to c + 7) of the key row at head, at position p, rotated.
-__device__ __forceinline__ uint4 rotate_octet(const Rotary& r, uint4 v, const __half* head, int c, int p) {
+// Octet v (channels c to c + 7) of the key row at head, of the token at position
+// p, rotated; freq: the frequencies of its channels.
+__device__ __forceinline__ uint4 rotate_octet(const Rotary& r, uint4 v, const __half* head, int c, int p,
+                                              const double (&freq)[8]) {
   if (c >= 2 * r.half) return v;
   float f[8], g[8], y[8];
   unpack8(v, f);
-  const bool second = c >= r.half;   // of whole octets' pairs
   if (r.interleaved) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) g[j] = f[j ^ 1];
   } else if (r.wide) {
-    unpack8(*reinterpret_cast<const uint4*>(head + (second ? c - r.half : c + r.half)), g);
+    unpack8(*reinterpret_cast<const uint4*>(head + (c >= r.half ? c - r.half : c + r.half)), g);
   } else {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
@@ -99,10 +104,9 @@ __device__ __forceinline__ uint4 rotate_octet(const Rotary& r, uint4 v, const __
     const int ch = c + j;
     y[j] = f[j];
     if (ch >= 2 * r.half) continue;   // an octet that the pairs end in
-    const bool upper = r.interleaved ? ch & 1 : ch >= r.half;
-    const int i = r.interleaved ? ch >> 1 : upper ? ch - r.half : ch;
-    const float2 t = rotary_angle(p, r.inv_freq[i], r.scale);
-    y[j] = upper ? rotary_second(g[j], f[j], t) : rotary_first(f[j], g[j], t);
+    const bool second = r.interleaved ? ch & 1 : ch >= r.half;
+    const float2 t = rotary_angle(p, freq[j], r.scale);
+    y[j] = second ? rotary_second(g[j], f[j], t) : rotary_first(f[j], g[j], t);
   }
   return pack8(y);
 }
@@ -136,21 +140,76 @@ __device__ __forceinline__ uint32_t slot_mask(int first, int lo, int hi) {
   return m;
 }
 
+// The keys of a page, rotated, into the cache: rounded to fp16 they wait in LDS
+// (stage) for the page's scale.  Loops that are not unrolled keep the kernel's
+// registers, which the workgroups of the queries have too, few.
+template <int D>
+__device__ __forceinline__ void rotary_page(const Rotary& r, const KvSeq& q, int blk, int lo, int hi, const __half* head,
+                                            int64_t ld, uint8_t* codes, float* scale, float had, int octet,
+                                            int first_slot, int slot_step, const double (&freq)[8], uint4* stage,
+                                            float* part) {
+  constexpr int kPer = kPage * (D / 8) / kThreads;
+  const int tid = threadIdx.x, c = 8 * octet;
+  const bool fresh = lo == 0;
+  float top = 0.0f;
+#pragma unroll 1
+  for (int i = 0; i < kPer; ++i) {
+    const int slot = first_slot + i * slot_step;
+    if (slot < lo || slot >= hi) continue;
+    const int p = blk * kPage + slot;
+    const __half* const row = head + ((int64_t)q.first_row + ((int64_t)p - q.start)) * ld;
+    const uint4 v = rotate_octet(r, *reinterpret_cast<const uint4*>(row + c), row, c, p, freq);
+    float f[8];
+    unpack8(v, f);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(f[j]));
+    stage[i * kThreads + tid] = v;
+  }
+  top = wave_max(top);
+  if ((tid & 63) == 0) part[tid / 64] = top;
+  __syncthreads();   // and everyone has read the scale
+#pragma unroll
+  for (int i = 0; i < kThreads / 64; ++i) top = fmaxf(top, part[i]);
+  const float s = fmaxf(__uint_as_float((uint32_t)(scale_exp(top) + 127) << 23), had);
+  const bool grew = !fresh && s > had;
+  const float ratio = had / s, inv = 1.0f / s;   // exact for powers of two
+  if (tid == 0) *scale = s;
+#pragma unroll 1
+  for (int i = 0; i < kPer; ++i) {
+    const int slot = first_slot + i * slot_step;
+    uint2* const dst = reinterpret_cast<uint2*>(codes + slot * D + c);
+    if (slot >= lo && slot < hi) {
+      float f[8];
+      unpack8(stage[i * kThreads + tid], f);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) f[j] *= inv;
+      *dst = make_uint2(to_e4m3<true>(f[2], f[3], to_e4m3<false>(f[0], f[1], 0)),
+                        to_e4m3<true>(f[6], f[7], to_e4m3<false>(f[4], f[5], 0)));
+    } else if (slot >= hi) {
+      if (fresh) *dst = make_uint2(0, 0);
+    } else if (grew) {
+      const uint2 o = *dst;
+      *dst = make_uint2(rescale4(o.x, ratio), rescale4(o.y, ratio));
+    }
+  }
+  __syncthreads();   // part is free again
+}
+
 template <int D, bool ROTARY>
-__global__ void __launch_bounds__(kThreads) kv8_append_kernel(AppendArgs a, RotaryQ rq) {
+__global__ void __launch_bounds__(kThreads, !ROTARY ? 1 : D == 256 ? 2 : 3) kv8_append_kernel(AppendArgs a, RotaryQ rq) {
   constexpr int kOctets = D / 8;                       // of channels
   constexpr int kPer = kPage * kOctets / kThreads;     // tokens x octets of a thread
   constexpr int kRow = kPage + 4;                      // of the staged V codes, a channel a row
   __shared__ float part[kThreads / 64];
-  __shared__ __align__(8) uint8_t stage[D * kRow];
-  const int b = blockIdx.z, head = blockIdx.y >> 1;
+  // The staged V codes, or the page's rotated keys, or a token's angles in each wave.
+  __shared__ __align__(16) uint8_t stage[ROTARY ? kPage * D * 2 : D * kRow];
+  const int b = blockIdx.z, head = (int)blockIdx.y >> 1;
   const bool is_v = blockIdx.y & 1;
   const KvSeq q = kv_seq(a.cu, a.lengths, b, a.T);
   if constexpr (ROTARY) {
     if ((int)blockIdx.y >= 2 * a.heads) {
-      __shared__ float2 angles[kThreads / 64][D / 2];
-      float2* const mine = angles[threadIdx.x >> 6];
-      const int slice = blockIdx.y - 2 * a.heads, slices = gridDim.y - 2 * a.heads;
+      float2* const mine = reinterpret_cast<float2*>(stage) + (threadIdx.x >> 6) * (D / 2);
+      const int slice = (int)blockIdx.y - 2 * a.heads, slices = (int)gridDim.y - 2 * a.heads;
       if (rq.r.interleaved)
         rq.r.wide ? rotate_q<true, true>(rq, q, slice, slices, mine) : rotate_q<true, false>(rq, q, slice, slices, mine);
       else
@@ -168,6 +227,18 @@ __global__ void __launch_bounds__(kThreads) kv8_append_kernel(AppendArgs a, Rota
   // ones, which make one LDS store of a channel.
   const int octet = tid % kOctets, first_slot = tid / kOctets * (is_v ? kPer : 1);
   const int slot_step = is_v ? 1 : kPage / kPer;
+  // The frequencies of the octet's channels, ahead of the table and the rows.
+  double freq[8] = {};
+  if constexpr (ROTARY) {
+    if (!is_v) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int ch = 8 * octet + j;
+        const int pair = rq.r.interleaved ? ch >> 1 : ch >= rq.r.half ? ch - rq.r.half : ch;
+        if (ch < 2 * rq.r.half) freq[j] = rq.r.inv_freq[pair];
+      }
+    }
+  }
   for (int blk = begin / kPage + blockIdx.x; blk <= last_block; blk += gridDim.x) {
     const int page = a.table[(int64_t)b * a.max_pages + blk];
     if ((uint32_t)page >= (uint32_t)a.num_pages) continue;
@@ -179,6 +250,14 @@ __global__ void __launch_bounds__(kThreads) kv8_append_kernel(AppendArgs a, Rota
     const __half* const rows = a.x[is_v] + (int64_t)head * D + 8 * octet;
     const float had = fresh ? 0.0f : a.scales[is_v][at];
 
+    if constexpr (ROTARY) {
+      if (!is_v) {
+        rotary_page<D>(rq.r, q, blk, lo, hi, rows - 8 * octet, a.ld[0], codes, a.scales[0] + at, had, octet, first_slot,
+                       slot_step, freq, reinterpret_cast<uint4*>(stage), part);
+        continue;
+      }
+    }
+
     // The new tokens' values and their largest magnitude.
     uint4 v[kPer];
     float top = 0.0f;
@@ -189,18 +268,6 @@ __global__ void __launch_bounds__(kThreads) kv8_append_kernel(AppendArgs a, Rota
       if (slot >= lo && slot < hi) {
         const int64_t t = (int64_t)q.first_row + ((int64_t)blk * kPage + slot - q.start);
         v[i] = *reinterpret_cast<const uint4*>(rows + t * a.ld[is_v]);
-      }
-    }
-    if constexpr (ROTARY) {
-      if (!is_v) {
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-          const int slot = first_slot + i * slot_step;
-          if (slot < lo || slot >= hi) continue;
-          const int p = blk * kPage + slot;
-          const int64_t t = (int64_t)q.first_row + ((int64_t)p - q.start);
-          v[i] = rotate_octet(rq.r, v[i], rows - 8 * octet + t * a.ld[0], 8 * octet, p);
-        }
       }
     }
 #pragma unroll
@@ -344,10 +411,10 @@ hipError_t launch_rotary_kv8_append(const Kv8Cache& c, const RotaryCall& r, cons
   rq.ld_out = r.ld_q_out;
   rq.heads = r.heads;
   rq.parts = (int)(((int64_t)r.heads * rq.r.units + 64 * kRotaryUnits - 1) / (64 * kRotaryUnits));
-  // Slices of the queries of up to 64 tokens: as many as give a wave four
-  // tokens' parts.
+  // A wave to each token and part; behind the pages' workgroups, whose chains of
+  // loads are the longer ones (queries first: 46 us for 40, 4500 tokens).
   const int64_t waves = (max_new < 64 ? max_new : 64) * rq.parts;
-  const int64_t slices = (waves + 15) / 16;
+  const int64_t slices = (waves + kThreads / 64 - 1) / (kThreads / 64);
   const dim3 grid(tiles((max_new + kPage - 2) / kPage + 1), (unsigned)(2 * c.kv_heads + (slices < 1024 ? slices : 1024)),
                   (unsigned)c.B);
   return launch<true>(a, rq, c.head_dim, grid, stream);

@@ -26,6 +26,7 @@ struct Rotary {
   bool wide;                // the pairs' octets of channels are whole: 16-byte loads
   int units;                // of a head: an octet of pairs (wide) or a pair, and what is only copied
   uint32_t units_inv;       // ceil(2^32 / units); 0 for one unit
+  uint32_t half_inv;        // the same of half
 };
 // rotary_dim even, at most D; D a multiple of 8, at most kMaxRotaryHead (rotary.hip).
 Rotary make_rotary(const double* inv_freq, int D, int rotary_dim, bool interleaved, float scale);
@@ -51,6 +52,11 @@ __device__ __forceinline__ float2 rotary_angle(int p, double f, float scale) {
   const int quadrant = (int)k;                        // -2 .. 2
   const float a = quadrant & 1 ? s : c, b = quadrant & 1 ? c : s;   // |cos|, |sin|
   return make_float2(scale * ((quadrant + 1) & 2 ? -a : a), scale * (quadrant & 2 ? -b : b));
+}
+
+// i / n for i n < 2^32, with inv = ceil(2^32 / n), 0 for n = 1.
+__device__ __forceinline__ int rotary_divide(int i, uint32_t inv) {
+  return inv ? (int)__umulhi((uint32_t)i, inv) : i;
 }
 
 // The empty asm keeps a result an fp32 value: the backend may fold an FMA and the
@@ -112,7 +118,7 @@ __device__ __forceinline__ void rotary_units(const Rotary& r, const float2* cs, 
 #pragma unroll
   for (int n = 0; n < N; ++n) {
     const int i = first + 64 * n + lane;
-    const int h = r.units_inv ? (int)__umulhi((uint32_t)i, r.units_inv) : i;   // i / units
+    const int h = rotary_divide(i, r.units_inv);
     unit[n] = i < total ? i - h * r.units : -1;
     const bool second = h >= a.heads;
     const int64_t at = (int64_t)(second ? h - a.heads : h) * r.D;
