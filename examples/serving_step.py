@@ -1,7 +1,8 @@
 """Serving with dptq: prompts of several lengths and then single tokens through a
 small random transformer, with the norm that gives 8-bit activations, the
-quantized linears, the 8-bit paged KV cache with its attention, and the answers'
-log probabilities with their alternatives.
+quantized linears, rotary positions and the 8-bit paged KV cache with its
+attention, the gated feed-forward block, and answers drawn from the logits with
+their log probabilities and alternatives.
 
     python examples/serving_step.py          # needs an MI355X and the built library
 """
@@ -41,8 +42,11 @@ class Model:
         g.manual_seed(seed)
 
         def linear(n, k, had_size):
-            w = torch.randn((n, k), generator=g, device="cuda") * k ** -0.5
-            return dptq.prepare_weights(w, had_size)
+            return dptq.prepare_weights(torch.randn((n, k), generator=g, device="cuda") * k ** -0.5, had_size)
+
+        def gate_and_up():
+            w = torch.randn((2 * FFN, HIDDEN), generator=g, device="cuda") * HIDDEN ** -0.5
+            return dptq.prepare_weights(dptq.gate_up_rows(*w.chunk(2)), 1)
 
         def norm():
             return (1 + 0.1 * torch.randn(HIDDEN, generator=g, device="cuda")).half()
@@ -52,8 +56,9 @@ class Model:
         # Linears behind a norm take its codes as they are (had_size 1: nothing to undo), the others rotate.
         self.layers = [dict(norm1=norm(), qkv=linear((HEADS + 2 * KV_HEADS) * D, HIDDEN, 1),
                             out=linear(HIDDEN, HEADS * D, HEADS * D), norm2=norm(),
-                            up=linear(2 * FFN, HIDDEN, 1), down=linear(HIDDEN, FFN, FFN)) for _ in range(LAYERS)]
+                            up=gate_and_up(), down=linear(HIDDEN, FFN, FFN)) for _ in range(LAYERS)]
         self.norm, self.head = norm(), linear(VOCAB, HIDDEN, 1)
+        self.inv_freq = dptq.rotary_inv_freq(D)
 
     def step(self, tokens, cu, most, seqs):
         """Logits [T, VOCAB] of the new tokens, whose keys and values go into the caches."""
@@ -64,30 +69,32 @@ class Model:
                                                    residual=None if x is None else h)
             qkv = dptq.qlinear(codes, scales, 8, *layer["qkv"]).unflatten(1, (HEADS + 2 * KV_HEADS, D))
             q, k, v = qkv.split([HEADS, KV_HEADS, KV_HEADS], dim=1)
-            dptq.kv8_append(k, v, cu, seqs.lengths, seqs.table, cache, max_new=most)
+            q = dptq.rotary_kv8_append(q, k, v, cu, seqs.lengths, seqs.table, cache, self.inv_freq, max_new=most)
             y, _ = dptq.kv8_attention(q, cu, seqs.lengths, seqs.table, cache, window=self.window, sinks=self.sinks,
                                       max_q=most)
             codes, scales = dptq.rotate_quant(y.flatten(1), HEADS * D, 8)
             x = dptq.qlinear(codes, scales, 8, *layer["out"])
             codes, scales, h = dptq.rms_norm_quant(x, layer["norm2"], 1e-5, residual=h, sum=h)
-            gate, up = dptq.qlinear(codes, scales, 8, *layer["up"]).chunk(2, dim=1)
-            y = torch.nn.functional.silu(gate) * up
+            y = dptq.qlinear_gated(codes, scales, 8, *layer["up"])
             codes, scales = dptq.rotate_quant(y, FFN, 8)
             x = dptq.qlinear(codes, scales, 8, *layer["down"])
         codes, scales, _ = dptq.rms_norm_quant(x, self.norm, 1e-5, residual=h, sum=h)
         return dptq.qlinear(codes, scales, 8, *self.head)
 
 
-def generate(model, prompts, new_tokens, top=5):
-    """Greedy answers to the prompts (lists of token ids): per sequence its tokens, and per step the log
-    probabilities, entropies and alternatives."""
+def generate(model, prompts, new_tokens, top=5, seed=0, temperature=0.0, **limits):
+    """Answers to the prompts (lists of token ids), greedy or drawn (temperature; top_k, top_p and min_p): per sequence
+    its tokens, and per step the log probabilities, entropies and alternatives."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
     seqs = Sequences(len(prompts), max(len(p) for p in prompts) + new_tokens)
     cu, most = seqs.extend([len(p) for p in prompts])
     tokens = torch.tensor([t for p in prompts for t in p], device="cuda")
     logits = model.step(tokens, cu, most, seqs)[cu[1:].long() - 1]      # of each prompt's last token
     answers, steps = [], []
     for i in range(new_tokens):
-        tokens = logits.argmax(1)
+        uniform = torch.rand((len(prompts),), generator=g, device="cuda")
+        tokens, _ = dptq.sample_tokens(logits, uniform, temperature=temperature, **limits)
         answers.append(tokens)
         steps.append(dptq.token_logprobs(logits, tokens, top=top))
         if i + 1 < new_tokens:
@@ -100,7 +107,7 @@ def main():
     g = torch.Generator()
     g.manual_seed(1)
     prompts = [torch.randint(0, VOCAB, (n,), generator=g).tolist() for n in (5, 130, 61)]
-    answers, steps = generate(Model(window=96, sinks=4), prompts, 8)
+    answers, steps = generate(Model(window=96, sinks=4), prompts, 8, temperature=0.7, top_p=0.9)
     for b, prompt in enumerate(prompts):
         print(f"prompt of {len(prompt)} tokens -> {answers[b].tolist()}")
         for logprob, entropy, top, ids in steps[:2]:
