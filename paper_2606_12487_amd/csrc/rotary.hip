@@ -81,6 +81,7 @@ hipError_t launch_rotary(const RotaryCall& c, hipStream_t stream) {
   const bool few = c.T * units < (int64_t)device_cus() * 4 * 64 * 4;
   a.parts = (int)((units + (few ? 63 : 255)) / (few ? 64 : 256));
   a.waves = c.T * a.parts;
+  if ((a.waves + kWaves - 1) / kWaves > 0x7FFFFFFF) return hipErrorInvalidValue;
   if (few) launch_n<1>(a, stream);
   else launch_n<4>(a, stream);
   return hipGetLastError();

@@ -24,6 +24,21 @@
 // the sums would change one token in a hundred.  2^t = 2^n (1 + f q(f)) with n
 // the nearest integer and q the interpolant of degree 6 at Chebyshev's nodes on
 // [-1/2, 1/2], to 1.2e-10, and alternating, so that sums are closer.
+//
+// A row to a workgroup where rows are many; few rows are cut into parts whose
+// histograms one launch forms, relative to their own largest logit, and a second
+// joins.  What bounds it: 256 rows of 100003 fp32 take 60 us, of which the
+// histogram is 36 (28 without the weights; some 30 vector instructions a logit,
+// 13 of them of 64 bits) and the gathering of the border's bin 15 (a second read
+// at 6.8 TB/s).  64 rows of 131072 fp16 that ask for different things take 37 us,
+// 12 for the histograms of four parts each and 22 for the second launch on one
+// compute unit a row: joining and summing the bins 2.5, gathering 8, sorting and
+// summing the list 2, and up to four borders in turn, 0.6 each.  One row of 32000
+// takes 21 us, the same chain.  Dropped, each measured: the gathering shared by a
+// row's workgroups, with fences of the device's scope (160 us) or accesses of it
+// (56 us: four trips to memory); three loads ahead (registers spill, 39 us); a
+// bitonic sort alone (64 rows: 51 us); loops over a chunk's vectors unrolled (the
+// code is 50 KB instead of 20 and comes into the instruction cache first: 54 us).
 #include "internal.h"
 #include "wave_device.h"
 
@@ -33,7 +48,8 @@ namespace {
 constexpr int kThreads = 1024, kWaves = kThreads / 64;
 constexpr int kBinBits = 10, kBins = 1 << kBinBits;   // one a thread
 constexpr int kCap = 2048;        // tokens that are sorted at once
-constexpr int kMinPart = 16384;    // logits of a part of a row, at least
+constexpr int kMinPart = 16384;   // logits of a part of a row, at least
+constexpr int kXcds = 8;
 
 // Values as integers in their order; -0 is 0.
 constexpr uint32_t kLowestKey = 0x00800000u;   // of -FLT_MAX; what is not masked is this or above
@@ -125,6 +141,11 @@ struct Reader {
   // Vectors [at, at + kSpan); -inf for those that there are not.
   __device__ __forceinline__ void load(int at, Chunk& c) const {
     const uint4* const p = reinterpret_cast<const uint4*>(x + first);
+    if (at + kSpan <= vectors) {
+#pragma unroll
+      for (int n = 0; n < kLoads; ++n) c.v[n] = p[at + n * kThreads + (int)threadIdx.x];
+      return;
+    }
 #pragma unroll
     for (int n = 0; n < kLoads; ++n) {
       const int i = at + n * kThreads + (int)threadIdx.x;
@@ -179,6 +200,48 @@ __device__ __forceinline__ float value_at(uint4 v, int j) {
   if constexpr (sizeof(T) == 2) return __half2float(__ushort_as_half((unsigned short)(j & 1 ? w >> 16 : w)));
   else return __uint_as_float(w);
 }
+
+// Which values of a vector lie in [least, most], as bits; element(b): which value
+// a bit is.  NaN does not; -0 is 0.
+template <typename T>
+struct Within {
+  float least, most;
+  __device__ __forceinline__ Within(float lo, float hi) : least(lo), most(hi) {}
+  __device__ __forceinline__ uint32_t marks(uint4 v) const {
+    uint32_t m = 0;
+    values<T>(v, [&](float e, int j) { m |= e >= least && e <= most ? 1u << j : 0u; });
+    return m;
+  }
+  __device__ __forceinline__ static int element(int b) { return b; }
+};
+// fp16: two at a time, those that clamping to the bounds (rounded into the range)
+// leaves as they are.
+template <>
+struct Within<__half> {
+  typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
+  typedef unsigned short ushort2_t __attribute__((ext_vector_type(2)));
+  half2_t least, most;
+  __device__ __forceinline__ Within(float lo, float hi) {
+    const unsigned short l = __half_as_ushort(__float2half_ru(lo)), h = __half_as_ushort(__float2half_rd(hi));
+    const ushort2_t a = {l, l}, b = {h, h};
+    least = __builtin_bit_cast(half2_t, a);
+    most = __builtin_bit_cast(half2_t, b);
+  }
+  __device__ __forceinline__ uint32_t marks(uint4 v) const {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    const ushort2_t one = {1, 1};
+    uint32_t out = 0;   // bits k and 16 + k: the values of dword k lie outside
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const half2_t e = __builtin_bit_cast(half2_t, w[k]) + (half2_t)(_Float16)0;
+      const half2_t c = __builtin_elementwise_min(__builtin_elementwise_max(e, least), most);
+      const ushort2_t d = __builtin_bit_cast(ushort2_t, __builtin_bit_cast(uint32_t, c) ^ __builtin_bit_cast(uint32_t, e));
+      out |= __builtin_bit_cast(uint32_t, __builtin_elementwise_min(d, one)) << k;
+    }
+    return ~out & 0x000F000Fu;
+  }
+  __device__ __forceinline__ static int element(int b) { return 2 * (b & 3) + (b >> 4); }
+};
 
 struct SampleArgs {
   const void* x;
@@ -448,11 +511,10 @@ struct Selector {
     __syncthreads();   // the list's readers are done
     if (threadIdx.x == 0) s.n = 0;
     __syncthreads();
-    const float least = value_of(r.lo), most = value_of(r.hi);
+    const Within<T> within(value_of(r.lo), value_of(r.hi));
     // A thread marks what it has of a vector that begins at index i.
     const auto take = [&](uint4 v, int i) {
-      uint32_t mine = 0;
-      values<T>(v, [&](float e, int j) { mine |= e >= least && e <= most ? 1u << j : 0u; });
+      uint32_t mine = within.marks(v);
       if (!mine) return;
       // One addition for each lane as it is: the compiler would sum up a uniform
       // address's over the wave, which takes longer for the few lanes here.
@@ -460,21 +522,29 @@ struct Selector {
       asm("v_mov_b32 %0, 0" : "=v"(offset));
       int to = atomicAdd(&s.n + offset, __popc(mine));
       for (; mine; mine &= mine - 1, ++to) {
-        const int j = __ffs((int)mine) - 1;
+        const int j = Within<T>::element(__ffs((int)mine) - 1);
         if (to < kCap) s.list[to] = (u64)key_of(value_at<T>(v, j)) << 32 | (uint32_t)~(i + j);
       }
     };
     using R = Reader<T>;
     const R reader(x, 0, V);
-    typename R::Chunk now, next;
+    const auto take_all = [&](const typename R::Chunk& c, int at) {
+#pragma unroll
+      for (int n = 0; n < R::kLoads; ++n)
+        take(c.v[n], reader.first + (at + n * kThreads + (int)threadIdx.x) * R::kEach);
+    };
+    typename R::Chunk even, odd;   // one on its way while the other is taken
     int i;
     const uint4 ends = reader.ends(i);
-    reader.load(0, now);
+    reader.load(0, even);
     take(ends, i);
-    for (int at = 0; at < reader.vectors; at += R::kSpan) {
-      if (at + R::kSpan < reader.vectors) reader.load(at + R::kSpan, next);
-      reader.each(now, at, take);
-      now = next;
+    for (int at = 0; at < reader.vectors; at += 2 * R::kSpan) {
+      const int next = at + R::kSpan;
+      if (next < reader.vectors) reader.load(next, odd);
+      take_all(even, at);
+      if (next >= reader.vectors) break;
+      if (next + R::kSpan < reader.vectors) reader.load(next + R::kSpan, even);
+      take_all(odd, next);
     }
     __syncthreads();
     return min(s.n, kCap);
@@ -671,7 +741,7 @@ __device__ __forceinline__ void select(const SampleArgs& a, int64_t row, float m
     uint32_t lo = kLowestKey - 1, hi = key_of(m);   // hi has the weight, lo has it not
     while (hi - lo > 1) {
       const uint32_t lane = threadIdx.x & 63, span = hi - lo;
-      const auto key = [&](uint32_t l) { return lo + (uint32_t)(((u64)span * l + 63) / 64); };
+      const auto key = [&](uint32_t l) { return lo + (span >> 6) * l + (((span & 63) * l + 63) >> 6); };   // + span l / 64
       const u64 yes = __ballot(sel.weight_of(key(lane + 1)) >= (double)min_p);
       const uint32_t first = yes ? (uint32_t)__ffsll((long long)yes) - 1 : 63;
       const uint32_t next = key(first + 1);
@@ -771,12 +841,17 @@ template <typename T>
 __global__ void __launch_bounds__(kThreads) sample_histogram_kernel(SampleArgs a) {
   __shared__ Histogram h;
   __shared__ float part[2][kWaves];
-  const int64_t row = blockIdx.y;
-  const int lo = (int)blockIdx.x * a.part, hi = min(lo + a.part, a.V);
+  // A row's parts on the XCD (workgroup mod 8) that its second launch runs on,
+  // whose L2 then has their histograms and the row (64 rows of 131072 in four
+  // parts: 12 us for 13, and the second launch reads them in 1.3 us for 1.9).
+  const int turn = (int)blockIdx.x / kXcds, split = turn % a.splits;
+  const int64_t row = (int64_t)(turn / a.splits) * kXcds + blockIdx.x % kXcds;
+  if (row >= a.M) return;
+  const int lo = split * a.part, hi = min(lo + a.part, a.V);
   const Asked asked = asked_of(a, row);
   const float m = histogram(static_cast<const T*>(a.x) + row * a.ld, lo, hi, asked.c, a.unit, h, part);
   __syncthreads();
-  const int64_t at = row * a.splits + blockIdx.x;
+  const int64_t at = row * a.splits + split;
   if (threadIdx.x == 0) a.most[at] = m;
   a.mass[at * kBins + threadIdx.x] = h.mass[threadIdx.x];
   a.count[at * kBins + threadIdx.x] = h.count[threadIdx.x];
@@ -814,7 +889,8 @@ hipError_t launch(const SampleArgs& a, hipStream_t stream) {
     sample_kernel<T><<<(unsigned)(a.M < 65535 ? a.M : 65535), kThreads, 0, stream>>>(a);
     return hipGetLastError();
   }
-  sample_histogram_kernel<T><<<dim3((unsigned)a.splits, (unsigned)a.M), kThreads, 0, stream>>>(a);
+  const unsigned grid = (unsigned)((a.M + kXcds - 1) / kXcds * kXcds * a.splits);
+  sample_histogram_kernel<T><<<grid, kThreads, 0, stream>>>(a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   sample_select_kernel<T><<<(unsigned)a.M, kThreads, 0, stream>>>(a);

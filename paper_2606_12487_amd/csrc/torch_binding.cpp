@@ -11,6 +11,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/core/DeviceGuard.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -433,6 +434,7 @@ PyObject* gated(PyObject* o_codes, PyObject* o_as, int32_t bits, PyObject* o_w, 
   same_device(w, "w", codes, "codes");
   same_device(ws, "w_scales", codes, "codes");
   const int32_t act = gate_activation(o_act);
+  const c10::DeviceGuard on(codes.device());
   Out y(o_y, "y", at::kHalf, {M, F}, codes);
   allocate(y);
   same_device(y.t, "y", codes, "codes");
@@ -468,6 +470,7 @@ PyObject* qlinear_gated_fp6(PyObject* const* a) {
   same_device(w6, "w_fp6", a6, "a_fp6");
   same_device(ws, "w_scales", a6, "a_fp6");
   const int32_t act = gate_activation(a[8]);
+  const c10::DeviceGuard on(a6.device());
   Out y(a[7], "y", at::kHalf, {M, F}, a6);
   allocate(y);
   same_device(y.t, "y", a6, "a_fp6");
@@ -730,6 +733,7 @@ PyObject* rotary(PyObject* const* a) {
   const int64_t Hkv = keys ? k.size(1) : 0;
   if (keys) same_device(k, "k", q, "q");
   if (H < 1 || H > 8192 || Hkv > 8192 || D > 8192) fail(PyExc_ValueError, "q and k must have 1 to 8192 heads");
+  const c10::DeviceGuard on(q.device());
   const at::Tensor& positions = tensor_of(a[2], "positions", at::kInt, {T});
   same_device(positions, "positions", q, "q");
   const at::Tensor& f = frequencies(a[3], D, q, "q");
@@ -757,6 +761,7 @@ PyObject* rotary_kv8_append(PyObject* const* a) {
   same_device(k, "k", c.k, "k_pages");
   same_device(v, "v", c.k, "k_pages");
   if (H < 1 || H > 8192 || c.heads > 8192) fail(PyExc_ValueError, "q must have 1 to 8192 heads");
+  const c10::DeviceGuard on(q.device());
   const at::Tensor& f = frequencies(a[10], c.D, q, "q");
   const int64_t max_new = size_hint(a[13], "max_new");
   RowsOut q_out(a[14], "q_out", T, H, c.D, q, "q");
@@ -803,41 +808,6 @@ PyObject* kv8_attention(PyObject* const* a) {
   return tuple(out, lse);
 }
 
-// token_logprobs(logits, tokens, top, logprobs, entropy, top_logprobs, top_ids)
-PyObject* token_logprobs(PyObject* const* a) {
-  if (!THPVariable_Check(a[0])) fail(PyExc_TypeError, "logits must be a torch.Tensor");
-  const at::ScalarType type = THPVariable_Unpack(a[0]).scalar_type();
-  const bool half = type == at::kHalf;
-  if (!half && type != at::kFloat) fail(PyExc_TypeError, "logits must have dtype torch.float16 or torch.float32");
-  const at::Tensor& x = gpu_tensor(a[0], "logits", half ? at::kHalf : at::kFloat);
-  two_d(x, "logits must be 2-D [M, V]");
-  const int64_t M = x.size(0), V = x.size(1);
-  const int64_t ld = M > 1 ? x.stride(0) : V;
-  if ((V > 1 && x.stride(1) != 1) || ld < V) fail(PyExc_ValueError, "logits must have dense rows");
-  const at::Tensor& tokens = tensor_of(a[1], "tokens", at::kLong, {M});
-  same_device(tokens, "tokens", x, "logits");
-  const int32_t top = small_count(a[2], "top");
-  if (top > V || top > DPTQ_MAX_TOP)
-    fail(PyExc_ValueError, "top must be at most min(V, " + std::to_string(DPTQ_MAX_TOP) + ")");
-  Out lp(a[3], "logprobs", at::kFloat, {M}, x);
-  Out entropy(a[4], "entropy", at::kFloat, {M}, x);
-  Out top_lp(a[5], "top_logprobs", at::kFloat, {M, top}, x);
-  Out ids(a[6], "top_ids", at::kLong, {M, top}, x);
-  const int32_t dtype = half ? DPTQ_F16 : DPTQ_F32;
-  const int64_t bytes = dptq_token_logprobs_workspace(M, V, top, dtype);
-  Out work(Py_None, "workspace", at::kByte, {bytes > 0 ? bytes : 0}, x);
-  if (bytes > 0) allocate(lp, entropy, top_lp, ids, work);
-  else allocate(lp, entropy, top_lp, ids);
-  same_device(lp.t, "logprobs", x, "logits");
-  same_device(entropy.t, "entropy", x, "logits");
-  same_device(top_lp.t, "top_logprobs", x, "logits");
-  same_device(ids.t, "top_ids", x, "logits");
-  call("dptq_token_logprobs", x, dptq_token_logprobs, ptr(x), dtype, ld, M, V, ptr<int64_t>(tokens), top,
-       lp.ptr<float>(), entropy.ptr<float>(), top_lp.ptr<float>(), ids.ptr<int64_t>(),
-       bytes > 0 ? work.ptr() : nullptr, bytes > 0 ? bytes : 0);
-  return tuple(lp, entropy, top_lp, ids);
-}
-
 // Logits [M, V], fp16 or fp32, rows *ld apart.
 const at::Tensor& logit_rows(PyObject* o, int32_t* dtype, int64_t* ld) {
   if (!THPVariable_Check(o)) fail(PyExc_TypeError, "logits must be a torch.Tensor");
@@ -850,6 +820,35 @@ const at::Tensor& logit_rows(PyObject* o, int32_t* dtype, int64_t* ld) {
   if ((x.size(1) > 1 && x.stride(1) != 1) || *ld < x.size(1)) fail(PyExc_ValueError, "logits must have dense rows");
   *dtype = half ? DPTQ_F16 : DPTQ_F32;
   return x;
+}
+
+// token_logprobs(logits, tokens, top, logprobs, entropy, top_logprobs, top_ids)
+PyObject* token_logprobs(PyObject* const* a) {
+  int32_t dtype;
+  int64_t ld;
+  const at::Tensor& x = logit_rows(a[0], &dtype, &ld);
+  const int64_t M = x.size(0), V = x.size(1);
+  const at::Tensor& tokens = tensor_of(a[1], "tokens", at::kLong, {M});
+  same_device(tokens, "tokens", x, "logits");
+  const int32_t top = small_count(a[2], "top");
+  if (top > V || top > DPTQ_MAX_TOP)
+    fail(PyExc_ValueError, "top must be at most min(V, " + std::to_string(DPTQ_MAX_TOP) + ")");
+  Out lp(a[3], "logprobs", at::kFloat, {M}, x);
+  Out entropy(a[4], "entropy", at::kFloat, {M}, x);
+  Out top_lp(a[5], "top_logprobs", at::kFloat, {M, top}, x);
+  Out ids(a[6], "top_ids", at::kLong, {M, top}, x);
+  const int64_t bytes = dptq_token_logprobs_workspace(M, V, top, dtype);
+  Out work(Py_None, "workspace", at::kByte, {bytes > 0 ? bytes : 0}, x);
+  if (bytes > 0) allocate(lp, entropy, top_lp, ids, work);
+  else allocate(lp, entropy, top_lp, ids);
+  same_device(lp.t, "logprobs", x, "logits");
+  same_device(entropy.t, "entropy", x, "logits");
+  same_device(top_lp.t, "top_logprobs", x, "logits");
+  same_device(ids.t, "top_ids", x, "logits");
+  call("dptq_token_logprobs", x, dptq_token_logprobs, ptr(x), dtype, ld, M, V, ptr<int64_t>(tokens), top,
+       lp.ptr<float>(), entropy.ptr<float>(), top_lp.ptr<float>(), ids.ptr<int64_t>(),
+       bytes > 0 ? work.ptr() : nullptr, bytes > 0 ? bytes : 0);
+  return tuple(lp, entropy, top_lp, ids);
 }
 
 // A parameter of each row, a tensor [M] (nullptr: a number for all).
@@ -878,6 +877,7 @@ PyObject* sample_tokens(PyObject* const* a) {
   if (k_all < 0 || k_all > 0x7FFFFFFF) fail(PyExc_ValueError, "top_k must be in [0, 2^31)");
   if (!p && !(p_all >= 0)) fail(PyExc_ValueError, "top_p must not be negative");
   if (!m && !(m_all >= 0)) fail(PyExc_ValueError, "min_p must not be negative");
+  const c10::DeviceGuard on(x.device());   // of the workspace's size and the launch
   Out tokens(a[6], "tokens", at::kLong, {M}, x);
   Out probs(a[7], "probs", at::kFloat, {M}, x);
   const int64_t bytes = dptq_sample_tokens_workspace(M, V, dtype);
