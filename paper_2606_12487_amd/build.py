@@ -26,8 +26,8 @@ BINDING_PATH = os.path.join(PKG_DIR, "_dptq_torch.so")
 
 SOURCES = ["rotate_quant.hip", "decode_fused.hip", "qgemm_ksplit.hip", "range_quant.hip",
            "qgemm.hip", "qgemm_decode.hip", "qgemm_fp6.hip", "qgemm_fp6_ksplit.hip", "kv_quant.hip",
-           "norm_quant.hip", "rotary.hip", "kv8_append.hip", "kv8_attention.hip", "kv8_prompt.hip", "logprobs.hip", "sample.hip",
-           "dptq_api.hip"]
+           "norm_quant.hip", "rotary.hip", "kv8_append.hip", "kv8_rotary_append.hip", "kv8_attention.hip",
+           "kv8_prompt.hip", "logprobs.hip", "sample.hip", "dptq_api.hip"]
 ARCH = "gfx950"
 
 HIPCC_FLAGS = [

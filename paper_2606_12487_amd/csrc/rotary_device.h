@@ -1,5 +1,6 @@
 // Rotary positions on rows of fp16 heads, shared by the kernel that only
-// rotates (rotary.hip) and the one that writes the cache too (kv8_append.hip).
+// rotates (rotary.hip) and the one that writes the cache too
+// (kv8_rotary_append.hip).
 //
 // Pair i of the first r = 2 half channels of a head, channels (i, i + half) or,
 // interleaved, (2i, 2i + 1), turns by the angle position * inv_freq[i]:
