@@ -11,7 +11,9 @@ namespace dptq {
 
 // GEMM kernels (values of dptq_gemm_kernel, then kGemmKsplit: the K-split
 // kernel that serves kGemmDecode, for M > 16 on a tile the dispatch chose).
-constexpr int kGemmAuto = 0, kGemmDecode = 1, kGemmTile = 2, kGemmWide = 3, kGemmKsplit = 4;
+// kGemmTall and kGemmSmall: the tile kernel on the gated products' other tiles.
+constexpr int kGemmAuto = 0, kGemmDecode = 1, kGemmTile = 2, kGemmWide = 3, kGemmKsplit = 4, kGemmTall = 5,
+              kGemmSmall = 6;
 
 namespace rules {
 
@@ -162,6 +164,55 @@ inline GemmRoute gemm_route(int64_t M, int64_t N, int K, int bits, int cus) {
     if (1.08 * us < tile_kernel_us(M, N, K, bits, wide, cus)) return {kGemmKsplit, p.tile};
   }
   return {wide ? kGemmWide : kGemmTile, -1};
+}
+
+// ---------------------------------------------------------------------------
+// Gated products (M > 16): two more tiles of the tile kernel, for the rounds that
+// the others leave partly filled.  256 x 192 (n x m) where it saves a round (M =
+// 333, N = 28672, K = 4096, 8 bits: 224 tiles in one round, 44 us, against 336 of
+// 256 x 128 in two, 60; M = 192, N = 57344, K = 8192: 90 against 123), 128 x 128
+// where a round of the larger tiles is half empty (M = 128, N = 28672, K = 4096: 22
+// against 30 us; M = 300, N = 8192, K = 1024: 8.1 against 11.1).  Estimates: a
+// start, then per round of one tile a compute unit a fixed part and its k loop
+// (slower when every unit is busy), the weights' way and the output's; fitted to
+// 260 shapes a bit width (M 17-2500, N 1024-57344, K 256-16384, weights cycling
+// through 300 MB), within 3 to 5% (one standard deviation) where they are near the
+// other kernels.
+// ---------------------------------------------------------------------------
+constexpr int kTallN = 256, kTallM = 192, kSmallN = 128, kSmallM = 128;
+struct TileCost {
+  int bn, bm;
+  double start, round, round_k, fill_k, kn, mn;
+};
+constexpr TileCost kGatedTiles[2][2] = {
+    // 4 bits: tall, small
+    {{kTallN, kTallM, 2.55, 4.53, 7.58e-3, 1.37e-3, 3.16e-8, 1.64e-7},
+     {kSmallN, kSmallM, 1.88, 2.34, 3.29e-3, 5.01e-4, 1.61e-8, 2.37e-7}},
+    // 8 bits
+    {{kTallN, kTallM, 2.98, 4.36, 6.25e-3, 2.57e-3, 1.58e-8, 2.03e-7},
+     {kSmallN, kSmallM, 1.87, 2.58, 2.83e-3, 9.47e-4, 1.94e-8, 2.53e-7}}};
+inline double gated_tile_us(const TileCost& t, int64_t M, int64_t N, int K, int cus) {
+  const int64_t tiles = ceil_div(M, t.bm) * ceil_div(N, t.bn);
+  const double rounds = (double)ceil_div(tiles, cus), k = (double)K;
+  const double fill = tiles < cus ? (double)tiles / cus : 1.0;
+  return t.start + rounds * (t.round + k * (t.round_k + t.fill_k * fill)) + t.kn * k * (double)N +
+         t.mn * (double)M * (double)N;
+}
+
+// gemm_route, or one of the two tiles where its estimate is 5% below that one's.
+inline GemmRoute gated_route(int64_t M, int64_t N, int K, int bits, int cus) {
+  const GemmRoute c = gemm_route(M, N, K, bits, cus);
+  if (c.kernel == kGemmDecode) return c;
+  double us = c.kernel == kGemmKsplit
+                  ? ksplit_plan(M, N, K, bits, cus).cost + ksplit_extra_us(c.tile, M, N, K, bits, cus)
+                  : tile_kernel_us(M, N, K, bits, c.kernel == kGemmWide, cus);
+  GemmRoute best = c;
+  us *= 0.95;
+  for (int i = 0; i < 2; ++i) {
+    const double t = gated_tile_us(kGatedTiles[bits == 8][i], M, N, K, cus);
+    if (t < us) us = t, best = {i == 0 ? kGemmTall : kGemmSmall, -1};
+  }
+  return best;
 }
 
 // ---------------------------------------------------------------------------

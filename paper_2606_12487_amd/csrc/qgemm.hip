@@ -107,6 +107,11 @@ struct Cfg {
 };
 
 template <int BITS> using PrefillCfg = Cfg<BITS, 256, 128, 4, 2>;
+// Gated products only (gemm_rules.h: gated_route has what they measured).  The tall
+// one's wavefronts have 64 x 96 each, 96 accumulator registers of 256 (three to six
+// spilled in the last stage, behind the k loop), and two stages fill the LDS at 8 bits.
+template <int BITS> using TallCfg = Cfg<BITS, rules::kTallN, rules::kTallM, 4, 2>;
+template <int BITS> using SmallCfg = Cfg<BITS, rules::kSmallN, rules::kSmallM, 4, 2>;
 
 // ZP (the prefill kernels and the decode kernel alike): the range quantizer's
 // zero-point correction acc + (2^(BITS-1) - a_zeros[m]) * w_sums[n], exact in
@@ -964,7 +969,19 @@ hipError_t launch_t(const uint8_t* a, const float* as, int64_t M, int K,
                     const int32_t* az = nullptr, const int32_t* wsum = nullptr, const Gate& gate = Gate{}) {
   if (M == 0) return hipSuccess;
   const int cus = device_cus();
-  const rules::GemmRoute c = kernel == kGemmAuto ? rules::gemm_route(M, N, K, BITS, cus) : rules::GemmRoute{kernel, -1};
+  const rules::GemmRoute c = kernel != kGemmAuto ? rules::GemmRoute{kernel, -1}
+                             : GATED             ? rules::gated_route(M, N, K, BITS, cus)
+                                                 : rules::gemm_route(M, N, K, BITS, cus);
+  if constexpr (GATED) {
+    if (c.kernel == kGemmTall) {
+      launch_prefill<TallCfg<BITS>, ACC_OUT, WA8, ZP, GATED>(a, as, M, K, w, ws, N, y, acc, az, wsum, gate, stream);
+      return hipGetLastError();
+    }
+    if (c.kernel == kGemmSmall) {
+      launch_prefill<SmallCfg<BITS>, ACC_OUT, WA8, ZP, GATED>(a, as, M, K, w, ws, N, y, acc, az, wsum, gate, stream);
+      return hipGetLastError();
+    }
+  }
   switch (c.kernel) {
     case kGemmDecode:
     case kGemmKsplit:

@@ -72,6 +72,19 @@ def test_each_tile_kernel(M, K, N, bits):
     test_each_int8_kernel(M, K, N, bits)
 
 
+# The gated products' own tiles: ragged rows and channels, a last stage of 128 k, one to three rounds.
+# test_gated_rules.py keeps each on the tile named at 256 compute units.
+SMALL_CASES = [(211, 384, 10960, 4), (211, 384, 10960, 8), (100, 1152, 28688, 4), (300, 1152, 8208, 8),
+               (129, 128, 12304, 8), (65536, 128, 64, 8)]
+TALL_CASES = [(339, 1152, 30256, 4), (339, 1152, 30256, 8), (190, 128, 54096, 4), (190, 640, 54096, 8),
+              (2100, 512, 16400, 4), (1100, 256, 8208, 8)]
+
+
+@pytest.mark.parametrize("M,K,N,bits", SMALL_CASES + TALL_CASES)
+def test_each_gated_tile(M, K, N, bits):
+    test_each_int8_kernel(M, K, N, bits)
+
+
 @pytest.mark.parametrize("M,N,K", FP6_CASES)
 def test_each_fp6_kernel(M, N, K):
     a, a_s, w, w_s = _operands(M, K, N, 4)
