@@ -151,3 +151,24 @@ def test_append_odd_batches():
         out.fill_(9.0)
         dptq.rotary_kv8_append(q, k, v, _d(cu), _d(n), t, cache, f, q_out=out)
         assert torch.equal(out[:80], want_q) and bool((out[80:] == 9).all())
+
+
+@pytest.mark.parametrize("new,interleaved", [((850,), True), ((600, 0, 660), True), ((600, 1, 660), False)])
+def test_append_of_many_query_heads(new, interleaved):
+    """More than 64 angles a token, which a wave turns several parts of the heads by."""
+    rng = np.random.default_rng(sum(new))
+    H, Hkv, D = 64, 1, 256
+    T, P = sum(new), _pages(new)
+    arrays, table = _garbage(rng, P, Hkv, D), _table(rng, list(new), P)
+    rows = torch.randn((T, H + 2 * Hkv, D), device="cuda", generator=torch.Generator("cuda").manual_seed(T)).half()
+    q, k, v = rows.split([H, Hkv, Hkv], dim=1)
+    n, positions = _d(np.array(new, np.int32)), _d(np.concatenate([np.arange(b) for b in new]).astype(np.int32))
+    for r in (D, 200):
+        f = dptq.rotary_inv_freq(r)
+        one, two = _cache(arrays), _cache(arrays)
+        got = dptq.rotary_kv8_append(q, k, v, _d(_cu(new)), n, _d(table), one, f, interleaved)
+        want_q, want_k = dptq.rotary(q, k, positions, f, interleaved)
+        assert torch.equal(got, want_q)
+        dptq.kv8_append(want_k, v, _d(_cu(new)), n, _d(table), two)
+        for a, b in zip(one, two):
+            assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
