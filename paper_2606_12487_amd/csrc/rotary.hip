@@ -80,11 +80,23 @@ hipError_t launch_rotary(const RotaryCall& c, hipStream_t stream) {
   const int64_t units = (int64_t)(c.heads + c.kv_heads) * a.r.units;
   const bool few = c.T * units < (int64_t)device_cus() * 4 * 64 * 4;
   a.parts = (int)((units + (few ? 63 : 255)) / (few ? 64 : 256));
-  a.waves = c.T * a.parts;
-  if ((a.waves + kWaves - 1) / kWaves > 0x7FFFFFFF) return hipErrorInvalidValue;
-  if (few) launch_n<1>(a, stream);
-  else launch_n<4>(a, stream);
-  return hipGetLastError();
+  // A launch holds less than 2^32 threads.
+  const int64_t most = 0xFFFFFFFFll / 64 / a.parts - kWaves;
+  for (int64_t t = 0; t < c.T; t += most) {
+    a.waves = (c.T - t < most ? c.T - t : most) * a.parts;
+    if (few) launch_n<1>(a, stream);
+    else launch_n<4>(a, stream);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    a.positions += most;
+    a.q += most * c.ld_q;
+    a.q_out += most * c.ld_q_out;
+    if (c.kv_heads > 0) {
+      a.k += most * c.ld_k;
+      a.k_out += most * c.ld_k_out;
+    }
+  }
+  return hipSuccess;
 }
 
 }  // namespace dptq

@@ -187,3 +187,19 @@ def test_long_rows_of_many_sequences():
     assert bool((out[:-1] == 1).all())
     small, _ = dptq.rotary(q[-1:], None, positions[-1:], f)
     assert torch.equal(out[-1:], small) and not torch.equal(small, q[:1])
+
+
+def test_more_tokens_than_a_launch_holds():
+    """Rotary positions of 2^26 + 5 tokens of one small head, a wave each: more than 2^32 threads."""
+    T, D, piece = (1 << 26) + 5, 8, 1 << 24
+    q = torch.empty((T, 1, D), dtype=torch.float16, device="cuda")
+    g = torch.Generator("cuda").manual_seed(3)
+    for t in range(0, T, piece):
+        q[t:t + piece] = torch.randn((min(piece, T - t), 1, D), device="cuda", generator=g).half()
+    positions = torch.arange(T, dtype=torch.int32, device="cuda")
+    f = dptq.rotary_inv_freq(D)
+    out, _ = dptq.rotary(q, None, positions, f)
+    for t in (0, (1 << 26) - 4100, T - 4097):
+        want, _ = dptq.rotary(q[t:t + 4097], None, positions[t:t + 4097], f)
+        assert torch.equal(out[t:t + 4097], want), t
+    assert bool((out.view(torch.int16)[piece:] != q.view(torch.int16)[piece:]).any(-1).all())
