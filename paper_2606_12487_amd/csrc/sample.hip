@@ -34,7 +34,8 @@
 // 12 for the histograms of four parts each and 22 for the second launch on one
 // compute unit a row: joining and summing the bins 2.5, gathering 8, sorting and
 // summing the list 2, and up to four borders in turn, 0.6 each.  One row of 32000
-// takes 21 us, the same chain.  Dropped, each measured: the gathering shared by a
+// takes 18 us, the same chain (21 while every wave went through its share of a whole
+// span, there or not).  Dropped, each measured: the gathering shared by a
 // row's workgroups, with fences of the device's scope (160 us) or accesses of it
 // (56 us: four trips to memory); three loads ahead (registers spill, 39 us); a
 // bitonic sort alone (64 rows: 51 us); loops over a chunk's vectors unrolled (the
@@ -48,7 +49,8 @@ namespace {
 constexpr int kThreads = 1024, kWaves = kThreads / 64;
 constexpr int kBinBits = 10, kBins = 1 << kBinBits;   // one a thread
 constexpr int kCap = 2048;        // tokens that are sorted at once
-constexpr int kMinPart = 16384;   // logits of a part of a row, at least
+// Parts of a row: logits of each, at least, and how many, at most.
+constexpr int kMinPart = 8192, kMaxParts = 8;
 constexpr int kXcds = 8;
 
 // Values as integers in their order; -0 is 0.
@@ -153,12 +155,16 @@ struct Reader {
       if (i < vectors) c.v[n] = p[i];
     }
   }
+  // Whether this wave has any of the n-th vectors of the span at `at`.
+  __device__ __forceinline__ bool any(int at, int n) const {
+    return at + n * kThreads + __builtin_amdgcn_readfirstlane((int)threadIdx.x & ~63) < vectors;
+  }
   // f(logit, number in its vector, index of the vector's first logit), vector by vector.
   template <typename F>
   __device__ __forceinline__ void each(Chunk c, int at, const F& f) const {
     int i = first + (at + (int)threadIdx.x) * kEach;
 #pragma unroll 1
-    for (int n = 0; n < kLoads; ++n) {
+    for (int n = 0; n < kLoads && any(at, n); ++n) {
       f(c.v[0], i);
 #pragma unroll
       for (int k = 0; k + 1 < kLoads; ++k) c.v[k] = c.v[k + 1];
@@ -877,10 +883,14 @@ __global__ void __launch_bounds__(kThreads) sample_select_kernel(SampleArgs a) {
   select<T>(a, row, m, asked, count, mass, s);
 }
 
-// Parts of a row: a workgroup for each compute unit, of kMinPart logits or more.
+// Parts of a row: a workgroup for each compute unit, within bounds: a histogram
+// costs its second launch 0.3 us, and one of fewer logits is hardly shorter (one row
+// of 32000 fp16 in 2, 4 and 8 parts 19.1, 17.9 and 18.6 us, of 131072 in 8, 16 and 32
+// 25.4, 26.1 and 30.6).
 int choose_splits(const SampleTokens& c) {
   const int64_t want = device_cus() / c.M, most = ((int64_t)c.V + kMinPart - 1) / kMinPart;
-  return (int)(want < 1 ? 1 : want < most ? want : most);
+  const int64_t parts = most < kMaxParts ? most : kMaxParts;
+  return (int)(want < 1 ? 1 : want < parts ? want : parts);
 }
 
 template <typename T>
