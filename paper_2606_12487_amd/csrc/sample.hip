@@ -18,7 +18,8 @@
 // place.  A bin of more than 2048 tokens is cut into 1024 again and again until
 // it is small or all its values are equal, when index and sum are arithmetic.
 // Where everything down to the lowest border is at most 2048 tokens, which
-// top-k and top-p mostly leave, they are gathered once for all borders.
+// top-k and top-p mostly leave, they are gathered once for all borders; and with a
+// top-p border's bin the bins in which the token's border then lies.
 //
 // w in 64 bits: with 131072 tokens of like weight a relative error of 2^-24 in
 // the sums would change one token in a hundred.  2^t = 2^n (1 + f q(f)) with n
@@ -27,15 +28,18 @@
 //
 // A row to a workgroup where rows are many; few rows are cut into parts whose
 // histograms one launch forms, relative to their own largest logit, and a second
-// joins.  What bounds it: 256 rows of 100003 fp32 take 60 us, of which the
+// joins.  What bounds it: 256 rows of 100003 fp32 take 59 us, of which the
 // histogram is 36 (28 without the weights; some 30 vector instructions a logit,
-// 13 of them of 64 bits) and the gathering of the border's bin 15 (a second read
-// at 6.8 TB/s).  64 rows of 131072 fp16 that ask for different things take 37 us,
+// 13 of them of 64 bits) and the gathering of the border's bin 13 (a second read
+// at 7.8 TB/s).  64 rows of 131072 fp16 that ask for different things take 37 us,
 // 12 for the histograms of four parts each and 22 for the second launch on one
-// compute unit a row: joining and summing the bins 2.5, gathering 8, sorting and
-// summing the list 2, and up to four borders in turn, 0.6 each.  One row of 32000
-// takes 18 us, the same chain (21 while every wave went through its share of a whole
-// span, there or not).  Dropped, each measured: the gathering shared by a
+// compute unit a row: joining and summing the bins 2.5, gathering 7.5 (13 of two
+// ranges), sorting and summing the list 2, and up to four borders in turn, 0.6 each.
+// One row of 32000 takes 18 us, the same chain (21 while every wave went through its
+// share of a whole span, there or not).  With top-p alone 64 rows of 131072 take 43
+// us: two gatherings took 49, at an addition for each vector and not for four.  No
+// kernel uses scratch memory: with 92 bytes of it 512 rows of 100003 took 116 us for
+// 107.  Dropped, each measured: the gathering shared by a
 // row's workgroups, with fences of the device's scope (160 us) or accesses of it
 // (56 us: four trips to memory); three loads ahead (registers spill, 39 us); a
 // bitonic sort alone (64 rows: 51 us); loops over a chunk's vectors unrolled (the
@@ -198,15 +202,6 @@ __device__ __forceinline__ void values(uint4 v, const F& f) {
   }
 }
 
-// Value j of a vector.
-template <typename T>
-__device__ __forceinline__ float value_at(uint4 v, int j) {
-  const int k = sizeof(T) == 2 ? j >> 1 : j;
-  const uint32_t w = k < 2 ? (k ? v.y : v.x) : k == 2 ? v.z : v.w;
-  if constexpr (sizeof(T) == 2) return __half2float(__ushort_as_half((unsigned short)(j & 1 ? w >> 16 : w)));
-  else return __uint_as_float(w);
-}
-
 // Which values of a vector lie in [least, most], as bits; element(b): which value
 // a bit is.  NaN does not; -0 is 0.
 template <typename T>
@@ -218,7 +213,7 @@ struct Within {
     values<T>(v, [&](float e, int j) { m |= e >= least && e <= most ? 1u << j : 0u; });
     return m;
   }
-  __device__ __forceinline__ static int element(int b) { return b; }
+  __device__ __forceinline__ static int element(int b) { return b & 3; }
 };
 // fp16: two at a time, those that clamping to the bounds (rounded into the range)
 // leaves as they are.
@@ -254,6 +249,7 @@ struct SampleArgs {
   int64_t ld, M;
   int V, splits, part;      // part: logits of a split
   double unit;              // 2^e of the sums of a row
+  u64 one;                  // the same
   const float* u;
   const float *temperature, *top_p, *min_p;   // of each row, or nullptr and the value
   const int32_t* top_k;
@@ -293,17 +289,32 @@ struct Histogram {
   uint32_t count[kBins];
 };
 
+// All tokens of a range, in the list.
+struct Segment {
+  Range range;
+  uint32_t first, held;   // in the list
+  uint32_t before_n;      // tokens of the row before it
+  u64 before_sum;
+};
+
 struct Shared {
   Histogram h;                 // of the row, then of a bin that is cut again
   u64 mass[kBins + 1];         // before bin kBins - 1 - j
   uint32_t count[kBins + 1];
   u64 list[kCap];              // key and ~index, in the order
   u64 sum[kCap];               // up to each
+  Segment seg[2];              // what the list holds: a range, or two, the second before the first
   u64 wave_m[2][kWaves];
   uint32_t wave_n[2][kWaves];
   float wave_f[2][kWaves];
   int n, found;
 };
+
+// A value that all lanes have, in a scalar register.
+__device__ __forceinline__ uint32_t scalar(uint32_t x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ u64 scalar(u64 x) {
+  return (u64)scalar((uint32_t)(x >> 32)) << 32 | scalar((uint32_t)x);
+}
 
 // The sum of the waves before this one, of each wave's value (lane 63's), in
 // part; a barrier comes before the reads, and the callers alternate between two
@@ -478,92 +489,120 @@ struct Selector {
   float m;
   double c, unit;
   Shared& s;
-  // What the list holds: all tokens of a range, those before it.
-  Range range;
-  uint32_t before_n, held;
-  u64 before_sum;
+
+  // Tokens of a range of keys: `count` of them after n0 of sum sum0.
+  struct Part {
+    Range r;
+    uint32_t n0, count;
+    u64 sum0;
+  };
 
   __device__ __forceinline__ double weight_of(uint32_t key) const { return weight(value_of(key), m, c); }
 
-  // The cumulative counts and sums of the bins, descending (this thread's is the
-  // one after those of lower threads), after n tokens of sum `sum`.
-  __device__ __forceinline__ void cumulate(uint32_t count, u64 mass, uint32_t n, u64 sum) {
+  // The cumulative counts and sums of bins, descending (this thread's is the one
+  // after those of lower threads), after n tokens of sum `sum`.
+  __device__ __forceinline__ void cumulate(uint32_t count, u64 mass, uint32_t n, u64 sum, uint32_t* counts,
+                                           u64* sums) {
     const uint32_t cn = wave_scan(count);
     const u64 cm = wave_scan(mass);
     put_wave(cn, s.wave_n[0]);
     put_wave(cm, s.wave_m[0]);
     __syncthreads();
-    s.count[threadIdx.x + 1] = n + waves_before(s.wave_n[0]) + cn;
-    s.mass[threadIdx.x + 1] = sum + waves_before(s.wave_m[0]) + cm;
-    if (threadIdx.x == 0) s.count[0] = n, s.mass[0] = sum;
+    counts[threadIdx.x + 1] = n + waves_before(s.wave_n[0]) + cn;
+    sums[threadIdx.x + 1] = sum + waves_before(s.wave_m[0]) + cm;
+    if (threadIdx.x == 0) counts[0] = n, sums[0] = sum;
     __syncthreads();
   }
 
   // Which of the cumulated bins (0: the first in the order) a border is in; the
   // last that is not empty where rounding leaves none.  kKey does not come here.
-  __device__ __forceinline__ int bin_with(const Border& b) const {
+  __device__ __forceinline__ int bin_with(const Border& b, const uint32_t* counts, const u64* sums) const {
     int j = kBins;
-    if (b.by == By::kSum) j = first_of(kBins, [&](int i) { return s.mass[i + 1] >= b.sum; });
+    if (b.by == By::kSum) j = first_of(kBins, [&](int i) { return sums[i + 1] >= b.sum; });
     if (j == kBins) {
-      const uint32_t n = b.by == By::kCount ? b.n : s.count[kBins];
-      j = first_of(kBins, [&](int i) { return s.count[i + 1] >= n; });
+      const uint32_t n = b.by == By::kCount ? b.n : counts[kBins];
+      j = first_of(kBins, [&](int i) { return counts[i + 1] >= n; });
     }
     return min(j, kBins - 1);
   }
+  // Of the row's.
+  __device__ __forceinline__ int bin_with(const Border& b) const { return bin_with(b, s.count, s.mass); }
 
-  // Gathers the tokens of a range into the list, in any order; their number, at
-  // most kCap.
-  __device__ __forceinline__ int gather(Range r) {
+  // The tokens of bins j to k of the row's.
+  __device__ __forceinline__ Part bins(int j, int k) const {
+    const uint32_t n0 = scalar(s.count[j]);
+    return {Range{range_of(kBins - 1 - k).lo, range_of(kBins - 1 - j).hi}, n0, scalar(s.count[k + 1]) - n0,
+            scalar(s.mass[j])};
+  }
+
+  // Gathers the tokens of a range, or of two, into the list, in any order; their
+  // number, at most kCap.
+  __device__ __forceinline__ int gather(Range r, bool two, Range r2) {
     __syncthreads();   // the list's readers are done
     if (threadIdx.x == 0) s.n = 0;
     __syncthreads();
-    const Within<T> within(value_of(r.lo), value_of(r.hi));
-    // A thread marks what it has of a vector that begins at index i.
-    const auto take = [&](uint4 v, int i) {
+    const Within<T> within(value_of(r.lo), value_of(r.hi)), within2(value_of(r2.lo), value_of(r2.hi));
+    using R = Reader<T>;
+    // The row's address is made anew: the compiler would keep those of all loads over
+    // the selection's steps, and spill others for them.
+    const T* row = x;
+    asm volatile("" : "+s"(row));
+    const R reader(row, 0, V);
+    // A thread marks what it has of up to four vectors, index_of(bit) the first bit's
+    // logit and so on, and puts down the indices.
+    const auto marks = [&](uint4 v) {
       uint32_t mine = within.marks(v);
+      if (two) mine |= within2.marks(v);
+      return mine;
+    };
+    const auto put = [&](uint32_t mine, const auto& index_of) {
       if (!mine) return;
       // One addition for each lane as it is: the compiler would sum up a uniform
       // address's over the wave, which takes longer for the few lanes here.
       int offset;
       asm("v_mov_b32 %0, 0" : "=v"(offset));
       int to = atomicAdd(&s.n + offset, __popc(mine));
-      for (; mine; mine &= mine - 1, ++to) {
-        const int j = Within<T>::element(__ffs((int)mine) - 1);
-        if (to < kCap) s.list[to] = (u64)key_of(value_at<T>(v, j)) << 32 | (uint32_t)~(i + j);
-      }
+      for (; mine; mine &= mine - 1, ++to)
+        if (to < kCap) s.list[to] = (u64)index_of(__ffs((int)mine) - 1);
     };
-    using R = Reader<T>;
-    const R reader(x, 0, V);
-    const auto take_all = [&](const typename R::Chunk& c, int at) {
+    const auto take = [&](const typename R::Chunk& c, int at) {
+      uint32_t mine = 0;
 #pragma unroll
-      for (int n = 0; n < R::kLoads; ++n)
-        take(c.v[n], reader.first + (at + n * kThreads + (int)threadIdx.x) * R::kEach);
+      for (int n = 0; n < R::kLoads; ++n) mine |= marks(c.v[n]) << (4 * n);
+      const int i = reader.first + (at + (int)threadIdx.x) * R::kEach;
+      put(mine, [&](int b) { return i + (b >> 2 & 3) * kThreads * R::kEach + Within<T>::element(b); });
     };
     typename R::Chunk even, odd;   // one on its way while the other is taken
     int i;
     const uint4 ends = reader.ends(i);
     reader.load(0, even);
-    take(ends, i);
+    put(marks(ends), [&](int) { return i; });
     for (int at = 0; at < reader.vectors; at += 2 * R::kSpan) {
       const int next = at + R::kSpan;
       if (next < reader.vectors) reader.load(next, odd);
-      take_all(even, at);
+      take(even, at);
       if (next >= reader.vectors) break;
       if (next + R::kSpan < reader.vectors) reader.load(next + R::kSpan, even);
-      take_all(odd, next);
+      take(odd, next);
     }
     __syncthreads();
-    return min(s.n, kCap);
+    const int count = min((int)scalar((uint32_t)s.n), kCap);
+    for (int k = threadIdx.x; k < count; k += kThreads) {
+      const int at = (int)s.list[k];
+      s.list[k] = (u64)key_of((float)row[at]) << 32 | (uint32_t)~at;
+    }
+    return count;
   }
 
-  // Sorts the list's tokens: counted into kBins stretches of the range, scattered
-  // to their stretch, and each put behind those of it that come first.  A stretch
-  // holds a few; false, and nothing done, where one holds more than kCrowd.
-  __device__ __forceinline__ bool sort_by_buckets(int count, Range r) {
+  // Sorts the list's tokens: counted into kBins stretches of the range (without the
+  // `gap` keys below `split`), scattered to their stretch, and each put behind those
+  // of it that come first.  A stretch holds a few; false, and nothing done, where one
+  // holds more than kCrowd.
+  __device__ __forceinline__ bool sort_by_buckets(int count, Range r, uint32_t split, uint32_t gap) {
     constexpr int E = kCap / kThreads, kCrowd = 64;
     uint32_t* const offset = reinterpret_cast<uint32_t*>(s.h.mass);   // [kBins + 1]
     const int tid = threadIdx.x;
-    const int shift = max(32 - kBinBits - __clz((int)(r.hi - r.lo)), 0);
+    const int shift = max(32 - kBinBits - __clz((int)(r.hi - r.lo - gap)), 0);
     s.h.count[tid] = 0;
     if (tid == 0) s.found = 0;
     __syncthreads();
@@ -574,7 +613,8 @@ struct Selector {
       const int i = e * kThreads + tid;
       if (i >= count) continue;
       v[e] = s.list[i];
-      bucket[e] = (r.hi - (uint32_t)(v[e] >> 32)) >> shift;
+      const uint32_t key = (uint32_t)(v[e] >> 32);
+      bucket[e] = (r.hi - key - (key < split ? gap : 0)) >> shift;
       place[e] = atomicAdd(&s.h.count[bucket[e]], 1u);
       if (place[e] >= (uint32_t)kCrowd) s.found = 1;
     }
@@ -603,10 +643,12 @@ struct Selector {
     return true;
   }
 
-  // Puts `count` gathered tokens in their order, with their sums: all of a range,
-  // after n of sum `sum`.
-  __device__ __forceinline__ void arrange(int count, Range r, uint32_t n, u64 sum) {
-    if (!sort_by_buckets(count, r)) {
+  // Puts `count` gathered tokens in their order, with their sums: all of the part,
+  // or, `ahead` holding any, of that one too.
+  __device__ __forceinline__ void arrange(int count, const Part& part, const Part& ahead) {
+    const bool two = ahead.count > 0;
+    const Range r{part.r.lo, two ? ahead.r.hi : part.r.hi};
+    if (!sort_by_buckets(count, r, two ? ahead.r.lo : 0, two ? ahead.r.lo - part.r.hi - 1 : 0)) {
       int size = 64;
       while (size < count) size *= 2;
       for (int i = count + threadIdx.x; i < size; i += kThreads) s.list[i] = 0;   // behind all
@@ -619,28 +661,50 @@ struct Selector {
     const u64 up_to = wave_scan(w0 + w1);
     put_wave(up_to, s.wave_m[1]);
     __syncthreads();
-    const u64 all = sum + waves_before(s.wave_m[1]) + up_to;
+    const u64 all = waves_before(s.wave_m[1]) + up_to;
     s.sum[a] = all - w1;
     s.sum[a + 1] = all;
+    if (threadIdx.x == 0) {
+      const uint32_t first = min(ahead.count, (uint32_t)count);
+      s.seg[0] = Segment{part.r, first, (uint32_t)count - first, part.n0, part.sum0};
+      s.seg[1] = Segment{ahead.r, 0, first, ahead.n0, ahead.sum0};
+    }
     __syncthreads();
-    range = r;
-    before_n = n;
-    before_sum = sum;
-    held = (uint32_t)count;
   }
 
-  // A border among the list's tokens.
-  __device__ __forceinline__ Place in_list(const Border& b) const {
-    uint32_t n;   // tokens of the list before the border
-    if (b.by == By::kCount) n = b.n - before_n;
-    else if (b.by == By::kKey) n = first_of(kCap, [&](int i) { return i >= (int)held || (uint32_t)(s.list[i] >> 32) < b.key; });
-    else n = 1 + first_of(kCap, [&](int i) { return i >= (int)held || s.sum[i] >= b.sum; });
-    n = min(n, held);
-    Place p{before_n + n, before_sum, 0, -1};
+  // The segment that holds all of a range; -1: none.
+  __device__ __forceinline__ int holder(Range r) const {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      if (s.seg[i].held > 0 && r.lo >= s.seg[i].range.lo && r.hi <= s.seg[i].range.hi) return i;
+    return -1;
+  }
+
+  // A border among a segment's tokens.
+  __device__ __forceinline__ Place in_list(const Border& b, int held) const {
+    const Segment& in = s.seg[held];
+    const struct {
+      uint32_t first, held, before_n;
+      u64 before_sum;
+    } g{scalar(in.first), scalar(in.held), scalar(in.before_n), scalar(in.before_sum)};
+    const int first = (int)g.first, end = (int)(g.first + g.held);
+    const u64 base = first ? scalar(s.sum[first - 1]) : 0;
+    uint32_t n;   // tokens of it before the border
+    if (b.by == By::kCount) {
+      n = b.n - g.before_n;
+    } else if (b.by == By::kKey) {
+      n = first_of(kCap, [&](int i) { return i >= end || (i >= first && (uint32_t)(s.list[i] >> 32) < b.key); }) - first;
+    } else {
+      const u64 least = b.sum - min(b.sum, g.before_sum) + base;
+      n = 1 + first_of(kCap, [&](int i) { return i >= end || (i >= first && s.sum[i] >= least); }) - first;
+    }
+    n = min(n, g.held);
+    Place p{g.before_n + n, g.before_sum, 0, -1};
     if (n) {
-      p.sum = s.sum[n - 1];
-      p.key = (uint32_t)(s.list[n - 1] >> 32);
-      p.index = (int)~(uint32_t)s.list[n - 1];
+      const u64 last = scalar(s.list[first + n - 1]);
+      p.sum = g.before_sum + (scalar(s.sum[first + n - 1]) - base);
+      p.key = (uint32_t)(last >> 32);
+      p.index = (int)~(uint32_t)last;
     }
     return p;
   }
@@ -677,15 +741,13 @@ struct Selector {
     return p;
   }
 
-  // Tokens of a range of keys: `count` of them after n0 of sum sum0.
-  struct Part {
-    Range r;
-    uint32_t n0, count;
-    u64 sum0;
-  };
   // The part of a range with more than kCap tokens that a border is in: at most
-  // kCap, or all equal.  Uses the bins.
+  // kCap, or all equal.  The list's memory holds the bins' sums meanwhile, so the
+  // list is empty.
   __device__ __forceinline__ Part narrow(const Border& b, Part p) {
+    uint32_t* const counts = reinterpret_cast<uint32_t*>(s.list);
+    u64* const sums = s.sum;
+    static_assert(kCap > kBins, "the bins' sums in the list");
     while (p.count > (uint32_t)kCap && p.r.lo < p.r.hi) {
       // 2^shift keys a bin, at most kBins of them.
       int shift = 0;
@@ -693,6 +755,7 @@ struct Selector {
       s.h.mass[threadIdx.x] = 0;
       s.h.count[threadIdx.x] = 0;
       __syncthreads();
+      if (threadIdx.x < 2) s.seg[threadIdx.x].held = 0;
       for (int i = threadIdx.x; i < V; i += kThreads) {
         const float v = (float)x[i];
         const uint32_t k = key_of(v);
@@ -703,11 +766,11 @@ struct Selector {
       }
       __syncthreads();
       const int mine = kBins - 1 - (int)threadIdx.x;
-      cumulate(s.h.count[mine], s.h.mass[mine], p.n0, p.sum0);
-      const int j = b.by == By::kKey ? kBins - 1 - (int)((b.key - p.r.lo) >> shift) : bin_with(b);
-      p.n0 = s.count[j];
-      p.sum0 = s.mass[j];
-      p.count = s.count[j + 1] - p.n0;
+      cumulate(s.h.count[mine], s.h.mass[mine], p.n0, p.sum0, counts, sums);
+      const int j = b.by == By::kKey ? kBins - 1 - (int)((b.key - p.r.lo) >> shift) : bin_with(b, counts, sums);
+      p.n0 = scalar(counts[j]);
+      p.sum0 = scalar(sums[j]);
+      p.count = scalar(counts[j + 1]) - p.n0;
       const uint32_t lo = p.r.lo + ((uint32_t)(kBins - 1 - j) << shift);
       p.r = Range{lo, min(p.r.hi, lo + ((1u << shift) - 1))};
       __syncthreads();
@@ -717,15 +780,22 @@ struct Selector {
 };
 
 // The least sum that is not below p of `sum`, and the least that is above u of it.
-__device__ __forceinline__ u64 below(float p, u64 sum) { return max(__double2ull_ru((double)p * (double)sum), 1ull); }
+// (The empty asm keeps the conversion of p or u here: the compiler would make them
+// ahead of the selection's steps, and spill them.)
+__device__ __forceinline__ double wide(float p) {
+  asm volatile("" : "+s"(p));
+  return (double)p;
+}
+__device__ __forceinline__ u64 below(float p, u64 sum) { return max(__double2ull_ru(wide(p) * (double)sum), 1ull); }
 __device__ __forceinline__ u64 above(float u, u64 sum) {
-  return __double2ull_rd(fmax((double)u * (double)sum, 0.0)) + 1;
+  return __double2ull_rd(fmax(wide(u) * (double)sum, 0.0)) + 1;
 }
 
 // The row's token, from its histogram: this thread's bin (kBins - 1 - thread) has
 // count tokens of sum mass.
 template <typename T>
-__device__ __forceinline__ void select(const SampleArgs& a, int64_t row, float m, const Asked& asked, uint32_t count, u64 mass, Shared& s) {
+__device__ __forceinline__ void select(const SampleArgs& a, int64_t row, float m, const Asked& asked, uint32_t count,
+                                       u64 mass, Shared& s) {
   const T* const x = static_cast<const T*>(a.x) + row * a.ld;
   if (m == -INFINITY) {   // nothing to choose from
     if (threadIdx.x == 0) {
@@ -734,12 +804,15 @@ __device__ __forceinline__ void select(const SampleArgs& a, int64_t row, float m
     }
     return;
   }
-  Selector<T> sel{x, a.V, m, asked.c, a.unit, s, Range{1, 0}, 0, 0, 0};
-  sel.cumulate(count, mass, 0, 0);
-  const uint32_t all = s.count[kBins];
+  m = __uint_as_float(scalar(__float_as_uint(m)));
+  Selector<T> sel{x, a.V, m, asked.c, a.unit, s};
+  if (threadIdx.x < 2) s.seg[threadIdx.x].held = 0;
+  sel.cumulate(count, mass, 0, 0, s.count, s.mass);
+  const uint32_t all = scalar(s.count[kBins]);
   const float top_p = asked.top_p, min_p = asked.min_p;
   const uint32_t k = asked.top_k ? min(asked.top_k, all) : all;
-  const bool by_k = k < all, by_p = !asked.greedy && top_p < 1.0f && k > 1, by_min = !asked.greedy && min_p > 0.0f && k > 1;
+  const bool by_k = k < all, by_p = !asked.greedy && top_p < 1.0f && k > 1;
+  const bool by_min = !asked.greedy && min_p > 0.0f && k > 1;
 
   // The smallest key of weight min_p: 64 keys of what is left at a time.
   uint32_t least = kLowestKey;
@@ -767,16 +840,17 @@ __device__ __forceinline__ void select(const SampleArgs& a, int64_t row, float m
   const int last = min_first ? bin_min : bin_first;
 
   uint32_t n = all;
-  u64 sum = s.mass[kBins];
+  u64 sum = scalar(s.mass[kBins]);
   Place p{};
   bool whole = false;   // the list has all
   for (int step = -1; step < 5; ++step) {
     Border b{};
-    typename Selector<T>::Part part{};
-    bool held = false, ties = false;
+    typename Selector<T>::Part part{}, ahead{};
+    int held = -1;
+    bool ties = false;
     if (step < 0) {
       // All that the borders can need, if it is little.
-      part = {Range{range_of(kBins - 1 - last).lo, key_of(m)}, 0, s.count[last + 1], 0};
+      part = {Range{range_of(kBins - 1 - last).lo, key_of(m)}, 0, scalar(s.count[last + 1]), 0};
       if (part.count > (uint32_t)kCap) continue;
       whole = true;
     } else {
@@ -796,29 +870,42 @@ __device__ __forceinline__ void select(const SampleArgs& a, int64_t row, float m
         if (n > 1 && p.n <= n) continue;
         b = Border{By::kCount, n, 0, 0};
       }
-      held = whole;
-      if (!held) {
+      if (whole) {
+        held = 0;
+      } else {
         const int j = b.by == By::kKey ? bin_min : sel.bin_with(b);
-        part = {range_of(kBins - 1 - j), s.count[j], s.count[j + 1] - s.count[j], s.mass[j]};
+        part = sel.bins(j, j);
         // Whatever a border needs is in the list if that holds the border's bin.
-        held = sel.held > 0 && part.r.lo >= sel.range.lo && part.r.hi <= sel.range.hi;
+        held = sel.holder(part.r);
+        if (held < 0 && step == 1 && !by_min) {
+          // The token's border is in one of these bins, wherever in bin j this one
+          // turns out to be: gathered with it where both are little.
+          const int from = sel.bin_with(Border{By::kSum, 0, above(asked.u, s.mass[j]), 0});
+          const int to = sel.bin_with(Border{By::kSum, 0, above(asked.u, s.mass[j + 1]), 0});
+          if (s.count[min(to, j) + 1] - s.count[from] + part.count <= (uint32_t)kCap) {
+            if (to < j) ahead = sel.bins(from, to);
+            else part = sel.bins(min(from, j), j);
+          }
+        }
       }
-      if (!held && part.count > (uint32_t)kCap) {
+      if (held < 0 && part.count > (uint32_t)kCap) {
         part = sel.narrow(b, part);
         ties = part.count > (uint32_t)kCap;
         if (ties) p = sel.in_ties(b, part.r.lo, part.n0, part.sum0, part.count);
-        sel.cumulate(count, mass, 0, 0);   // the row's bins again
       }
     }
-    if (!held && !ties) sel.arrange(sel.gather(part.r), part.r, part.n0, part.sum0);
+    if (held < 0 && !ties) {
+      sel.arrange(sel.gather(part.r, ahead.count > 0, ahead.r), part, ahead);
+      held = 0;
+    }
     if (step < 0) continue;
-    if (!ties) p = sel.in_list(b);
+    if (!ties) p = sel.in_list(b, held);
     if (step < 3 && (p.n < n || step == 0)) {
       n = p.n;
       sum = p.sum;
       if (n < 1) {   // the first one is always kept
         n = 1;
-        sum = (u64)a.unit;
+        sum = a.one;
       }
     }
   }
@@ -828,18 +915,16 @@ __device__ __forceinline__ void select(const SampleArgs& a, int64_t row, float m
   }
 }
 
-// A row to a workgroup.
+// A row to a workgroup, from row `first`.
 template <typename T>
-__global__ void __launch_bounds__(kThreads) sample_kernel(SampleArgs a) {
+__global__ void __launch_bounds__(kThreads) sample_kernel(SampleArgs a, int64_t first) {
   __shared__ Shared s;
-  for (int64_t row = blockIdx.x; row < a.M; row += gridDim.x) {
-    const Asked asked = asked_of(a, row);
-    const float m = histogram(static_cast<const T*>(a.x) + row * a.ld, 0, a.V, asked.c, a.unit, s.h, s.wave_f);
-    __syncthreads();
-    const int mine = kBins - 1 - (int)threadIdx.x;
-    select<T>(a, row, m, asked, s.h.count[mine], s.h.mass[mine], s);
-    __syncthreads();
-  }
+  const int64_t row = first + blockIdx.x;
+  const Asked asked = asked_of(a, row);
+  const float m = histogram(static_cast<const T*>(a.x) + row * a.ld, 0, a.V, asked.c, a.unit, s.h, s.wave_f);
+  __syncthreads();
+  const int mine = kBins - 1 - (int)threadIdx.x;
+  select<T>(a, row, m, asked, s.h.count[mine], s.h.mass[mine], s);
 }
 
 // A part of a row to a workgroup; then a row to a workgroup again.
@@ -896,8 +981,15 @@ int choose_splits(const SampleTokens& c) {
 template <typename T>
 hipError_t launch(const SampleArgs& a, hipStream_t stream) {
   if (a.splits == 1) {
-    sample_kernel<T><<<(unsigned)(a.M < 65535 ? a.M : 65535), kThreads, 0, stream>>>(a);
-    return hipGetLastError();
+    // A launch holds less than 2^32 threads.
+    constexpr int64_t kMostRows = 0xFFFFFFFFll / kThreads;
+    for (int64_t first = 0; first < a.M; first += kMostRows) {
+      const int64_t rows = a.M - first < kMostRows ? a.M - first : kMostRows;
+      sample_kernel<T><<<(unsigned)rows, kThreads, 0, stream>>>(a, first);
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
   }
   const unsigned grid = (unsigned)((a.M + kXcds - 1) / kXcds * kXcds * a.splits);
   sample_histogram_kernel<T><<<grid, kThreads, 0, stream>>>(a);
@@ -926,7 +1018,8 @@ hipError_t launch_sample_tokens(const SampleTokens& c, hipStream_t stream) {
   a.splits = (int)(((int64_t)c.V + a.part - 1) / a.part);
   int e = 46;   // the sum of V weights stays below 2^63
   while (((int64_t)c.V >> (63 - e)) != 0) --e;
-  a.unit = (double)((int64_t)1 << e);
+  a.one = 1ull << e;
+  a.unit = (double)a.one;
   a.u = c.uniform;
   a.temperature = c.temperature;
   a.top_p = c.top_p;

@@ -183,3 +183,24 @@ def test_frequencies_of_drawn_tokens():
     p = torch.softmax(x[0].double(), 0).tolist()
     for t, count in enumerate(torch.bincount(tokens, minlength=5).tolist()):
         assert abs(count - n * p[t]) <= 2
+
+
+@pytest.mark.parametrize("half", [False, True])
+@pytest.mark.parametrize("V", [50304, 131072])
+def test_top_p_of_long_rows(V, half):
+    """Top-p alone, whose border and the token's are in bins of hundreds of tokens, far apart and next to each other."""
+    rng = np.random.default_rng([V, half])
+    u = np.repeat(np.float32([0.01, 0.3, 0.6, 0.9, 0.97, 0.999]), 5)
+    x = np.concatenate([_logits(rng, len(u) // 2, V, half, "usual"),
+                        (2 * rng.standard_normal((len(u) - len(u) // 2, V))).astype(np.float16 if half else np.float32)])
+    _check(x, [dict(top_p=p, temperature=t) for p, t in ((0.5, 1.0), (0.8, 0.7), (0.9, 1.0), (0.95, 1.5), (0.99, 0.5))] * 6,
+           u, V)
+
+
+def test_more_rows_than_a_launch_holds():
+    M = (2 ** 32 - 1) // 1024 + 5
+    x = torch.zeros((M, 2), dtype=torch.float16, device="cuda")
+    x[-7:, 1] = torch.tensor([3.0, -3.0, 3.0, -3.0, 3.0, 3.0, -3.0], device="cuda").half()
+    tokens, probs = dptq.sample_tokens(x, torch.zeros(M, device="cuda"), top_k=1)
+    assert tokens[-7:].tolist() == [1, 0, 1, 0, 1, 1, 0] and int(tokens[:-7].sum()) == 0
+    assert bool((probs == 1).all())
