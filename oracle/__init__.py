@@ -30,6 +30,9 @@ Modules
             and the zero-point correction of the integer GEMM.
   serving   RMS norm with 8-bit codes, the 8-bit paged KV cache and the
             attention over it, log probabilities of tokens.
+  rotary    rotary positions.
+  gated     the gated feed-forward block and the order of its weight rows.
+  sampling  tokens under temperature, top-k, top-p and min-p.
 """
 
 from .hadamard import (sylvester, paley28, hadamard, split_had_size,
