@@ -172,3 +172,32 @@ def test_append_of_many_query_heads(new, interleaved):
         dptq.kv8_append(want_k, v, _d(_cu(new)), n, _d(table), two)
         for a, b in zip(one, two):
             assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_append_in_pieces_of_growing_size(D):
+    """Pages filled by calls of 1 to 70 tokens whose values grow now and then, so that older codes are scaled again from
+    every slot on."""
+    rng = np.random.default_rng(D)
+    B, H, Hkv, P = 2, 4, 2, 12
+    one, two = dptq.kv8_cache(P, Hkv, D), dptq.kv8_cache(P, Hkv, D)
+    for pages in (*one[:2], *two[:2]):
+        pages.view(torch.uint8).fill_(0x7F)      # a new cache's pages hold anything
+    table = _d(np.arange(P, dtype=np.int32)[rng.permutation(P)].reshape(B, P // B))
+    f = dptq.rotary_inv_freq(D // 2)
+    size, start = 2.0 ** -9, np.zeros(B, np.int64)
+    for step, new in enumerate([(1, 5), (1, 1), (3, 0), (6, 2), (8, 1), (1, 9), (20, 16), (24, 31), (1, 64), (70, 1), (5, 3),
+                                (1, 1), (17, 70), (40, 8)]):
+        size *= (1.0, 1.5, 16.0, 0.25)[step % 4]
+        cu, start = _cu(new), start + np.array(new)
+        rows = (size * torch.randn((sum(new), H + 2 * Hkv, D), device="cuda",
+                                   generator=torch.Generator("cuda").manual_seed(step))).half()
+        q, k, v = rows.split([H, Hkv, Hkv], dim=1)
+        n = _d(start.astype(np.int32))
+        positions = _d(np.concatenate([np.arange(e - c, e) for e, c in zip(start, new)]).astype(np.int32))
+        got = dptq.rotary_kv8_append(q, k, v, _d(cu), n, table, one, f, max_new=max(new))
+        want_q, want_k = dptq.rotary(q, k, positions, f)
+        dptq.kv8_append(want_k, v, _d(cu), n, table, two, max_new=max(new))
+        assert torch.equal(got, want_q)
+        for a, b, what in zip(one, two, ("K", "V", "K's scales", "V's scales")):
+            assert torch.equal(a.view(torch.uint8), b.view(torch.uint8)), (step, what)
