@@ -19,7 +19,9 @@
 // it is small or all its values are equal, when index and sum are arithmetic.
 // Where everything down to the lowest border is at most 2048 tokens, which
 // top-k and top-p mostly leave, they are gathered once for all borders; and with a
-// top-p border's bin the bins in which the token's border then lies.
+// top-p border's bin the bins in which the token's border then lies.  A top-k of up
+// to 1024 needs no sums but those of the list: its histogram is of counts alone (256
+// x 128256 fp16: 58 -> 42 us; should the list not hold them, the sums are made then).
 //
 // w in 64 bits: with 131072 tokens of like weight a relative error of 2^-24 in
 // the sums would change one token in a hundred.  2^t = 2^n (1 + f q(f)) with n
@@ -35,7 +37,7 @@
 // 12 for the histograms of four parts each and 22 for the second launch on one
 // compute unit a row: joining and summing the bins 2.5, gathering 7.5 (13 of two
 // ranges), sorting and summing the list 2, and up to four borders in turn, 0.6 each.
-// One row of 32000 takes 18 us, the same chain (21 while every wave went through its
+// One row of 32000 takes 17 us, the same chain (21 while every wave went through its
 // share of a whole span, there or not).  With top-p alone 64 rows of 131072 take 43
 // us: two gatherings took 49, at an addition for each vector and not for four.  No
 // kernel uses scratch memory: with 92 bytes of it 512 rows of 100003 took 116 us for
@@ -269,6 +271,9 @@ struct Asked {
   float u, top_p, min_p;
   uint32_t top_k;  // 0: all
   bool greedy;
+  // Whether the row's sums are needed: not where the list will hold the top_k
+  // tokens, and with them all that is asked for.
+  bool sums;
 };
 __device__ __forceinline__ Asked asked_of(const SampleArgs& a, int64_t row) {
   const float t = a.temperature ? a.temperature[row] : a.temperature_all;
@@ -281,6 +286,7 @@ __device__ __forceinline__ Asked asked_of(const SampleArgs& a, int64_t row) {
   q.c = 1.4426950408889634 / (q.greedy ? 1.0 : (double)t);
   // A top_p of 0 or a min_p above 1 leaves the first one, as a greedy row does.
   q.top_k = q.greedy || q.top_p <= 0.0f || q.min_p > 1.0f ? 1u : k > 0 ? (uint32_t)k : 0u;
+  q.sums = q.top_k == 0 || q.top_k > (uint32_t)kCap / 2;
   return q;
 }
 
@@ -340,9 +346,10 @@ __device__ __forceinline__ V waves_before(const V* part) {
 
 // The histogram of logits [lo, hi) of a row, relative to the largest of them,
 // which it returns: chunk by chunk, and where a larger one comes up the sums so
-// far are scaled down to it.  Barriers: none at the end.
+// far are scaled down to it.  Without `sums` these stay 0.  Barriers: none at the
+// end.
 template <typename T>
-__device__ __forceinline__ float histogram(const T* x, int lo, int hi, double c, double unit, Histogram& h,
+__device__ __forceinline__ float histogram(const T* x, int lo, int hi, double c, double unit, bool sums, Histogram& h,
                                            float (*part)[kWaves]) {
   using R = Reader<T>;
   const int tid = threadIdx.x;
@@ -380,11 +387,18 @@ __device__ __forceinline__ float histogram(const T* x, int lo, int hi, double c,
         atomicAdd(&h.count[b], 1u);
         atomicAdd(&h.mass[b], w);
       };
-      r.each(now, at, [&](uint4 v, int) { values<T>(v, add); });
+      const auto count = [&](float v, int) {
+        if (v > -INFINITY) atomicAdd(&h.count[bin_of(v)], 1u);
+      };
+      if (sums) r.each(now, at, [&](uint4 v, int) { values<T>(v, add); });
+      else r.each(now, at, [&](uint4 v, int) { values<T>(v, count); });
       if (at == 0 && (lo < r.first || hi > r.first + r.vectors * R::kEach)) {
         // The ends' single logits.
-        if constexpr (sizeof(T) == 2) add(__half2float(__ushort_as_half((unsigned short)ends.x)), 0);
-        else add(__uint_as_float(ends.x), 0);
+        float v;
+        if constexpr (sizeof(T) == 2) v = __half2float(__ushort_as_half((unsigned short)ends.x));
+        else v = __uint_as_float(ends.x);
+        if (sums) add(v, 0);
+        else count(v, 0);
       }
     }
     now = next;
@@ -832,12 +846,25 @@ __device__ __forceinline__ void select(const SampleArgs& a, int64_t row, float m
   const int bin_min = kBins - 1 - bin_of(least);
 
   // Which borders there are.  Without both of top-k and top-p, one that is bins
-  // below that of min-p does not count.
+  // below that of min-p does not count.  (Without the sums a border by one is behind
+  // the last token here: a row of at most top_k tokens, all in the list.)
   int bin_first = kBins - 1;
   if (by_k) bin_first = sel.bin_with(Border{By::kCount, k, 0, 0});
   else if (by_p) bin_first = sel.bin_with(Border{By::kSum, 0, below(top_p, s.mass[kBins]), 0});
-  const bool min_first = by_min && !(by_k && by_p) && bin_min < bin_first;
+  const bool min_first = by_min && (by_k ? !by_p : asked.sums) && bin_min < bin_first;
   const int last = min_first ? bin_min : bin_first;
+
+  if (!asked.sums && s.count[last + 1] > (uint32_t)kCap) {
+    // More tokens in the bin than expected: the sums after all.
+    s.h.mass[threadIdx.x] = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < a.V; i += kThreads) {
+      const float v = (float)x[i];
+      if (v > -INFINITY) atomicAdd(&s.h.mass[bin_of(v)], fixed(weight(v, m, asked.c), a.unit));
+    }
+    __syncthreads();
+    sel.cumulate(count, s.h.mass[kBins - 1 - (int)threadIdx.x], 0, 0, s.count, s.mass);
+  }
 
   uint32_t n = all;
   u64 sum = scalar(s.mass[kBins]);
@@ -898,7 +925,10 @@ __device__ __forceinline__ void select(const SampleArgs& a, int64_t row, float m
       sel.arrange(sel.gather(part.r, ahead.count > 0, ahead.r), part, ahead);
       held = 0;
     }
-    if (step < 0) continue;
+    if (step < 0) {
+      if (part.count == all) sum = scalar(s.sum[all - 1]);
+      continue;
+    }
     if (!ties) p = sel.in_list(b, held);
     if (step < 3 && (p.n < n || step == 0)) {
       n = p.n;
@@ -921,7 +951,8 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(SampleArgs a, int64_t 
   __shared__ Shared s;
   const int64_t row = first + blockIdx.x;
   const Asked asked = asked_of(a, row);
-  const float m = histogram(static_cast<const T*>(a.x) + row * a.ld, 0, a.V, asked.c, a.unit, s.h, s.wave_f);
+  const float m =
+      histogram(static_cast<const T*>(a.x) + row * a.ld, 0, a.V, asked.c, a.unit, asked.sums, s.h, s.wave_f);
   __syncthreads();
   const int mine = kBins - 1 - (int)threadIdx.x;
   select<T>(a, row, m, asked, s.h.count[mine], s.h.mass[mine], s);
@@ -940,7 +971,7 @@ __global__ void __launch_bounds__(kThreads) sample_histogram_kernel(SampleArgs a
   if (row >= a.M) return;
   const int lo = split * a.part, hi = min(lo + a.part, a.V);
   const Asked asked = asked_of(a, row);
-  const float m = histogram(static_cast<const T*>(a.x) + row * a.ld, lo, hi, asked.c, a.unit, h, part);
+  const float m = histogram(static_cast<const T*>(a.x) + row * a.ld, lo, hi, asked.c, a.unit, asked.sums, h, part);
   __syncthreads();
   const int64_t at = row * a.splits + split;
   if (threadIdx.x == 0) a.most[at] = m;
