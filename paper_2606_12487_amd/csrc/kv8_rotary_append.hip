@@ -11,13 +11,14 @@
 // The queries are bound by bytes, the pages by their chain of loads (offsets,
 // table, rows) and by the angles, 64-bit products, and all by how many workgroups
 // are resident: loops that are not unrolled and angles by way of LDS, a wave's lanes
-// each a pair's, keep it to 89 registers, five workgroups a CU (four at 256
-// channels).  Each key's octet with its own eight angles had 125 (4500 tokens of
-// three prompts, 64 + 8 heads of 128: 41 us for 35); a page's rows in registers, as
-// kv8_append.hip has them, one workgroup at 256 channels (2 x 1000 tokens of 32 + 32
-// heads: 60 us for 37).  Dropped: four heads of 64 or two of 128 to a workgroup and
-// its angles (39 us; 32 x 152 tokens of 16 + 16 heads of 64 27 for 24): the chains
-// take longer than the angles.
+// each a pair's, keep it to 80 registers, six workgroups a CU (four at 256
+// channels).  Reading the next rows ahead costs eight registers more than it gains
+// (256 single tokens of 32 + 8 heads: 14.5 us for 13).  Each key's octet with its own
+// eight angles had 125 (4500 tokens of three prompts, 64 + 8 heads of 128: 41 us for
+// 35); a page's rows in registers, as kv8_append.hip has them, one workgroup at 256
+// channels (2 x 1000 tokens of 32 + 32 heads: 60 us for 38).  Dropped: four heads of
+// 64 or two of 128 to a workgroup and its angles (39 us; 32 x 152 tokens of 16 + 16
+// heads of 64 27 for 21): the chains take longer than the angles.
 //
 // 4500 tokens of three prompts: 35 us, 4.8 TB/s (rotary alone 33 for 4099 tokens);
 // 64 single tokens: 5.6 (9.5 with an octet's own angles, 7.6 with all eighths of V's
@@ -159,19 +160,14 @@ __device__ __forceinline__ void append_pages(const AppendArgs& a, const Rotary& 
     float top = 0.0f;
     const __half* const row0 = a.x[IS_V] + (int64_t)head * D;
     const int from = lo / kStep * kStep;
-    const auto load = [&](int first) {
-      const int slot = first + tid / kOctets;
-      const int64_t row = (int64_t)q.first_row + ((int64_t)(blk * kPage + slot) - q.start);
-      KeyOctet k{};
-      if (slot >= lo && slot < hi) k = key_octet(r, row0 + row * a.ld[IS_V], c, !IS_V);
-      return k;
-    };
-    KeyOctet next = load(from);
 #pragma unroll 1
     for (int first = from; first < hi; first += kStep) {
       const int slot = first + tid / kOctets;
-      KeyOctet k = next;
-      if (first + kStep < hi) next = load(first + kStep);
+      const int64_t row = (int64_t)q.first_row + ((int64_t)(blk * kPage + slot) - q.start);
+      const __half* const x = row0 + row * a.ld[IS_V];
+      const bool is_new = slot >= lo && slot < hi;
+      KeyOctet k{};
+      if (is_new) k = key_octet(r, x, c, !IS_V);
       if constexpr (!IS_V) {
         // The angles of the wave's tokens.
 #pragma unroll 2
@@ -184,11 +180,8 @@ __device__ __forceinline__ void append_pages(const AppendArgs& a, const Rotary& 
         __builtin_amdgcn_wave_barrier();
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
       }
-      if (slot >= lo && slot < hi) {
-        if constexpr (!IS_V) {
-          const int64_t row = (int64_t)q.first_row + ((int64_t)(blk * kPage + slot) - q.start);
-          k.v = rotate_octet(r, k, row0 + row * a.ld[0], c, mine + lane / kOctets * kPairs);
-        }
+      if (is_new) {
+        if constexpr (!IS_V) k.v = rotate_octet(r, k, x, c, mine + lane / kOctets * kPairs);
         float f[8];
         unpack8(k.v, f);
 #pragma unroll
