@@ -602,8 +602,9 @@ struct Selector {
     __syncthreads();
     const int count = min((int)scalar((uint32_t)s.n), kCap);
     for (int k = threadIdx.x; k < count; k += kThreads) {
-      const int at = (int)s.list[k];
-      s.list[k] = (u64)key_of((float)row[at]) << 32 | (uint32_t)~at;
+      const uint32_t at = (uint32_t)s.list[k];   // V < 2^30: 32 bits of bytes
+      const T v = *reinterpret_cast<const T*>(reinterpret_cast<const char*>(row) + at * (uint32_t)sizeof(T));
+      s.list[k] = (u64)key_of((float)v) << 32 | ~at;
     }
     return count;
   }
