@@ -47,50 +47,20 @@
 // bitonic sort alone (64 rows: 51 us); loops over a chunk's vectors unrolled (the
 // code is 50 KB instead of 20 and comes into the instruction cache first: 54 us).
 #include "internal.h"
+#include "sample_ranges.h"
 #include "wave_device.h"
 
 namespace dptq {
 namespace {
 
+using namespace sampling;
+
 constexpr int kThreads = 1024, kWaves = kThreads / 64;
-constexpr int kBinBits = 10, kBins = 1 << kBinBits;   // one a thread
+static_assert(kBins == kThreads, "a bin a thread");
 constexpr int kCap = 2048;        // tokens that are sorted at once
 // Parts of a row: logits of each, at least, and how many, at most.
 constexpr int kMinPart = 8192, kMaxParts = 8;
 constexpr int kXcds = 8;
-
-// Values as integers in their order; -0 is 0.
-constexpr uint32_t kLowestKey = 0x00800000u;   // of -FLT_MAX; what is not masked is this or above
-__device__ __forceinline__ uint32_t key_of(float x) {
-  const uint32_t u = __float_as_uint(x + 0.0f);
-  return u ^ (u >> 31 ? 0xFFFFFFFFu : 0x80000000u);
-}
-__device__ __forceinline__ float value_of(uint32_t k) {
-  return __uint_as_float(k ^ (k >> 31 ? 0x80000000u : 0xFFFFFFFFu));
-}
-
-// Bins: five bits of the mantissa and 16 octaves, 2^-6 to 2^10, for each sign;
-// smaller magnitudes in the bins at zero, larger ones in the outermost.
-constexpr int kBinShift = 18, kBinBase = (127 - 6) << 5;
-// Of a value that counts, and of its key.
-__device__ __forceinline__ int bin_of(float x) {
-  const uint32_t u = __float_as_uint(x + 0.0f);   // -0 is 0
-  const int q = (int)(u << 1 >> (kBinShift + 1)) - kBinBase;
-  const int c = min(max(q, 0), kBins / 2 - 1);
-  return c ^ ((int)u >> 31 & (kBins - 1)) ^ kBins / 2;   // negative: kBins / 2 - 1 - c
-}
-__device__ __forceinline__ int bin_of(uint32_t k) { return bin_of(value_of(k)); }
-struct Range {
-  uint32_t lo, hi;   // keys, both in it
-};
-__device__ __forceinline__ Range range_of(int bin) {
-  const bool positive = bin >= kBins / 2;
-  const int c = positive ? bin - kBins / 2 : kBins / 2 - 1 - bin;
-  const uint32_t a = c == 0 ? 0 : (uint32_t)(c + kBinBase) << kBinShift;
-  const uint32_t b = c == kBins / 2 - 1 ? 0x7F800000u : ((uint32_t)(c + kBinBase + 1) << kBinShift) - 1;
-  if (positive) return Range{a | 0x80000000u, b | 0x80000000u};
-  return Range{b == 0x7F800000u ? kLowestKey : 0x7FFFFFFFu - b, 0x7FFFFFFFu - a};   // magnitudes a to b, negative
-}
 
 // a b + c with c in scalar registers: as an FMA of three operands; the compiler
 // keeps the constants in vector registers and copies each before its FMA.
@@ -204,12 +174,18 @@ __device__ __forceinline__ void values(uint4 v, const F& f) {
   }
 }
 
-// Which values of a vector lie in [least, most], as bits; element(b): which value
-// a bit is.  NaN does not; -0 is 0.
+// A value that all lanes have, in a scalar register.
+__device__ __forceinline__ uint32_t scalar(uint32_t x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ u64 scalar(u64 x) {
+  return (u64)scalar((uint32_t)(x >> 32)) << 32 | scalar((uint32_t)x);
+}
+
+// Which values of a vector lie in a range, as bits; element(b): which value a bit
+// is.  NaN does not; -0 is 0.
 template <typename T>
 struct Within {
   float least, most;
-  __device__ __forceinline__ Within(float lo, float hi) : least(lo), most(hi) {}
+  __device__ __forceinline__ explicit Within(Range r) : least(value_of(r.lo)), most(value_of(r.hi)) {}
   __device__ __forceinline__ uint32_t marks(uint4 v) const {
     uint32_t m = 0;
     values<T>(v, [&](float e, int j) { m |= e >= least && e <= most ? 1u << j : 0u; });
@@ -217,15 +193,16 @@ struct Within {
   }
   __device__ __forceinline__ static int element(int b) { return b & 3; }
 };
-// fp16: two at a time, those that clamping to the bounds (rounded into the range)
-// leaves as they are.
+// fp16: two at a time, those that clamping to the range's least and most fp16
+// number leaves as they are.
 template <>
 struct Within<__half> {
   typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
   typedef unsigned short ushort2_t __attribute__((ext_vector_type(2)));
   half2_t least, most;
-  __device__ __forceinline__ Within(float lo, float hi) {
-    const unsigned short l = __half_as_ushort(__float2half_ru(lo)), h = __half_as_ushort(__float2half_rd(hi));
+  __device__ __forceinline__ explicit Within(Range r) {
+    const HalfRange in = halves_of(Range{scalar(r.lo), scalar(r.hi)});
+    const unsigned short l = half_bits(in.least), h = half_bits(in.most);
     const ushort2_t a = {l, l}, b = {h, h};
     least = __builtin_bit_cast(half2_t, a);
     most = __builtin_bit_cast(half2_t, b);
@@ -315,12 +292,6 @@ struct Shared {
   float wave_f[2][kWaves];
   int n, found;
 };
-
-// A value that all lanes have, in a scalar register.
-__device__ __forceinline__ uint32_t scalar(uint32_t x) { return __builtin_amdgcn_readfirstlane(x); }
-__device__ __forceinline__ u64 scalar(u64 x) {
-  return (u64)scalar((uint32_t)(x >> 32)) << 32 | scalar((uint32_t)x);
-}
 
 // The sum of the waves before this one, of each wave's value (lane 63's), in
 // part; a barrier comes before the reads, and the callers alternate between two
@@ -555,7 +526,7 @@ struct Selector {
     __syncthreads();   // the list's readers are done
     if (threadIdx.x == 0) s.n = 0;
     __syncthreads();
-    const Within<T> within(value_of(r.lo), value_of(r.hi)), within2(value_of(r2.lo), value_of(r2.hi));
+    const Within<T> within(r), within2(r2);
     using R = Reader<T>;
     // The row's address is made anew: the compiler would keep those of all loads over
     // the selection's steps, and spill others for them.
@@ -842,7 +813,7 @@ __device__ __forceinline__ void select(const SampleArgs& a, int64_t row, float m
       if (first > 0) lo = key(first);
       hi = next;
     }
-    least = hi;
+    least = key_of(value_of(hi));   // -0 is 0
   }
   const int bin_min = kBins - 1 - bin_of(least);
 
