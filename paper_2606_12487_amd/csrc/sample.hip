@@ -194,16 +194,19 @@ struct Within {
   __device__ __forceinline__ static int element(int b) { return b & 3; }
 };
 // fp16: two at a time, those that clamping to the range's least and most fp16
-// number leaves as they are.
+// number leaves as they are; none where no number lies in the range, as clamping
+// leaves `most` as it is there.
 template <>
 struct Within<__half> {
   typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
   typedef unsigned short ushort2_t __attribute__((ext_vector_type(2)));
   half2_t least, most;
+  uint32_t all;   // the bits of a vector's values
   __device__ __forceinline__ explicit Within(Range r) {
     const HalfRange in = halves_of(Range{scalar(r.lo), scalar(r.hi)});
     const unsigned short l = half_bits(in.least), h = half_bits(in.most);
     const ushort2_t a = {l, l}, b = {h, h};
+    all = in.least <= in.most ? 0x000F000Fu : 0;
     least = __builtin_bit_cast(half2_t, a);
     most = __builtin_bit_cast(half2_t, b);
   }
@@ -218,7 +221,7 @@ struct Within<__half> {
       const ushort2_t d = __builtin_bit_cast(ushort2_t, __builtin_bit_cast(uint32_t, c) ^ __builtin_bit_cast(uint32_t, e));
       out |= __builtin_bit_cast(uint32_t, __builtin_elementwise_min(d, one)) << k;
     }
-    return ~out & 0x000F000Fu;
+    return ~out & all;
   }
   __device__ __forceinline__ static int element(int b) { return 2 * (b & 3) + (b >> 4); }
 };
@@ -588,7 +591,7 @@ struct Selector {
     constexpr int E = kCap / kThreads, kCrowd = 64;
     uint32_t* const offset = reinterpret_cast<uint32_t*>(s.h.mass);   // [kBins + 1]
     const int tid = threadIdx.x;
-    const int shift = max(32 - kBinBits - __clz((int)(r.hi - r.lo - gap)), 0);
+    const Buckets buckets = buckets_of(r, split, gap);
     s.h.count[tid] = 0;
     if (tid == 0) s.found = 0;
     __syncthreads();
@@ -599,8 +602,7 @@ struct Selector {
       const int i = e * kThreads + tid;
       if (i >= count) continue;
       v[e] = s.list[i];
-      const uint32_t key = (uint32_t)(v[e] >> 32);
-      bucket[e] = (r.hi - key - (key < split ? gap : 0)) >> shift;
+      bucket[e] = bucket_of(buckets, (uint32_t)(v[e] >> 32));
       place[e] = atomicAdd(&s.h.count[bucket[e]], 1u);
       if (place[e] >= (uint32_t)kCrowd) s.found = 1;
     }
@@ -846,7 +848,7 @@ __device__ __forceinline__ void select(const SampleArgs& a, int64_t row, float m
     Border b{};
     typename Selector<T>::Part part{}, ahead{};
     int held = -1;
-    bool ties = false;
+    bool placed = false;
     if (step < 0) {
       // All that the borders can need, if it is little.
       part = {Range{range_of(kBins - 1 - last).lo, key_of(m)}, 0, scalar(s.count[last + 1]), 0};
@@ -889,11 +891,17 @@ __device__ __forceinline__ void select(const SampleArgs& a, int64_t row, float m
       }
       if (held < 0 && part.count > (uint32_t)kCap) {
         part = sel.narrow(b, part);
-        ties = part.count > (uint32_t)kCap;
-        if (ties) p = sel.in_ties(b, part.r.lo, part.n0, part.sum0, part.count);
+        placed = part.count > (uint32_t)kCap;
+        if (placed) p = sel.in_ties(b, part.r.lo, part.n0, part.sum0, part.count);
+      }
+      // No token in a border's range (a min-p border's, and most stretches of one that
+      // is cut are empty): it stands behind those before the range.
+      if (held < 0 && part.count == 0) {
+        placed = true;
+        p = Place{part.n0, part.sum0, 0, -1};
       }
     }
-    if (held < 0 && !ties) {
+    if (held < 0 && !placed) {
       sel.arrange(sel.gather(part.r, ahead.count > 0, ahead.r), part, ahead);
       held = 0;
     }
@@ -901,7 +909,7 @@ __device__ __forceinline__ void select(const SampleArgs& a, int64_t row, float m
       if (part.count == all) sum = scalar(s.sum[all - 1]);
       continue;
     }
-    if (!ties) p = sel.in_list(b, held);
+    if (!placed) p = sel.in_list(b, held);
     if (step < 3 && (p.n < n || step == 0)) {
       n = p.n;
       sum = p.sum;

@@ -58,7 +58,8 @@ constexpr int half_within(uint32_t a) {
 }
 constexpr int half_beyond(uint32_t a) { return a ? half_within(a - 1) + 1 : 0; }
 
-// The fp16 numbers of a range: least to most, as magnitudes with their sign.
+// The fp16 numbers of a range: least to most, as magnitudes with their sign; least
+// above most where none lies in it.
 struct HalfRange {
   int least, most;
 };
@@ -69,6 +70,24 @@ constexpr HalfRange halves_of(Range r) {
 }
 constexpr uint16_t half_bits(int magnitude) {
   return (uint16_t)(magnitude < 0 ? 0x8000 - magnitude : magnitude);
+}
+
+// Which of kBins stretches of a range (without the `gap` keys below `split`), from
+// its upper end, a key is in.  A key that is not in the range, as of a row that
+// changes between two readings, gets one of them too.
+struct Buckets {
+  Range r;
+  uint32_t split, gap;
+  int shift;
+};
+constexpr Buckets buckets_of(Range r, uint32_t split, uint32_t gap) {
+  const uint32_t keys = r.hi - r.lo - gap;   // and one
+  const int bits = keys ? 32 - __builtin_clz(keys) : 0;
+  return Buckets{r, split, gap, bits > kBinBits ? bits - kBinBits : 0};
+}
+constexpr uint32_t bucket_of(const Buckets& b, uint32_t key) {
+  const uint32_t i = (b.r.hi - key - (key < b.split ? b.gap : 0)) >> b.shift;
+  return i < kBins ? i : kBins - 1;
 }
 
 }  // namespace sampling

@@ -25,6 +25,7 @@ def check(tmp_path_factory):
 
 def test_ranges_hold_their_values_and_no_others(check):
     """Every bin, and stretches of bins down to single keys: what a comparison with a range's ends takes is what its
-    keys are; zeros of both signs belong to the bin above them."""
+    keys are, none where no fp16 value lies between them; zeros of both signs belong to the bin above them.  Places
+    for sorting are in order, and in bounds for any key."""
     r = subprocess.run([check], capture_output=True, text=True, timeout=100)
     assert r.returncode == 0 and r.stdout == "", r.stdout
