@@ -623,8 +623,8 @@ def rotary_inv_freq(rotary_dim, base=10000.0, factor=1.0, original_length=None, 
     """Frequencies of rotary positions: float64 [rotary_dim / 2], base ** (-2 i / rotary_dim).  For contexts `factor`
     times as long as those of the training: divided by factor; with original_length, the length trained for, only
     where a pair turns at most low_turns times over it, not at all where it turns high_turns times or more, and in
-    between in proportion to the turns (ramp "turns") or to i (ramp "index", from the whole i below high_turns to the
-    one above low_turns)."""
+    between in proportion to the turns (ramp "turns") or to i (ramp "index", from the last i with high_turns or more
+    to the first with low_turns or fewer, within 0 and rotary_dim - 1: the ramp may end behind the last pair)."""
     if rotary_dim < 2 or rotary_dim % 2:
         raise ValueError("rotary_dim must be even and positive")
     if not (base > 1 and factor > 0):
@@ -641,7 +641,7 @@ def rotary_inv_freq(rotary_dim, base=10000.0, factor=1.0, original_length=None, 
         turns = original_length / (2 * math.pi)    # of a pair of frequency 1
         if ramp == "index":                        # f = turns^-1 t at index n log(turns / t) / log(base)
             first, last = (n * math.log(turns / t) / math.log(base) for t in (high_turns, low_turns))
-            first, last = max(math.floor(first), 0), min(math.ceil(last), n - 1)
+            first, last = max(math.floor(first), 0), min(math.ceil(last), rotary_dim - 1)
             kept = [1 - (i - first) / max(last - first, 1e-3) for i in range(n)]
         else:
             kept = [(x * turns - low_turns) / (high_turns - low_turns) for x in f]
