@@ -465,7 +465,9 @@ int dptq_kv8_append(const void* k, int64_t ld_k, const void* v, int64_t ld_v, in
  *   rotary_dim even, 2 <= rotary_dim <= head_dim
  *   scale      finite
  *   q_out, k_out  device, fp16 outputs, ld_q_out and ld_k_out as ld_q: q and k
- *              themselves (with the same ld), or memory that does not overlap them
+ *              themselves (with the same ld), or rows apart from those of q, k and
+ *              the other output, else DPTQ_ERR_INVALID_ARG.  Rows of unequal ld
+ *              count as overlapping where their extents (first to last element) do
  */
 int dptq_rotary(const void* q, int64_t ld_q, int32_t heads, const void* k, int64_t ld_k, int32_t kv_heads,
                 int64_t T, int32_t head_dim, const int32_t* positions, const double* inv_freq,
@@ -480,7 +482,8 @@ int dptq_rotary(const void* q, int64_t ld_q, int32_t heads, const void* k, int64
  * Token row cu_seqlens[b] + i is at position lengths[b] - (new tokens of b) + i,
  * of q as of k; q is rotated whether or not the token's page is there.  Rows
  * that cu_seqlens gives to no sequence are not written in q_out.  k itself is
- * only read.  Arguments as for the two calls; head_dim as for the cache.
+ * only read.  Arguments as for the two calls; head_dim as for the cache; q_out is
+ * q itself or apart from q, k and v, as for dptq_rotary.
  */
 int dptq_rotary_kv8_append(const void* q, int64_t ld_q, int32_t heads, const void* k, int64_t ld_k,
                            const void* v, int64_t ld_v, int64_t T, const int32_t* cu_seqlens,

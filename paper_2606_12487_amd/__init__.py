@@ -654,7 +654,7 @@ def rotary(q, k, positions, inv_freq, interleaved=False, scale=1.0, q_out=None, 
     """Rotary positions on queries and keys (fp16 [T, heads, head_dim]; rows may be parts of wider ones; k may be
     None) -> (q_out, k_out).  positions int32 [T]; inv_freq float64 [r / 2] (rotary_inv_freq): of each head the first r
     channels turn, in pairs (i, i + r / 2), or (2i, 2i + 1) where interleaved, by positions * inv_freq[i].  scale: of
-    the channels that turn.  q_out, k_out may be q and k."""
+    the channels that turn.  q_out and k_out may be q and k; other outputs that overlap what is read are refused."""
     return _binding().rotary(q, k, positions, inv_freq, interleaved, scale, q_out, k_out)
 
 
@@ -662,7 +662,8 @@ def rotary_kv8_append(q, k, v, cu_seqlens, lengths, page_table, cache, inv_freq,
                       max_new=None, q_out=None):
     """rotary and kv8_append in one launch, with the same bits: rotates the new tokens' queries into q_out, which it
     returns, and writes their rotated keys and their values into the cache, in place.  Positions are those of the
-    tokens in their sequences; q_out may be q, and its rows that cu_seqlens gives to no sequence are not written."""
+    tokens in their sequences; q_out may be q, but not overlap k or v, and its rows that cu_seqlens gives to no
+    sequence are not written."""
     return _binding().rotary_kv8_append(q, k, v, cu_seqlens, lengths, page_table, *cache, inv_freq, interleaved, scale,
                                         max_new, q_out)
 

@@ -89,6 +89,29 @@ bool kv8_pointers(const dptq::Kv8Cache& c) {
 // Rows of n elements, ld apart, that 16-byte loads take.
 bool rows_ok(const void* p, int64_t ld, int64_t n) { return p && aligned16(p) && ld >= n && ld % 8 == 0; }
 
+// T rows of n fp16 elements, ld apart.
+struct Rows {
+  const void* p;
+  int64_t ld, n;
+};
+
+// Whether no element is in a row of both.  Rows of equal distance are compared by
+// where they stand in it; of unequal ones all between the first and the last
+// element counts.
+bool apart(const Rows& a, const Rows& b, int64_t T) {
+  if (reinterpret_cast<uintptr_t>(a.p) > reinterpret_cast<uintptr_t>(b.p)) return apart(b, a, T);
+  using wide = unsigned __int128;
+  const wide d = reinterpret_cast<uintptr_t>(b.p) - reinterpret_cast<uintptr_t>(a.p);   // bytes
+  const wide ld = 2 * (wide)a.ld, n_a = 2 * (wide)a.n, n_b = 2 * (wide)b.n;
+  if (d >= (wide)(T - 1) * ld + n_a) return true;
+  return T > 1 && a.ld == b.ld && d % ld >= n_a && ld - d % ld >= n_b;
+}
+
+// An output of rotary positions beside rows that are read: the same rows, or apart.
+bool in_place_or_apart(const Rows& out, const Rows& in, int64_t T) {
+  return (out.p == in.p && out.ld == in.ld && out.n == in.n) || apart(out, in, T);
+}
+
 // The sizes of a kv8_attention call; max_q and max_len within what T and the
 // page table allow.
 int attention_shape(int64_t T, int64_t B, int64_t max_pages, int64_t num_pages, int32_t heads, int32_t kv_heads,
@@ -583,7 +606,10 @@ int dptq_rotary(const void* q, int64_t ld_q, int32_t heads, const void* k, int64
   if (!rows_ok(q, ld_q, row) || !rows_ok(q_out, ld_q_out, row)) return DPTQ_ERR_INVALID_ARG;
   if (kv_heads > 0 && (!rows_ok(k, ld_k, kv_row) || !rows_ok(k_out, ld_k_out, kv_row))) return DPTQ_ERR_INVALID_ARG;
   if (!positions || !inv_freq || !aligned4(positions) || !aligned8(inv_freq)) return DPTQ_ERR_INVALID_ARG;
-  if ((q == q_out && ld_q != ld_q_out) || (kv_heads > 0 && k == k_out && ld_k != ld_k_out))
+  const Rows rq{q, ld_q, row}, rq_out{q_out, ld_q_out, row}, rk{k, ld_k, kv_row}, rk_out{k_out, ld_k_out, kv_row};
+  if (!in_place_or_apart(rq_out, rq, T)) return DPTQ_ERR_INVALID_ARG;
+  if (kv_heads > 0 && !(in_place_or_apart(rk_out, rk, T) && apart(rq_out, rk, T) && apart(rk_out, rq, T) &&
+                        apart(rq_out, rk_out, T)))
     return DPTQ_ERR_INVALID_ARG;
   const dptq::RotaryCall c{q, k, q_out, k_out, ld_q, ld_k, ld_q_out, ld_k_out, T, heads, kv_heads,
                            head_dim, rotary_dim, positions, inv_freq, interleaved != 0, scale};
@@ -606,9 +632,12 @@ int dptq_rotary_kv8_append(const void* q, int64_t ld_q, int32_t heads, const voi
                          T, B, max_pages, num_pages, kv_heads, head_dim};
   const int64_t row = (int64_t)heads * head_dim, kv_row = (int64_t)kv_heads * head_dim;
   if (!kv8_pointers(c) || !rows_ok(k, ld_k, kv_row) || !rows_ok(v, ld_v, kv_row)) return DPTQ_ERR_INVALID_ARG;
-  if (!rows_ok(q, ld_q, row) || !rows_ok(q_out, ld_q_out, row) || (q == q_out && ld_q != ld_q_out))
-    return DPTQ_ERR_INVALID_ARG;
+  if (!rows_ok(q, ld_q, row) || !rows_ok(q_out, ld_q_out, row)) return DPTQ_ERR_INVALID_ARG;
   if (!inv_freq || !aligned8(inv_freq)) return DPTQ_ERR_INVALID_ARG;
+  const Rows rq_out{q_out, ld_q_out, row};
+  if (!in_place_or_apart(rq_out, Rows{q, ld_q, row}, T) || !apart(rq_out, Rows{k, ld_k, kv_row}, T) ||
+      !apart(rq_out, Rows{v, ld_v, kv_row}, T))
+    return DPTQ_ERR_INVALID_ARG;
   const dptq::RotaryCall r{q, k, q_out, nullptr, ld_q, ld_k, ld_q_out, 0, T, heads, kv_heads,
                            head_dim, rotary_dim, nullptr, inv_freq, interleaved != 0, scale};
   return from_hip(dptq::launch_rotary_kv8_append(c, r, v, ld_v, max_new > 0 && max_new < T ? max_new : T,
