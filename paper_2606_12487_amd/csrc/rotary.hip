@@ -62,9 +62,7 @@ Rotary make_rotary(const double* inv_freq, int D, int rotary_dim, bool interleav
   r.interleaved = interleaved;
   r.wide = rotary_dim % (interleaved ? 8 : 16) == 0;
   r.units = !r.wide ? D - r.half : interleaved ? D / 8 : (D - r.half) / 8;
-  const auto inverse = [](int n) { return n > 1 ? (uint32_t)((((uint64_t)1 << 32) + n - 1) / n) : 0u; };
-  r.units_inv = inverse(r.units);
-  r.half_inv = inverse(r.half);
+  r.units_inv = r.units > 1 ? (uint32_t)((((uint64_t)1 << 32) + r.units - 1) / r.units) : 0u;
   return r;
 }
 

@@ -27,7 +27,6 @@ struct Rotary {
   bool wide;                // the pairs' octets of channels are whole: 16-byte loads
   int units;                // of a head: an octet of pairs (wide) or a pair, and what is only copied
   uint32_t units_inv;       // ceil(2^32 / units); 0 for one unit
-  uint32_t half_inv;        // the same of half
 };
 // rotary_dim even, at most D; D a multiple of 8, at most kMaxRotaryHead (rotary.hip).
 Rotary make_rotary(const double* inv_freq, int D, int rotary_dim, bool interleaved, float scale);
