@@ -698,8 +698,9 @@ def token_logprobs(logits, tokens, top=0, logprobs=None, entropy=None, top_logpr
 def sample_tokens(logits, uniform, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, tokens=None, probs=None):
     """One token of each row of logits (fp16 or fp32 [M, V]; rows may be parts of wider ones), drawn from the given
     uniform numbers (float32 [M], in [0, 1)): (tokens int64 [M], probs fp32 [M], the token's probability among those
-    that are left).  Each parameter is a number or a tensor [M] (float32; top_k int32).  In this order: the top_k
-    largest logits stay (0: all), of these the likeliest up to a probability of top_p, of these the ones at least min_p
-    times as likely as the first; then the likeliest tokens up to a probability of `uniform`, the last of which is
-    taken.  Temperature 0: the largest logit.  Logits of -inf are masked; a row of nothing else gives -1."""
+    that are left).  Each parameter is a number, not negative, or a tensor [M] (float32; top_k int32), where what is
+    negative counts as 0.  In this order: the top_k largest logits stay (0: all), of these the likeliest up to a
+    probability of top_p, of these the ones at least min_p times as likely as the first; then the likeliest tokens up to
+    a probability of `uniform`, the last of which is taken.  Temperature 0: the largest logit.  Logits of -inf are
+    masked; a row of nothing else gives -1."""
     return _binding().sample_tokens(logits, uniform, temperature, top_k, top_p, min_p, tokens, probs)

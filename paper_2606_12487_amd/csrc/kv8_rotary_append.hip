@@ -20,7 +20,8 @@
 // 64 or two of 128 to a workgroup and its angles (39 us; 32 x 152 tokens of 16 + 16
 // heads of 64 27 for 21): the chains take longer than the angles.
 //
-// 4500 tokens of three prompts: 35 us, 4.8 TB/s (rotary alone 33 for 4099 tokens);
+// 4500 tokens of three prompts: 37 us, 4.5 TB/s (35 to 38 on several cards; rotary
+// alone 33 for 4099 tokens);
 // 64 single tokens: 5.6 (9.5 with an octet's own angles, 7.6 with all eighths of V's
 // page looked through for the one that changes).
 #include "internal.h"

@@ -5,7 +5,7 @@
 // two 16-byte loads and stores).  It computes the token's angles once, a lane
 // each, into LDS, and every head reads them there.
 //
-// Bound by bytes: 4099 tokens of 64 + 8 heads of 128 take 32 us, 4.7 TB/s.  Loads and
+// Bound by bytes: 4099 tokens of 64 + 8 heads of 128 take 33 us, 4.6 TB/s.  Loads and
 // stores that do not stay in the caches take 29.5 us, but between a producer of the
 // rows and a reader of the result nothing is left of it (4099 tokens 78.4 for 78.7 us
 // of all three, 2048 tokens 39.7 for 37.9).
